@@ -75,7 +75,7 @@
 extern "C" {
 #endif
 
-#define FASTBFP_ABI_VERSION 7
+#define FASTBFP_ABI_VERSION 8
 
 typedef enum {
   BFP_ROUND_NEAREST = 0,    /* add half an LSB, then truncate (ties away from zero) */
@@ -563,6 +563,120 @@ double bfp_adaptive_threshold(double alpha, double beta, int64_t i, int64_t I, i
  * bfp_quantize_adaptive.
  */
 int bfp_adaptive_mantissa(double num, double den, double eps);
+
+/*
+ * The expert layer: a linear layer of which each token takes the weights of a
+ * few experts (a mixture of experts), trained and served in BFP like the dense
+ * one.  A slot is one choice of one token: slot = token * top + j, tokens * top
+ * of them.  A plan of the routing puts the slots in the order of their experts;
+ * with it
+ *   forward    bfp_quantize_experts (rows) and bfp_gemm_experts with W;
+ *   backward   bfp_quantize_experts (both groupings of dY, the token grouping of
+ *              X), bfp_gemm_experts with W grouped along its outputs for dX, and
+ *              bfp_gemm_experts_grad for dW;
+ *   around it  bfp_combine_experts and bfp_combine_experts_grad.
+ * The weights of all experts are one BFP tensor of experts * N rows, expert e's
+ * at e * N.  Experts without a token and dropped choices are ordinary input.
+ * experts is 1 .. 512 and tokens * top < 2^31 - 2^20 (BFP_E_UNSUPPORTED beyond).
+ * A plan's arrays are device data that the host does not read: the kernels clamp
+ * what they find there to the buffers whose sizes they are given.
+ */
+
+/* Host-side sizes for a routing of tokens * top slots over experts: the length
+ * of the token grouping (a multiple of 128 that every such routing fits), and
+ * the bytes of bfp_expert_plan's workspace (0: none). */
+int bfp_expert_plan_sizes(int64_t tokens, int top, int experts, int64_t* places, size_t* workspace_bytes);
+
+/*
+ * bfp_expert_plan -- the slots sorted by expert (stable: the slots of an expert
+ * stay in order).
+ *   ids        : int32 or int64 (ids_bits 32 or 64) [tokens][top], the expert of
+ *                each slot; any value outside [0, experts) is a dropped choice.
+ *   offsets    : int32 [experts + 1]: expert e's slots are order[offsets[e]] ..
+ *                order[offsets[e+1] - 1]; the dropped ones follow.
+ *   k_offsets  : int32 [experts + 1]: where expert e's places in the token
+ *                grouping begin, each a multiple of 128.
+ *   order      : int32 [tokens * top], the slots in that order.
+ *   place      : int32 [tokens * top], where each slot went: order[place[i]] = i.
+ *   workspace  : bfp_expert_plan_sizes bytes, 4-byte aligned; overwritten.
+ */
+int bfp_expert_plan(const void* ids, int ids_bits, int64_t tokens, int top, int experts, int32_t* offsets,
+                    int32_t* k_offsets, int32_t* order, int32_t* place, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/*
+ * bfp_quantize_experts -- FP32 -> BFP (as bfp_quantize, groups of 16) of the
+ * rows of an expert layer, in the experts' order, from one read:
+ *   mant_r, exp_r : optional (both or neither NULL): the row grouping, rows =
+ *                tokens * top, len = C: row p is slot order[p]'s.  Rows of
+ *                dropped slots are unspecified (the products do not read them).
+ *   mant_c, exp_c : optional: the token grouping, rows = C, len = places: expert
+ *                e's slots one after another from place k_offsets[e], zeros in
+ *                every other place, so that no group holds slots of two experts.
+ *   x          : FP32 [rows][C], row-major, contiguous, 16-byte aligned.  gather
+ *                = 1: the tokens (rows = tokens), slot i reads row i / top.
+ *                gather = 0: the slots in the experts' order (rows = tokens *
+ *                top).
+ *   C          : a multiple of 16 (BFP_E_SHAPE otherwise), below 2^22.
+ *   m_bits, round_mode, status_word : as bfp_quantize; seed_r and seed_c are the
+ *                seeds of the two outputs, gid a group's index in its exp.
+ * Outputs sized by bfp_quantized_sizes(tokens * top, C, 16, m_bits) and (C,
+ * places, 16, m_bits).  tokens * top * C / 16 and C * places / 16 below 2^31
+ * (BFP_E_UNSUPPORTED otherwise).
+ */
+int bfp_quantize_experts(const float* x, int64_t C, int gather, const int32_t* order, const int32_t* offsets,
+                         const int32_t* k_offsets, int64_t tokens, int top, int experts, int m_bits, int round_mode,
+                         uint64_t seed_r, uint64_t seed_c, uint8_t* mant_r, uint8_t* exp_r, uint8_t* mant_c,
+                         uint8_t* exp_c, uint32_t* status_word, void* stream);
+
+/*
+ * bfp_gemm_experts -- the products of experts (bfp_gemm for each, in one launch):
+ *   C[p][n] = sum over k of A[p][k] B[e N + n][k]  for offsets[e] <= p < offsets[e+1],
+ * and zeros in the rows of dropped slots.
+ *   A          : BFP [slots][K], B: BFP [experts * N][K], groups of 16; stored at
+ *                a_m_bits and b_m_bits, used at m_a and m_b: the stored width, or
+ *                that less the low chunk plane (BFP_E_UNSUPPORTED otherwise:
+ *                bfp_repack makes such an operand).
+ *   C          : FP32, row stride ldc >= N, 4-byte aligned.
+ * Products are exact, sums over groups FP32, as in bfp_gemm; their order depends
+ * on the sizes alone, not on the routing.  Size limits as bfp_gemm.
+ */
+int bfp_gemm_experts(const uint8_t* a_mant, const uint8_t* a_exp, int a_m_bits, const uint8_t* b_mant,
+                     const uint8_t* b_exp, int b_m_bits, const int32_t* offsets, int experts, int64_t slots, int64_t N,
+                     int64_t K, int m_a, int m_b, float* C, int64_t ldc, void* stream);
+
+/*
+ * bfp_gemm_experts_grad -- the weight gradients of experts:
+ *   C[e][i][j] = sum over the places k of expert e of A[i][k] B[j][k],
+ * with A [M][places] and B [N][places] the token groupings that
+ * bfp_quantize_experts writes (exponents 4-byte aligned); zeros for an expert
+ * without slots.
+ *   C          : FP32 [experts][M][N], contiguous.
+ * The rest as bfp_gemm_experts.
+ */
+int bfp_gemm_experts_grad(const uint8_t* a_mant, const uint8_t* a_exp, int a_m_bits, const uint8_t* b_mant,
+                          const uint8_t* b_exp, int b_m_bits, const int32_t* k_offsets, int experts, int64_t M,
+                          int64_t N, int64_t places, int m_a, int m_b, float* C, void* stream);
+
+/*
+ * bfp_combine_experts -- out[t][n] = sum over j of gates[t][j] y[place[t top + j]][n]
+ * in FP32, in the order of j; dropped choices add nothing.
+ *   y          : FP32 [tokens * top][N], in the experts' order; out FP32 [tokens][N].
+ *   gates      : FP32 [tokens][top], or NULL for ones.
+ */
+int bfp_combine_experts(const float* y, const float* gates, const int32_t* place, const int32_t* offsets,
+                        int64_t tokens, int top, int experts, int64_t N, float* out, void* stream);
+
+/*
+ * bfp_combine_experts_grad -- its gradients: dy[place[i]][n] = gates[i] dout[i /
+ * top][n] and dgates[i] = sum over n of dout[i / top][n] y[place[i]][n] for every
+ * slot i, zeros for dropped ones.
+ *   dgates     : FP32 [tokens][top], or NULL.  gates as above.
+ *   dy must not overlap y or dout.
+ */
+int bfp_combine_experts_grad(const float* dout, const float* y, const float* gates, const int32_t* place,
+                             const int32_t* offsets, int64_t tokens, int top, int experts, int64_t N, float* dy,
+                             float* dgates, void* stream);
 
 #ifdef __cplusplus
 }

@@ -25,7 +25,8 @@ from ._lib import BFPError, check, load
 __all__ = ["BFPTensor", "BFPError", "quantize", "quantize_dual", "weight_update", "dequantize", "gemm", "gemm_bfp",
            "gemm_group_partials", "quantize_adaptive", "quantize_adaptive_noalloc", "adaptive_threshold", "adaptive_mantissa", "chunks", "quantized_sizes", "ROUNDING",
            "PackedBFPTensor", "packed_sizes", "quantize_packed", "dequantize_packed", "gemm_packed", "repack",
-           "gemm_ws_size"]
+           "gemm_ws_size", "ExpertPlan", "expert_plan", "quantize_experts", "gemm_experts", "gemm_experts_grad",
+           "combine_experts", "combine_experts_grad"]
 
 ROUNDING = {"nearest": 0, "stochastic": 1, "truncate": 2}
 
@@ -551,3 +552,225 @@ def gemm_packed(A: PackedBFPTensor, B: PackedBFPTensor, m_a: int | None = None, 
                                  B.rows, A.len, m_a, m_b, C.data_ptr(), C.stride(0),
                                  _stream(A.device)), "bfp_gemm_packed")
     return C
+
+
+# ---- the expert layer -----------------------------------------------------
+
+
+@dataclass
+class ExpertPlan:
+    """A routing's slots in the order of their experts (see include/fastbfp.h).
+    Slot token * top + j is the j-th choice of a token.
+
+    offsets   int32 [experts + 1]: expert e's slots are order[offsets[e]:offsets[e + 1]];
+              dropped choices follow the last one's.
+    k_offsets int32 [experts + 1]: where expert e's places in the token grouping begin.
+    order     int32 [slots]: the slots in that order.
+    place     int32 [slots]: where each slot went.
+    places    length of the token grouping.
+    """
+    tokens: int
+    top: int
+    experts: int
+    places: int
+    data: torch.Tensor  # offsets, k_offsets, order and place, one after another
+
+    @property
+    def slots(self) -> int:
+        return self.tokens * self.top
+
+    @property
+    def device(self) -> torch.device:
+        return self.data.device
+
+    @property
+    def offsets(self) -> torch.Tensor:
+        return self.data[:self.experts + 1]
+
+    @property
+    def k_offsets(self) -> torch.Tensor:
+        return self.data[self.experts + 1:2 * self.experts + 2]
+
+    @property
+    def order(self) -> torch.Tensor:
+        return self.data[2 * self.experts + 2:2 * self.experts + 2 + self.slots]
+
+    @property
+    def place(self) -> torch.Tensor:
+        return self.data[2 * self.experts + 2 + self.slots:2 * self.experts + 2 + 2 * self.slots]
+
+    def _pointers(self):
+        """Device addresses of offsets, k_offsets, order and place."""
+        p, e = self.data.data_ptr(), 4 * (self.experts + 1)
+        return p, p + e, p + 2 * e, p + 2 * e + 4 * self.slots
+
+
+@functools.lru_cache(maxsize=4096)
+def _plan_sizes(tokens, top, experts):
+    """(places, workspace words) of a plan (a function of the sizes alone)."""
+    places, ws = ctypes.c_int64(0), ctypes.c_size_t(0)
+    check(load().bfp_expert_plan_sizes(tokens, top, experts, ctypes.byref(places), ctypes.byref(ws)),
+          "bfp_expert_plan_sizes")
+    return places.value, ws.value // 4
+
+
+def expert_plan(ids: torch.Tensor, experts: int) -> ExpertPlan:
+    """The plan of a routing: ids [tokens, top] (or [tokens]: one choice each),
+    int32 or int64, the expert of every slot; a value outside [0, experts) is a
+    choice that was dropped.  A stable sort by expert, in one or two launches,
+    with nothing read back: the layer's other calls take it on the same stream
+    or behind it."""
+    _need_cuda(ids, "ids")
+    if ids.dtype not in (torch.int32, torch.int64):
+        raise TypeError("ids must have dtype torch.int32 or torch.int64, got %s" % ids.dtype)
+    if ids.dim() not in (1, 2) or (ids.dim() == 2 and ids.shape[1] < 1):
+        raise ValueError("ids must be [tokens, top] or [tokens]")
+    tokens, top = ids.shape[0], ids.shape[1] if ids.dim() == 2 else 1
+    places, ws = _plan_sizes(tokens, top, experts)
+    slots = tokens * top
+    data = torch.empty(2 * (experts + 1) + 2 * slots + ws, dtype=torch.int32, device=ids.device)
+    plan = ExpertPlan(tokens, top, experts, places, data)
+    off, koff, order, place = plan._pointers()
+    check(load().bfp_expert_plan(ids.data_ptr(), 64 if ids.dtype == torch.int64 else 32, tokens, top, experts, off,
+                                 koff, order, place, place + 4 * slots if ws else None, 4 * ws, _stream(ids.device)),
+          "bfp_expert_plan")
+    return plan
+
+
+def quantize_experts(x: torch.Tensor, plan: ExpertPlan, gather: bool = False, m: int = 4, rounding: str = "nearest",
+                     seed_rows: int = 0, seed_cols: int = 0, rows: bool = True, cols: bool = True,
+                     status: torch.Tensor | None = None, out_rows: BFPTensor | None = None,
+                     out_cols: BFPTensor | None = None):
+    """FP32 -> BFP (groups of 16) in the experts' order, from one read: ``(tr, tc)``.
+    tr (None unless ``rows``): [slots, C], row p is slot plan.order[p], groups
+    along the row; rows of dropped slots are unspecified, the products skip them.
+    tc (None unless ``cols``): [C, plan.places], groups of 16 consecutive slots of
+    one expert, zeros behind an expert's last slot: the operand of
+    gemm_experts_grad.
+    ``gather``: x is [tokens, C] and slot i reads row i // top; otherwise x is
+    [slots, C], in the experts' order already (what gemm_experts returns, or its
+    gradient).  C a multiple of 16."""
+    _need_cuda(x, "x", torch.float32)
+    if rounding not in ROUNDING:
+        raise ValueError("rounding must be one of %s" % sorted(ROUNDING))
+    if x.dim() != 2 or x.shape[0] != (plan.tokens if gather else plan.slots):
+        raise ValueError("x must be [%d, C]" % (plan.tokens if gather else plan.slots))
+    if not rows and not cols:
+        raise ValueError("one of rows and cols must be asked for")
+    C = x.shape[1]
+    if C % 16:
+        raise ValueError("x must have a multiple of 16 columns")
+    tr = tc = None
+    if rows:
+        tr = out_rows if out_rows is not None else BFPTensor.empty(plan.slots, C, 16, m, x.device)
+        if (tr.rows, tr.len, tr.g, tr.m) != (plan.slots, C, 16, m):
+            raise ValueError("out_rows has the wrong shape or format")
+    if cols:
+        tc = out_cols if out_cols is not None else BFPTensor.empty(C, plan.places, 16, m, x.device)
+        if (tc.rows, tc.len, tc.g, tc.m) != (C, plan.places, 16, m):
+            raise ValueError("out_cols has the wrong shape or format")
+    off, koff, order, _ = plan._pointers()
+    check(load().bfp_quantize_experts(x.data_ptr(), C, 1 if gather else 0, order, off, koff, plan.tokens, plan.top,
+                                      plan.experts, m, ROUNDING[rounding], seed_rows & 0xFFFFFFFFFFFFFFFF,
+                                      seed_cols & 0xFFFFFFFFFFFFFFFF, tr.mant.data_ptr() if rows else None,
+                                      tr.exp.data_ptr() if rows else None, tc.mant.data_ptr() if cols else None,
+                                      tc.exp.data_ptr() if cols else None, _status_ptr(status), _stream(x.device)),
+          "bfp_quantize_experts")
+    return tr, tc
+
+
+def _expert_operands(A, B):
+    if A.g != 16 or B.g != 16:
+        raise ValueError("the products of experts take groups of 16 (repack another tensor first)")
+
+
+def gemm_experts(A: BFPTensor, W: BFPTensor, plan: ExpertPlan, m_a: int | None = None, m_b: int | None = None,
+                 out: torch.Tensor | None = None) -> torch.Tensor:
+    """The products of experts: FP32 [slots, N], row p = A[p] . W_e^T with the
+    weights of the expert e whose slot stands at p, zeros for dropped slots.  A
+    [slots, K] (quantize_experts), W [experts * N, K]: expert e's rows from e * N.
+    m_a, m_b: the stored width, or that without the low chunk plane (m - 2 of 5
+    and 6 bits, m - 4 of 7 and 8)."""
+    _expert_operands(A, W)
+    m_a, m_b = _gemm_args(A, W, m_a, m_b)
+    if A.rows != plan.slots or W.rows % plan.experts:
+        raise ValueError("A must have %d rows and W a multiple of %d" % (plan.slots, plan.experts))
+    N = W.rows // plan.experts
+    C = out if out is not None else torch.empty((A.rows, N), dtype=torch.float32, device=A.device)
+    _need_cuda(C, "out", torch.float32)
+    if C.dim() != 2 or C.shape[0] != A.rows or C.shape[1] != N:
+        raise ValueError("out must be [%d, %d]" % (A.rows, N))
+    check(load().bfp_gemm_experts(A.mant.data_ptr(), A.exp.data_ptr(), A.m, W.mant.data_ptr(), W.exp.data_ptr(), W.m,
+                                  plan._pointers()[0], plan.experts, A.rows, N, A.len, m_a, m_b, C.data_ptr(),
+                                  C.stride(0) if A.rows > 1 else N, _stream(A.device)), "bfp_gemm_experts")
+    return C
+
+
+def gemm_experts_grad(A: BFPTensor, B: BFPTensor, plan: ExpertPlan, m_a: int | None = None, m_b: int | None = None,
+                      out: torch.Tensor | None = None) -> torch.Tensor:
+    """The weight gradients of experts: FP32 [experts, A.rows, B.rows], of each
+    expert the product over its own slots of A and B, both token groupings
+    (quantize_experts' tc); zeros for an expert without slots."""
+    _expert_operands(A, B)
+    m_a, m_b = _gemm_args(A, B, m_a, m_b)
+    if A.len != plan.places:
+        raise ValueError("A and B must be token groupings of the plan (len %d)" % plan.places)
+    shape = (plan.experts, A.rows, B.rows)
+    C = out if out is not None else torch.empty(shape, dtype=torch.float32, device=A.device)
+    _need_cuda(C, "out", torch.float32)
+    if tuple(C.shape) != shape:
+        raise ValueError("out must be %s" % list(shape))
+    check(load().bfp_gemm_experts_grad(A.mant.data_ptr(), A.exp.data_ptr(), A.m, B.mant.data_ptr(), B.exp.data_ptr(),
+                                       B.m, plan._pointers()[1], plan.experts, A.rows, B.rows, A.len, m_a, m_b,
+                                       C.data_ptr(), _stream(A.device)), "bfp_gemm_experts_grad")
+    return C
+
+
+def _combine_args(y, plan, gates):
+    _need_cuda(y, "y", torch.float32)
+    if y.dim() != 2 or y.shape[0] != plan.slots:
+        raise ValueError("y must be [%d, N]" % plan.slots)
+    if gates is not None:
+        _need_cuda(gates, "gates", torch.float32)
+        if gates.numel() != plan.slots:
+            raise ValueError("gates must be [%d, %d]" % (plan.tokens, plan.top))
+    return y.shape[1]
+
+
+def combine_experts(y: torch.Tensor, plan: ExpertPlan, gates: torch.Tensor | None = None,
+                    out: torch.Tensor | None = None) -> torch.Tensor:
+    """The experts' outputs y [slots, N] (in their order) back at their tokens:
+    FP32 [tokens, N], the sum over a token's choices of gates [tokens, top] (None:
+    ones, e.g. for the gradient of the tokens) times the slot's row of y.  Dropped
+    choices add nothing."""
+    N = _combine_args(y, plan, gates)
+    o = out if out is not None else torch.empty((plan.tokens, N), dtype=torch.float32, device=y.device)
+    _need_cuda(o, "out", torch.float32)
+    if tuple(o.shape) != (plan.tokens, N):
+        raise ValueError("out must be [%d, %d]" % (plan.tokens, N))
+    off, _, _, place = plan._pointers()
+    check(load().bfp_combine_experts(y.data_ptr(), gates.data_ptr() if gates is not None else None, place, off,
+                                     plan.tokens, plan.top, plan.experts, N, o.data_ptr(), _stream(y.device)),
+          "bfp_combine_experts")
+    return o
+
+
+def combine_experts_grad(dout: torch.Tensor, y: torch.Tensor, plan: ExpertPlan, gates: torch.Tensor | None = None,
+                         out: torch.Tensor | None = None):
+    """The gradients of combine_experts for dout [tokens, N]: ``(dy, dgates)``, dy
+    [slots, N] in the experts' order (``out``: where it goes) and dgates [tokens,
+    top]; zeros for dropped choices."""
+    N = _combine_args(y, plan, gates)
+    _need_cuda(dout, "dout", torch.float32)
+    if tuple(dout.shape) != (plan.tokens, N):
+        raise ValueError("dout must be [%d, %d]" % (plan.tokens, N))
+    dy = out if out is not None else torch.empty_like(y)
+    _need_cuda(dy, "out", torch.float32)
+    if dy.shape != y.shape:
+        raise ValueError("out must be [%d, %d]" % (plan.slots, N))
+    dgates = torch.empty((plan.tokens, plan.top), dtype=torch.float32, device=y.device)
+    off, _, _, place = plan._pointers()
+    check(load().bfp_combine_experts_grad(dout.data_ptr(), y.data_ptr(), gates.data_ptr() if gates is not None else None,
+                                          place, off, plan.tokens, plan.top, plan.experts, N, dy.data_ptr(),
+                                          dgates.data_ptr(), _stream(y.device)), "bfp_combine_experts_grad")
+    return dy, dgates

@@ -54,9 +54,16 @@ SIGNATURES = {
     "bfp_adaptive_parts": (_I64, [_I64, _I64, _I, _I]),
     "bfp_adaptive_noalloc_max_parts": (_I64, []),
     "bfp_adaptive_threshold": (ctypes.c_double, [ctypes.c_double, ctypes.c_double, _I64, _I64, _I64, _I64]),
+    "bfp_expert_plan_sizes": (_I, [_I64, _I, _I, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_size_t)]),
+    "bfp_expert_plan": (_I, [_P, _I, _I64, _I, _I, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "bfp_quantize_experts": (_I, [_P, _I64, _I, _P, _P, _P, _I64, _I, _I, _I, _I, _U64, _U64, _P, _P, _P, _P, _P, _P]),
+    "bfp_gemm_experts": (_I, [_P, _P, _I, _P, _P, _I, _P, _I, _I64, _I64, _I64, _I, _I, _P, _I64, _P]),
+    "bfp_gemm_experts_grad": (_I, [_P, _P, _I, _P, _P, _I, _P, _I, _I64, _I64, _I64, _I, _I, _P, _P]),
+    "bfp_combine_experts": (_I, [_P, _P, _P, _P, _I64, _I, _I, _I64, _P, _P]),
+    "bfp_combine_experts_grad": (_I, [_P, _P, _P, _P, _P, _I64, _I, _I, _I64, _P, _P, _P]),
     "bfp_adaptive_mantissa": (_I, [ctypes.c_double, ctypes.c_double, ctypes.c_double]),
 }
-ABI_VERSION = 7
+ABI_VERSION = 8
 
 _lock = threading.Lock()
 _lib = None

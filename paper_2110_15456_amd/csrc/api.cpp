@@ -88,6 +88,27 @@ int check_packed(int64_t rows, int64_t len, int m) {
   return BFP_OK;
 }
 
+// A routing of tokens * top slots over experts.
+int check_routing(int64_t tokens, int64_t top, int experts) {
+  if (tokens < 0 || top < 1 || experts < 1) return BFP_E_ARG;
+  if (experts > fastbfp::kMaxExperts || tokens > ((int64_t(1) << 31) - (int64_t(1) << 20)) / top) return BFP_E_UNSUPPORTED;
+  return BFP_OK;
+}
+
+int check_combine(const float* y, const float* gates, const int32_t* place, const int32_t* offsets, int64_t tokens,
+                  int top, int experts, int64_t N, const float* out) {
+  const int st = check_routing(tokens, top, experts);
+  if (st != BFP_OK) return st;
+  if (N < 0) return BFP_E_ARG;
+  if (N > (int64_t(1) << 31)) return BFP_E_UNSUPPORTED;
+  if (tokens == 0) return BFP_OK;
+  if (N > 0 && (!y || !out)) return BFP_E_ARG;
+  if (!place || !offsets) return BFP_E_ARG;
+  if (!aligned(y, 4) || !aligned(out, 4) || !aligned(gates, 4) || !aligned(place, 4) || !aligned(offsets, 4))
+    return BFP_E_ARG;
+  return BFP_OK;
+}
+
 size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 
 // How bfp_gemm_ws runs a product: which operands it repacks into the layout
@@ -646,6 +667,119 @@ double bfp_adaptive_threshold(double alpha, double beta, int64_t i, int64_t I, i
 int bfp_adaptive_mantissa(double num, double den, double eps) {
   const double r = den > 0.0 ? num / den : 0.0;
   return r < eps ? 2 : 4;
+}
+
+int bfp_expert_plan_sizes(int64_t tokens, int top, int experts, int64_t* places, size_t* workspace_bytes) {
+  const int st = check_routing(tokens, top, experts);
+  if (st != BFP_OK) return st;
+  if (!places || !workspace_bytes) return BFP_E_ARG;
+  *places = fastbfp::expert_places(tokens * top, experts);
+  *workspace_bytes = (size_t)fastbfp::expert_plan_ws(tokens * top, experts) * 4;
+  return BFP_OK;
+}
+
+int bfp_expert_plan(const void* ids, int ids_bits, int64_t tokens, int top, int experts, int32_t* offsets,
+                    int32_t* k_offsets, int32_t* order, int32_t* place, void* workspace, size_t workspace_bytes,
+                    void* stream) {
+  const int st = check_routing(tokens, top, experts);
+  if (st != BFP_OK) return st;
+  const int64_t slots = tokens * top;
+  if (ids_bits != 32 && ids_bits != 64) return BFP_E_ARG;
+  if (!offsets || !k_offsets || !aligned(offsets, 4) || !aligned(k_offsets, 4)) return BFP_E_ARG;
+  if (slots > 0 && (!ids || !order || !place || !aligned(ids, ids_bits / 8) || !aligned(order, 4) || !aligned(place, 4)))
+    return BFP_E_ARG;
+  const size_t need = (size_t)fastbfp::expert_plan_ws(slots, experts) * 4;
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 4))) return BFP_E_ARG;
+  return status_of(fastbfp::launch_expert_plan(ids, ids_bits == 64, slots, experts, offsets, k_offsets, order, place,
+                                               static_cast<int32_t*>(workspace), static_cast<hipStream_t>(stream)));
+}
+
+int bfp_quantize_experts(const float* x, int64_t C, int gather, const int32_t* order, const int32_t* offsets,
+                         const int32_t* k_offsets, int64_t tokens, int top, int experts, int m_bits, int round_mode,
+                         uint64_t seed_r, uint64_t seed_c, uint8_t* mant_r, uint8_t* exp_r, uint8_t* mant_c,
+                         uint8_t* exp_c, uint32_t* status_word, void* stream) {
+  int st = check_routing(tokens, top, experts);
+  if (st != BFP_OK) return st;
+  const int64_t slots = tokens * top, places = fastbfp::expert_places(slots, experts);
+  st = check_tensor(slots, C, 16, m_bits);
+  if (st != BFP_OK) return st;
+  if (gather != 0 && gather != 1) return BFP_E_ARG;
+  if (round_mode < BFP_ROUND_NEAREST || round_mode > BFP_ROUND_TRUNCATE) return BFP_E_ARG;
+  if (C >= (int64_t(1) << 22)) return BFP_E_UNSUPPORTED;
+  if (slots * (C / 16) > 0x7fffffff || C * (places / 16) > 0x7fffffff) return BFP_E_UNSUPPORTED;
+  if (slots == 0 || C == 0) return BFP_OK;
+  if (!mant_r != !exp_r || !mant_c != !exp_c || (!mant_r && !mant_c)) return BFP_E_ARG;
+  if (!x || !aligned(x, 16) || !aligned(mant_r, 4) || !aligned(mant_c, 4) || !aligned(status_word, 4))
+    return BFP_E_ARG;
+  if (!order || !offsets || !k_offsets || !aligned(order, 4) || !aligned(offsets, 4) || !aligned(k_offsets, 4))
+    return BFP_E_ARG;
+  return status_of(fastbfp::launch_quantize_experts(x, gather ? tokens : slots, C, gather ? top : 0, order, offsets,
+                                                    k_offsets, experts, slots, places, m_bits, round_mode, seed_r,
+                                                    seed_c, mant_r, exp_r, mant_c, exp_c, status_word,
+                                                    static_cast<hipStream_t>(stream)));
+}
+
+int bfp_gemm_experts(const uint8_t* a_mant, const uint8_t* a_exp, int a_m_bits, const uint8_t* b_mant,
+                     const uint8_t* b_exp, int b_m_bits, const int32_t* offsets, int experts, int64_t slots, int64_t N,
+                     int64_t K, int m_a, int m_b, float* C, int64_t ldc, void* stream) {
+  int st = check_routing(slots, 1, experts);
+  if (st != BFP_OK) return st;
+  st = check_gemm(a_mant, a_m_bits, b_mant, b_m_bits, slots, N, K, 16, m_a, m_b);
+  if (st != BFP_OK) return st;
+  if (!fast_path(a_m_bits, b_m_bits, 16, m_a, m_b)) return BFP_E_UNSUPPORTED;
+  // (one tile more for each expert than rows fill)
+  if ((slots / 128 + experts + 1) * ((N + 63) / 64) > 0x7fffffff) return BFP_E_UNSUPPORTED;
+  if (ldc < N) return BFP_E_SHAPE;
+  if (slots == 0 || N == 0) return BFP_OK;
+  if (!C || !aligned(C, 4) || !offsets || !aligned(offsets, 4) || (K > 0 && (!a_exp || !b_exp))) return BFP_E_ARG;
+  return status_of(fastbfp::launch_gemm_experts(a_mant, a_exp, a_m_bits, planes_used(a_m_bits, m_a), b_mant, b_exp,
+                                                b_m_bits, planes_used(b_m_bits, m_b), offsets, experts, slots, N, K,
+                                                4 - m_a - m_b, C, ldc, static_cast<hipStream_t>(stream)));
+}
+
+int bfp_gemm_experts_grad(const uint8_t* a_mant, const uint8_t* a_exp, int a_m_bits, const uint8_t* b_mant,
+                          const uint8_t* b_exp, int b_m_bits, const int32_t* k_offsets, int experts, int64_t M,
+                          int64_t N, int64_t places, int m_a, int m_b, float* C, void* stream) {
+  int st = check_routing(0, 1, experts);
+  if (st != BFP_OK) return st;
+  st = check_gemm(a_mant, a_m_bits, b_mant, b_m_bits, M, N, places, 16, m_a, m_b);
+  if (st != BFP_OK) return st;
+  if (places % 128 != 0) return BFP_E_SHAPE;
+  if (!fast_path(a_m_bits, b_m_bits, 16, m_a, m_b)) return BFP_E_UNSUPPORTED;
+  if (((M + 127) / 128) * ((N + 63) / 64) > 0x7fffffff / experts) return BFP_E_UNSUPPORTED;
+  if (M == 0 || N == 0) return BFP_OK;
+  if (!C || !aligned(C, 4) || !k_offsets || !aligned(k_offsets, 4)) return BFP_E_ARG;
+  if (places > 0 && (!a_exp || !b_exp)) return BFP_E_ARG;
+  if (!aligned(a_exp, 4) || !aligned(b_exp, 4)) return BFP_E_ARG;
+  return status_of(fastbfp::launch_gemm_experts_grad(a_mant, a_exp, a_m_bits, planes_used(a_m_bits, m_a), b_mant,
+                                                     b_exp, b_m_bits, planes_used(b_m_bits, m_b), k_offsets, experts,
+                                                     M, N, places, 4 - m_a - m_b, C, static_cast<hipStream_t>(stream)));
+}
+
+int bfp_combine_experts(const float* y, const float* gates, const int32_t* place, const int32_t* offsets,
+                        int64_t tokens, int top, int experts, int64_t N, float* out, void* stream) {
+  const int st = check_combine(y, gates, place, offsets, tokens, top, experts, N, out);
+  if (st != BFP_OK || tokens == 0 || N == 0) return st;
+  if ((tokens * N + 255) / 256 > 0x7fffffff) return BFP_E_UNSUPPORTED;
+  return status_of(fastbfp::launch_combine_experts(y, gates, place, offsets, experts, tokens, top, N, out,
+                                                   static_cast<hipStream_t>(stream)));
+}
+
+int bfp_combine_experts_grad(const float* dout, const float* y, const float* gates, const int32_t* place,
+                             const int32_t* offsets, int64_t tokens, int top, int experts, int64_t N, float* dy,
+                             float* dgates, void* stream) {
+  const int st = check_combine(y, gates, place, offsets, tokens, top, experts, N, dy);
+  if (st != BFP_OK || tokens == 0) return st;
+  if (!aligned(dgates, 4)) return BFP_E_ARG;
+  if (N > 0) {
+    if (!dout || !aligned(dout, 4)) return BFP_E_ARG;
+    const uintptr_t bytes = (uintptr_t)tokens * (uintptr_t)N * 4, all = bytes * (uintptr_t)top;
+    const uintptr_t o = reinterpret_cast<uintptr_t>(dy), a = reinterpret_cast<uintptr_t>(y);
+    const uintptr_t d = reinterpret_cast<uintptr_t>(dout);
+    if ((a < o + all && o < a + all) || (d < o + all && o < d + bytes)) return BFP_E_ARG;  // dy overlaps y or dout
+  }
+  return status_of(fastbfp::launch_combine_experts_grad(dout, y, gates, place, offsets, experts, tokens, top, N, dy,
+                                                        dgates, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -21,6 +21,7 @@
 // at the last row).
 #pragma once
 #include "bfp_quant.h"
+#include "segments.h"
 
 namespace fastbfp {
 
@@ -184,12 +185,14 @@ template <int NP, int K0, int K1> struct Frag {
 }  // namespace direct
 
 // NA / NB, FA / FB, G: as mx::Cfg (planes read; FP4 codes, or split at 2 bits).
-// BOUT: C is written as BFP (N a multiple of 16).
-template <int NA, int NB, int FA, int FB, int G, int RM, int RN, bool BOUT>
+// BOUT: C is written as BFP (N a multiple of 16).  SEG = kSegRows: the products
+// of experts (segments.h; a tile stays within one segment, B holds N rows for
+// each).
+template <int NA, int NB, int FA, int FB, int G, int RM, int RN, bool BOUT, int SEG = kSegNone>
 __global__ __launch_bounds__(64 * direct::kMaxWaves) void k_gemm_direct(
     const uint8_t* __restrict__ a_mant, const uint8_t* __restrict__ a_exp, int64_t a_ps,
     const uint8_t* __restrict__ b_mant, const uint8_t* __restrict__ b_exp, int64_t b_ps, int M, int N, int ng,
-    float scale, float* __restrict__ C, int64_t ldc, direct::Out out) {
+    float scale, float* __restrict__ C, int64_t ldc, direct::Out out, typename SegArg<SEG>::type seg) {
   using namespace direct;
   constexpr int KA0 = (NA == 1 && FA) ? kPlaneFP4 : kPlaneFP6, KB0 = (NB == 1 && FB) ? kPlaneFP4 : kPlaneFP6;
   constexpr int KA1 = FA ? kPlaneLo2 : kPlaneFP6, KB1 = FB ? kPlaneLo2 : kPlaneFP6;
@@ -199,17 +202,27 @@ __global__ __launch_bounds__(64 * direct::kMaxWaves) void k_gemm_direct(
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nw = blockDim.x >> 6;
   const int lr = lane & 15, lb = lane >> 4;
-  const int row0 = blockIdx.y * (16 * RM), col0 = blockIdx.x * (16 * RN);
+  int row0 = blockIdx.y * (16 * RM);
+  const int col0 = blockIdx.x * (16 * RN);
+  int64_t b_row0 = col0;
+  if constexpr (SEG == kSegRows) {
+    const Segment sg = find_segment<16 * RM>(seg, blockIdx.y);
+    if (sg.index < 0) return;  // (the grid is sized for the most tiles there can be)
+    row0 = sg.first;
+    M = sg.end;
+    if (sg.index == seg.n) ng = 0;  // rows of no expert: zeros
+    else b_row0 += (int64_t)sg.index * N;
+  }
   const int a_rows = min(16 * RM, M - row0), b_rows = min(16 * RN, N - col0);
   const int ng_e = ng * 16 / G;
   constexpr int UA0 = KA0 == kPlaneFP6 ? 12 : 8, UB0 = KB0 == kPlaneFP6 ? 12 : 8;  // bytes per unit
   constexpr int UA1 = KA1 == kPlaneFP6 ? 12 : 8, UB1 = KB1 == kPlaneFP6 ? 12 : 8;
   const rsrc_t ra0 = make_rsrc(a_mant + (int64_t)row0 * ng * UA0, (uint32_t)a_rows * ng * UA0);
-  const rsrc_t rb0 = make_rsrc(b_mant + (int64_t)col0 * ng * UB0, (uint32_t)b_rows * ng * UB0);
+  const rsrc_t rb0 = make_rsrc(b_mant + b_row0 * ng * UB0, (uint32_t)b_rows * ng * UB0);
   const rsrc_t ra1 = make_rsrc(a_mant + a_ps + (int64_t)row0 * ng * UA1, NA == 2 ? (uint32_t)a_rows * ng * UA1 : 0u);
-  const rsrc_t rb1 = make_rsrc(b_mant + b_ps + (int64_t)col0 * ng * UB1, NB == 2 ? (uint32_t)b_rows * ng * UB1 : 0u);
+  const rsrc_t rb1 = make_rsrc(b_mant + b_ps + b_row0 * ng * UB1, NB == 2 ? (uint32_t)b_rows * ng * UB1 : 0u);
   const rsrc_t rea = make_rsrc(a_exp + (int64_t)row0 * ng_e, (uint32_t)a_rows * ng_e);
-  const rsrc_t reb = make_rsrc(b_exp + (int64_t)col0 * ng_e, (uint32_t)b_rows * ng_e);
+  const rsrc_t reb = make_rsrc(b_exp + b_row0 * ng_e, (uint32_t)b_rows * ng_e);
   constexpr int EA = G == 16 ? 4 : 2;  // exponent bytes per lane and superstep
   const bool dw = ng_e % EA == 0 && (reinterpret_cast<uintptr_t>(a_exp) % EA) == 0 &&
                   (reinterpret_cast<uintptr_t>(b_exp) % EA) == 0;
@@ -347,10 +360,10 @@ hipError_t launch_direct_t(int rm, int rn, const uint8_t* a_mant, const uint8_t*
   if (rm == RM && rn == RN) {                                                                                         \
     if (out)                                                                                                          \
       hipLaunchKernelGGL((k_gemm_direct<NA, NB, FA, FB, G, RM, RN, true>), grid, dim3(64 * nw), 0, s, a_mant, a_exp,  \
-                         a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, *out);                                   \
+                         a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, *out, NoSegments{});                                   \
     else                                                                                                              \
       hipLaunchKernelGGL((k_gemm_direct<NA, NB, FA, FB, G, RM, RN, false>), grid, dim3(64 * nw), 0, s, a_mant, a_exp, \
-                         a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, direct::Out{});                          \
+                         a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, direct::Out{}, NoSegments{});           \
     return hipGetLastError();                                                                                         \
   }
   FASTBFP_DIRECT_LAUNCH(1, 1)
@@ -359,6 +372,36 @@ hipError_t launch_direct_t(int rm, int rn, const uint8_t* a_mant, const uint8_t*
 #undef FASTBFP_DIRECT_LAUNCH
   return hipErrorInvalidValue;
 }
+
+// The products of experts (groups of 16); the tiles as above.
+template <int NA, int NB, int FA, int FB>
+hipError_t launch_direct_experts_t(int rm, int rn, const uint8_t* a_mant, const uint8_t* a_exp, int64_t a_ps,
+                                   const uint8_t* b_mant, const uint8_t* b_exp, int64_t b_ps, int M, int N, int ng,
+                                   float scale, float* C, int64_t ldc, const Segments& seg, hipStream_t s) {
+  const int nss = (ng + 15) / 16;
+  const int nw = nss < 1 ? 1 : nss > direct::kMaxWaves ? direct::kMaxWaves : nss;
+  const int64_t tiles = most_segment_tiles(seg, 16 * rm);
+  if (tiles > direct::kMaxRowTiles) return hipErrorInvalidValue;  // (the plan does not plan it)
+  const dim3 grid((unsigned)((N + 16 * rn - 1) / (16 * rn)), (unsigned)tiles);
+#define FASTBFP_DIRECT_LAUNCH(RM, RN)                                                                               \
+  if (rm == RM && rn == RN) {                                                                                       \
+    hipLaunchKernelGGL((k_gemm_direct<NA, NB, FA, FB, 16, RM, RN, false, kSegRows>), grid, dim3(64 * nw), 0, s,     \
+                       a_mant, a_exp, a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, direct::Out{}, seg);      \
+    return hipGetLastError();                                                                                       \
+  }
+  FASTBFP_DIRECT_LAUNCH(1, 1)
+  FASTBFP_DIRECT_LAUNCH(1, 2)
+  FASTBFP_DIRECT_LAUNCH(2, 2)
+  FASTBFP_DIRECT_LAUNCH(4, 2)
+#undef FASTBFP_DIRECT_LAUNCH
+  return hipErrorInvalidValue;
+}
+#define FASTBFP_DIRECT_EXPERTS_INSTANTIATE(NA, NB, FA, FB)                                                          \
+  template hipError_t launch_direct_experts_t<NA, NB, FA, FB>(int, int, const uint8_t*, const uint8_t*, int64_t,    \
+                                                              const uint8_t*, const uint8_t*, int64_t, int, int, int, \
+                                                              float, float*, int64_t, const Segments&, hipStream_t);
+#define FASTBFP_DIRECT_EXPERTS_DECLARE(NA, NB, FA, FB) extern FASTBFP_DIRECT_EXPERTS_INSTANTIATE(NA, NB, FA, FB)
+#define FASTBFP_DIRECT_EXPERTS_ALL(DO, NA, NB) DO(NA, NB, 0, 0) DO(NA, NB, 0, 1) DO(NA, NB, 1, 0) DO(NA, NB, 1, 1)
 
 // One operand-format combination's dispatch over the group sizes.
 #define FASTBFP_DIRECT_INSTANTIATE(NA, NB, FA, FB, G)                                                            \

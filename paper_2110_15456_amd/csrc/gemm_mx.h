@@ -52,6 +52,7 @@
 // tiles are ordered so that neighbours share panels in L2 on the same XCD.
 #pragma once
 #include "bfp_quant.h"
+#include "segments.h"
 
 namespace fastbfp {
 
@@ -178,6 +179,14 @@ __device__ __forceinline__ void tile_of(int bid, int nblocks, int tiles_m, int t
   const int in = lid % per_group;
   tm = first_m + in % rows_in_group;
   tn = in / rows_in_group;
+}
+
+// The same for any workgroup count (the first nblocks % 8 XCDs take one more).
+template <int GROUP_M>
+__device__ __forceinline__ void tile_of_any(int bid, int nblocks, int tiles_m, int tiles_n, int& tm, int& tn) {
+  constexpr int NXCD = 8;
+  const int xcd = bid % NXCD, lid = xcd * (nblocks / NXCD) + min(xcd, nblocks % NXCD) + bid / NXCD;
+  tile_of<GROUP_M>(lid, 1, tiles_m, tiles_n, tm, tn);
 }
 
 // The same with the K slabs split into parts (workgroup id -> tile and part):
@@ -462,13 +471,18 @@ struct OutBFP {
   uint32_t key0, key1;
 };
 
-template <class CF, bool EXP_FULL, int QNCH>
+//
+// SEG: the products of experts (segments.h).  kSegRows: A's rows and C's are
+// those of the segments one after another, B holds N rows for each segment; a
+// tile stays within one segment.  kSegK: K is the segments one after another,
+// each a whole number of slabs, and C holds an M x ldc matrix for each.
+template <class CF, bool EXP_FULL, int QNCH, int SEG = kSegNone>
 __global__ __launch_bounds__(CF::NT, CF::WAVES) void k_gemm_mx(const uint8_t* __restrict__ a_mant, const uint8_t* __restrict__ a_exp,
                                                  int64_t a_plane_stride, const uint8_t* __restrict__ b_mant,
                                                  const uint8_t* __restrict__ b_exp, int64_t b_plane_stride, int M,
                                                  int N, int ng, float scale, float* __restrict__ C, int64_t ldc,
                                                  int tiles_m, int tiles_n, int part_slabs, int64_t part_stride,
-                                                 OutBFP qo) {
+                                                 OutBFP qo, typename SegArg<SEG>::type seg) {
   constexpr int TM = CF::TM, TN = CF::TN, NA = CF::NA, NB = CF::NB, FA = CF::FA, FB = CF::FB;
   // Groups of 16 with full slabs (XP): the exponents of slab pair p (slabs 2p
   // and 2p + 1: 16 contiguous bytes per row) come in one 16-byte load per row,
@@ -503,14 +517,34 @@ __global__ __launch_bounds__(CF::NT, CF::WAVES) void k_gemm_mx(const uint8_t* __
   // part_slabs) into its part's own FP32 matrix, part_stride values after the
   // previous one (launch_parts_sum adds them up).
   int slab0 = 0;
-  if (QNCH == 0 && part_slabs > 0) {
+  int row_first = 0;       // kSegRows: the tile's first row
+  int64_t b_first = 0;     // and the first row of its segment's B
+  int seg_slabs = 0;       // kSegK: slabs of the tile's segment
+  if constexpr (SEG == kSegRows) {
+    const int tiles = segment_tiles<CF::BM>(seg);
+    if ((int)blockIdx.x >= tiles * tiles_n) return;  // (the grid is sized for the most tiles there can be)
+    tile_of_any<FASTBFP_MX_GM>(blockIdx.x, tiles * tiles_n, tiles, tiles_n, tm, tn);
+    const Segment sg = find_segment<CF::BM>(seg, tm);
+    if (sg.index < 0) return;
+    row_first = sg.first;
+    M = sg.end;
+    if (sg.index == seg.n) ng = 0;  // rows of no expert: zeros
+    else b_first = (int64_t)sg.index * N;
+  } else if constexpr (SEG == kSegK) {
+    const int e = split_tile_of<FASTBFP_MX_GM>(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn);
+    const int slabs = ng / mx::KG, end = min(max(seg.offsets[e + 1], 0) / (16 * mx::KG), slabs);
+    slab0 = min(max(seg.offsets[e], 0) / (16 * mx::KG), end);
+    seg_slabs = end - slab0;
+    C += e * part_stride;
+  } else if (QNCH == 0 && part_slabs > 0) {
     const int part = split_tile_of<FASTBFP_MX_GM>(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn);
     slab0 = part * part_slabs;
     C += part * part_stride;
   } else {
     tile_of<FASTBFP_MX_GM>(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn);
   }
-  const int row0 = tm * CF::BM, col0 = tn * CF::BN;
+  const int row0 = SEG == kSegRows ? row_first : tm * CF::BM, col0 = tn * CF::BN;
+  const int64_t b_row0 = b_first + col0;  // B's rows: those of the segment, then this tile's columns
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;  // wave index in an SGPR
   const int wr = wave / CF::WGN, wc = wave % CF::WGN;
   const int lr = lane & 15, lb = lane >> 4;
@@ -523,12 +557,12 @@ __global__ __launch_bounds__(CF::NT, CF::WAVES) void k_gemm_mx(const uint8_t* __
 
   const int ngl = ng - slab0 * mx::KG;  // 16-value halves from this part's first slab to the rows' end
   const int all_slabs = (ngl + mx::KG - 1) / mx::KG;
-  const int nslabs = (QNCH == 0 && part_slabs > 0) ? min(part_slabs, all_slabs) : all_slabs;
+  const int nslabs = SEG == kSegK ? seg_slabs : (QNCH == 0 && part_slabs > 0) ? min(part_slabs, all_slabs) : all_slabs;
   auto exp_row = [&](int k, const uint8_t*& src, int& grow, int& gend, int& lds) {
     const int r = tid + k * CF::NT;
     const bool is_a = r < CF::BM;
     const int rr = is_a ? r : r - CF::BM;
-    src = (is_a ? a_exp : b_exp) + slab0 * CF::EK;
+    src = (is_a ? a_exp : b_exp + b_first * (ng * 16 / CF::G)) + slab0 * CF::EK;
     grow = (is_a ? row0 : col0) + rr;
     gend = is_a ? M : N;
     lds = (is_a ? CF::OFF_EA : CF::OFF_EB) + rr * CF::EK;
@@ -549,7 +583,7 @@ __global__ __launch_bounds__(CF::NT, CF::WAVES) void k_gemm_mx(const uint8_t* __
   for (int p = 0; p < NB; ++p) {
     const uint32_t r = rbytes(mx::b_four<CF>(p));
     const uint32_t o = (uint32_t)slab0 * (mx::b_four<CF>(p) ? mx::KG * 8u : mx::KG * 12u);
-    rb[p] = make_rsrc(b_mant + p * b_plane_stride + (int64_t)col0 * r + o, (uint32_t)b_rows * r - o);
+    rb[p] = make_rsrc(b_mant + p * b_plane_stride + b_row0 * r + o, (uint32_t)b_rows * r - o);
   }
   // FP6: lane -> (row lane / 8 of the instruction's 8, slot lane % 8), loading
   // the group that the row's swizzle puts in that slot.
@@ -563,7 +597,7 @@ __global__ __launch_bounds__(CF::NT, CF::WAVES) void k_gemm_mx(const uint8_t* __
                       (reinterpret_cast<uintptr_t>(b_exp) & 3) == 0;
   const int eo = slab0 * CF::EK;
   const rsrc_t rea = make_rsrc(a_exp + (int64_t)row0 * ng_e + eo, (uint32_t)(a_rows * ng_e - eo));
-  const rsrc_t reb = make_rsrc(b_exp + (int64_t)col0 * ng_e + eo, (uint32_t)(b_rows * ng_e - eo));
+  const rsrc_t reb = make_rsrc(b_exp + b_row0 * ng_e + eo, (uint32_t)(b_rows * ng_e - eo));
   constexpr int DPR = CF::EK / 4;
   const uint32_t e_lane_off = (uint32_t)(lane / DPR) * (uint32_t)ng_e + (uint32_t)(lane % DPR) * 4u;
   const uint32_t x_lane_off = (uint32_t)lane * (uint32_t)ng_e;
@@ -1616,30 +1650,49 @@ static hipError_t launch_mx_v(const uint8_t* a_mant, const uint8_t* a_exp, int64
   const int64_t stride = (int64_t)M * ldc;
   if (!qo)
     hipLaunchKernelGGL((k_gemm_mx<CF, EXP_FULL, 0>), grid, block, 0, s, a_mant, a_exp, a_ps, b_mant, b_exp, b_ps, M, N,
-                       ng, scale, C, ldc, tiles_m, tiles_n, part_slabs, stride, OutBFP{});
+                       ng, scale, C, ldc, tiles_m, tiles_n, part_slabs, stride, OutBFP{}, NoSegments{});
   else if (qo->m > 4)
     hipLaunchKernelGGL((k_gemm_mx<CF, EXP_FULL, 2>), grid, block, 0, s, a_mant, a_exp, a_ps, b_mant, b_exp, b_ps, M, N,
-                       ng, scale, C, ldc, tiles_m, tiles_n, 0, stride, *qo);
+                       ng, scale, C, ldc, tiles_m, tiles_n, 0, stride, *qo, NoSegments{});
   else
     hipLaunchKernelGGL((k_gemm_mx<CF, EXP_FULL, 1>), grid, block, 0, s, a_mant, a_exp, a_ps, b_mant, b_exp, b_ps, M, N,
-                       ng, scale, C, ldc, tiles_m, tiles_n, 0, stride, *qo);
+                       ng, scale, C, ldc, tiles_m, tiles_n, 0, stride, *qo, NoSegments{});
+  return hipGetLastError();
+}
+
+// The products of experts: kSegRows, C [rows of all segments][N], `tiles_m` the
+// most tiles of rows that there can be; kSegK, C [segments][M][N] (ldc = N).
+template <class CF, bool EXP_FULL, int SEG>
+static hipError_t launch_mx_seg(const uint8_t* a_mant, const uint8_t* a_exp, int64_t a_ps, const uint8_t* b_mant,
+                                const uint8_t* b_exp, int64_t b_ps, int M, int N, int ng, float scale, float* C,
+                                int64_t ldc, const Segments& seg, hipStream_t s) {
+  const int64_t tiles_n = (N + CF::BN - 1) / CF::BN;
+  const int64_t tiles_m = SEG == kSegRows ? most_segment_tiles(seg, CF::BM) : (M + CF::BM - 1) / CF::BM;
+  const int64_t wgs = tiles_m * tiles_n * (SEG == kSegK ? seg.n : 1);
+  if (wgs > 0x7fffffff) return hipErrorInvalidValue;  // (the caller checks)
+  hipLaunchKernelGGL((k_gemm_mx<CF, EXP_FULL, 0, SEG>), dim3((unsigned)wgs), dim3(CF::NT), 0, s, a_mant, a_exp, a_ps,
+                     b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, (int)tiles_m, (int)tiles_n, 0, (int64_t)M * ldc,
+                     OutBFP{}, seg);
   return hipGetLastError();
 }
 
 // One operand-format combination: NA / NB planes read, FA / FB plane 0 of A /
 // B in FP4, G the group size.  a_ps / b_ps: byte offset of plane 1 (the stored
 // plane 0's size); ng: 16-value halves (K / 16) per row.
+template <int NA, int NB, int FA, int FB, int G> struct mx_default {
+  // The tile shrinks along an operand with two chunk planes so that two LDS
+  // stages fit in 160 KB; with FP4 upper planes on both sides (192 bytes per
+  // slab row instead of 256) A keeps 256 rows.
+  static constexpr bool WIDE22 = NA == 2 && NB == 2 && FA && FB;
+  using CF = mx::Cfg<(NA == 1 && NB == 1) ? FASTBFP_MX11_BM : (NA == 1 || WIDE22) ? FASTBFP_MX_BM : FASTBFP_MX_BM / 2,
+                     (NA == 1 && NB == 1) ? FASTBFP_MX11_BN : NB == 1 ? FASTBFP_MX_BN : FASTBFP_MX_BN / 2, NA, NB, FA,
+                     FB, G>;
+};
 template <int NA, int NB, int FA, int FB, int G>
 hipError_t launch_mx_t(const uint8_t* a_mant, const uint8_t* a_exp, int64_t a_ps, const uint8_t* b_mant,
                        const uint8_t* b_exp, int64_t b_ps, int M, int N, int ng, float scale, float* C, int64_t ldc,
                        const OutBFP* qo, int part_slabs, hipStream_t s) {
-  // The tile shrinks along an operand with two chunk planes so that two LDS
-  // stages fit in 160 KB; with FP4 upper planes on both sides (192 bytes per
-  // slab row instead of 256) A keeps 256 rows.
-  constexpr bool WIDE22 = NA == 2 && NB == 2 && FA && FB;
-  using CF = mx::Cfg<(NA == 1 && NB == 1) ? FASTBFP_MX11_BM : (NA == 1 || WIDE22) ? FASTBFP_MX_BM : FASTBFP_MX_BM / 2,
-                     (NA == 1 && NB == 1) ? FASTBFP_MX11_BN : NB == 1 ? FASTBFP_MX_BN : FASTBFP_MX_BN / 2, NA, NB, FA,
-                     FB, G>;
+  using CF = typename mx_default<NA, NB, FA, FB, G>::CF;
   auto al = [](const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; };
   // direct exponent loads need full slabs and 4-byte aligned exponent rows
   const bool ef = ng % mx::KG == 0 && al(a_exp, 4) && al(b_exp, 4);  // (K a multiple of 128 either way)
@@ -1675,6 +1728,34 @@ hipError_t launch_mx_11_tile(const uint8_t* a_mant, const uint8_t* a_exp, const 
   template hipError_t launch_mx_11_tile<BM, BN, FA, FB>(const uint8_t*, const uint8_t*, const uint8_t*,       \
                                                         const uint8_t*, int, int, int, float, float*, int64_t, \
                                                         const OutBFP*, int, hipStream_t);
+
+// The products of experts of one operand-format combination (groups of 16).
+// small: 128 x 128 tiles (one chunk plane per operand).
+template <int NA, int NB, int FA, int FB>
+hipError_t launch_mx_experts_t(bool small, bool k_segments, const uint8_t* a_mant, const uint8_t* a_exp, int64_t a_ps,
+                               const uint8_t* b_mant, const uint8_t* b_exp, int64_t b_ps, int M, int N, int ng,
+                               float scale, float* C, int64_t ldc, const Segments& seg, hipStream_t s) {
+  auto al = [](const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; };
+  const bool ef = ng % mx::KG == 0 && al(a_exp, 4) && al(b_exp, 4);
+  auto run = [&](auto cf) {
+    using CF = decltype(cf);
+    if (k_segments)  // (K is whole slabs, exponents 4-byte aligned: the caller checks)
+      return launch_mx_seg<CF, true, kSegK>(a_mant, a_exp, a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, seg, s);
+    if (ef)
+      return launch_mx_seg<CF, true, kSegRows>(a_mant, a_exp, a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, seg, s);
+    return launch_mx_seg<CF, false, kSegRows>(a_mant, a_exp, a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, seg, s);
+  };
+  if constexpr (NA == 1 && NB == 1) {
+    if (small) return run(mx::Cfg<128, 128, 1, 1, FA, FB, 16>{});
+  }
+  return run(typename mx_default<NA, NB, FA, FB, 16>::CF{});
+}
+#define FASTBFP_MX_EXPERTS_INSTANTIATE(NA, NB, FA, FB)                                                                \
+  template hipError_t launch_mx_experts_t<NA, NB, FA, FB>(bool, bool, const uint8_t*, const uint8_t*, int64_t,        \
+                                                          const uint8_t*, const uint8_t*, int64_t, int, int, int,    \
+                                                          float, float*, int64_t, const Segments&, hipStream_t);
+#define FASTBFP_MX_EXPERTS_DECLARE(NA, NB, FA, FB) extern FASTBFP_MX_EXPERTS_INSTANTIATE(NA, NB, FA, FB)
+#define FASTBFP_MX_EXPERTS_ALL(DO, NA, NB) DO(NA, NB, 0, 0) DO(NA, NB, 0, 1) DO(NA, NB, 1, 0) DO(NA, NB, 1, 1)
 
 #define FASTBFP_MX_DECLARE(NA, NB, FA, FB, G)                                                          \
   extern template hipError_t launch_mx_t<NA, NB, FA, FB, G>(const uint8_t*, const uint8_t*, int64_t,       \

@@ -1,0 +1,9 @@
+// gemm_mx_experts_12.hip -- the products of experts (gemm_mx.h, SEG) with 1 chunk
+// plane(s) of A and 2 of B, groups of 16, every plane-0 format of either operand.
+#include "gemm_mx.h"
+
+namespace fastbfp {
+
+FASTBFP_MX_EXPERTS_ALL(FASTBFP_MX_EXPERTS_INSTANTIATE, 1, 2)
+
+}  // namespace fastbfp

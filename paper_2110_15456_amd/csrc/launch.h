@@ -157,4 +157,39 @@ hipError_t launch_gemm_general(const uint8_t* a_mant, const uint8_t* a_exp, int 
                                const uint8_t* b_exp, int b_m, int m_b, int64_t M, int64_t N, int64_t K, int g,
                                float* C, int64_t ldc, int32_t* P, hipStream_t s, bool packed = false);
 
+
+// The expert layer (experts.hip, quantize.hip, gemm_experts.hip).
+//
+// Slots are the choices (token, j) of tokens x top experts, slot = token * top +
+// j.  Places of the token grouping: the least multiple of 128 that every routing
+// of `slots` slots over `experts` experts fits.
+constexpr int kMaxExperts = 512;  // (the counts of a workgroup of the plan: 35 KB of LDS)
+constexpr int kPlanBlock = 4096;  // slots a workgroup of the plan takes
+int64_t expert_places(int64_t slots, int experts);
+// int32 words of the plan's workspace (the counts of its workgroups; 0 for one).
+int64_t expert_plan_ws(int64_t slots, int experts);
+// order, place, offsets and k_offsets (include/fastbfp.h) of the routing ids.
+hipError_t launch_expert_plan(const void* ids, bool ids64, int64_t slots, int experts, int32_t* offsets,
+                              int32_t* k_offsets, int32_t* order, int32_t* place, int32_t* ws, hipStream_t s);
+// mr and er, or mc and ec, may be null (not both); top = 0: x in the experts'
+// order.
+hipError_t launch_quantize_experts(const float* x, int64_t rows, int64_t C, int top, const int32_t* order,
+                                   const int32_t* offsets, const int32_t* k_offsets, int experts, int64_t slots,
+                                   int64_t klen, int m, int mode, uint64_t seed_r, uint64_t seed_c, uint8_t* mr,
+                                   uint8_t* er, uint8_t* mc, uint8_t* ec, uint32_t* status, hipStream_t s);
+// C[p] = A[p] . B_e^T for the slots p of expert e (B: N rows of K for each).
+hipError_t launch_gemm_experts(const uint8_t* a_mant, const uint8_t* a_exp, int a_m, int na, const uint8_t* b_mant,
+                               const uint8_t* b_exp, int b_m, int nb, const int32_t* offsets, int experts,
+                               int64_t slots, int64_t N, int64_t K, int scale_log2, float* C, int64_t ldc,
+                               hipStream_t s);
+// C_e = A . B^T over the places of expert e.
+hipError_t launch_gemm_experts_grad(const uint8_t* a_mant, const uint8_t* a_exp, int a_m, int na, const uint8_t* b_mant,
+                                    const uint8_t* b_exp, int b_m, int nb, const int32_t* k_offsets, int experts,
+                                    int64_t M, int64_t N, int64_t klen, int scale_log2, float* C, hipStream_t s);
+hipError_t launch_combine_experts(const float* y, const float* gates, const int32_t* place, const int32_t* offsets,
+                                  int experts, int64_t tokens, int top, int64_t N, float* out, hipStream_t s);
+hipError_t launch_combine_experts_grad(const float* dout, const float* y, const float* gates, const int32_t* place,
+                                       const int32_t* offsets, int experts, int64_t tokens, int top, int64_t N,
+                                       float* dy, float* dgates, hipStream_t s);
+
 }  // namespace fastbfp

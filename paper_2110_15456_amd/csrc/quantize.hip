@@ -13,6 +13,7 @@
 #include <mutex>
 
 #include "bfp_quant.h"
+#include "segments.h"
 
 namespace fastbfp {
 
@@ -88,6 +89,32 @@ __global__ __launch_bounds__(1024) void k_improvement_finalize(double* out, cons
   }
 }
 
+// n / d for n < 2^31 with one high product (Granlund and Montgomery, PLDI'94,
+// figure 4.1: l = ceil(log2 d), mul = floor(2^32 (2^l - d) / d) + 1).
+struct Divisor {
+  uint32_t mul, l;
+  explicit Divisor(uint32_t d) : l(0) {
+    while ((uint64_t(1) << l) < d) ++l;
+    mul = (uint32_t)((((uint64_t(1) << l) - d) << 32) / d + 1);
+  }
+  __device__ __forceinline__ uint32_t div(uint32_t n) const {
+    const uint32_t t = __umulhi(mul, n);
+    return l == 0 ? n : (t + ((n - t) >> 1)) >> (l - 1);
+  }
+};
+
+// Rows taken from other places of x (GATHER of k_quantize_rows): row r is row
+// order[r] / top of x, whose rows hold `groups` groups.
+struct Gather {
+  const int32_t* order;
+  Divisor top, groups;
+  uint32_t row_groups;
+  int rows;  // of x
+};
+struct NoGather {};
+template <bool GATHER> struct GatherArg { typedef NoGather type; };
+template <> struct GatherArg<true> { typedef Gather type; };
+
 // Groups along the contiguous last axis: group gid covers x[gid*G, gid*G+G).
 // A lane owns GPL consecutive groups (two of 16 -- one 32-value packing unit
 // of the FP6 converter, also on the adaptive path -- or one of 32), a
@@ -99,11 +126,12 @@ __global__ __launch_bounds__(1024) void k_improvement_finalize(double* out, cons
 // all 64 banks on the read-back.  (Reading 64 contiguous bytes per lane
 // straight from global memory instead leaves each load instruction touching
 // 64 scattered 16-byte pieces, which costs about a third of HBM bandwidth.)
-template <int G, int MODE, int NCH, bool ADAPT, int P0, int P1>
+template <int G, int MODE, int NCH, bool ADAPT, int P0, int P1, bool GATHER = false>
 __global__ __launch_bounds__(256) void k_quantize_rows(const float* __restrict__ x, int64_t ngroups, uint32_t m,
                                                        uint32_t key0, uint32_t key1, uint8_t* __restrict__ mant0,
                                                        uint8_t* __restrict__ mant1, uint8_t* __restrict__ exps,
-                                                       uint32_t* status, double* part) {
+                                                       uint32_t* status, double* part,
+                                                       typename GatherArg<GATHER>::type from) {
   constexpr int GPL = G <= 16 ? 32 / G : 1;  // groups per lane: 32 values for g <= 16
   constexpr int CPG = G / 4;                         // 16-byte chunks per group
   constexpr int CPL = GPL * CPG;                     // 16-byte chunks per lane
@@ -123,6 +151,16 @@ __global__ __launch_bounds__(256) void k_quantize_rows(const float* __restrict__
     const int l = slot / CPL;
     const int c = (slot % CPL) ^ ((l / LANES_PER_SWZ) % CPL);
     // chunks of groups past the end reread the wave's last valid chunk (unused)
+    if constexpr (GATHER) {
+      const int q = min(l * CPL + c, qmax_chunk);
+      const uint32_t group = (uint32_t)g0 + (uint32_t)(q / CPG), row = from.groups.div(group);
+      const int src = min(max((int)from.top.div((uint32_t)from.order[row]), 0), from.rows - 1);
+      const uint8_t* at = reinterpret_cast<const uint8_t*>(x) +
+                          ((int64_t)src * from.row_groups + (group - row * from.row_groups)) * (G * 4) + (q % CPG) * 16;
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const void*>(at), (lds_void*)(&stage[wave][64 * 4 * k]), 16, 0,
+                                       0);  // (a row can be read again, for the token's other experts)
+      continue;
+    }
     const int off = min(l * CPL + c, qmax_chunk) * 16;
     __builtin_amdgcn_global_load_lds(reinterpret_cast<const void*>(base + off),
                                      (lds_void*)(&stage[wave][64 * 4 * k]), 16, 0, kStreamPolicy);
@@ -363,7 +401,7 @@ static hipError_t launch_rows_t(const float* x, int64_t ngroups, int m, uint64_t
   constexpr int GPL = G <= 16 ? 32 / G : 1;  // groups per lane (as in the kernel)
   const int64_t blocks = (ngroups + 256 * GPL - 1) / (256 * GPL);
   hipLaunchKernelGGL((k_quantize_rows<G, MODE, NCH, ADAPT, P0, P1>), dim3((unsigned)blocks), dim3(256), 0, s, x, ngroups,
-                     (uint32_t)m, (uint32_t)seed, (uint32_t)(seed >> 32), mant0, mant1, exps, status, part);
+                     (uint32_t)m, (uint32_t)seed, (uint32_t)(seed >> 32), mant0, mant1, exps, status, part, NoGather{});
   return hipGetLastError();
 }
 
@@ -691,6 +729,147 @@ hipError_t launch_weight_update(const float* w, const float* dw, float alpha, fl
                                 int m, int mode, uint64_t seed_r, uint64_t seed_c, uint8_t* mr, uint8_t* er,
                                 uint8_t* mc, uint8_t* ec, uint32_t* status, hipStream_t s) {
   return launch_dual_any<true>(w, dw, alpha, w_out, R, C, m, mode, seed_r, seed_c, mr, er, mc, ec, status, s);
+}
+
+// Both groupings of the slots of an expert layer (or the token grouping alone:
+// ROWS false), from one read of x.  Slot p of the experts' order is row order[p]
+// / top of x (top > 0), or row p (top = 0: x is in the experts' order already).
+// The row grouping is that of the slots in the experts' order (rows = slots, len
+// = C); the token grouping (rows = C, len = klen) has every expert's slots one
+// after another from k_offsets[e], a multiple of 128, with zeros behind them, so
+// that no group holds tokens of two experts and an expert's range is whole slabs
+// of the product that reads it.  Noise: gid is the group's index in its output.
+//
+// The tile, the order of tiles and the LDS layout are k_quantize_dual's, and so
+// is what bounds it, the transposed writes.  A tile of 64 token places lies
+// within one expert; the rows are read through registers, because places
+// behind an expert's last slot are zeros and rows can lie anywhere in x.
+struct ExpertSlots {
+  const int32_t* order;
+  const int32_t* offsets;    // first slot of each expert, in order
+  const int32_t* k_offsets;  // first place of each expert in the token grouping
+  int n, slots;              // experts, slots
+  int rows;                  // of x
+  Divisor top;
+  bool gather;
+};
+template <int MODE, int NCH, int P0, int P1, bool ROWS>
+__global__ __launch_bounds__(256) void k_quantize_experts(const float* __restrict__ x, ExpertSlots sl, int64_t C,
+                                                          int64_t klen, int tiles_c, uint32_t m, uint32_t kr0,
+                                                          uint32_t kr1, uint32_t kc0, uint32_t kc1,
+                                                          uint8_t* __restrict__ mr0, uint8_t* __restrict__ mr1,
+                                                          uint8_t* __restrict__ er, uint8_t* __restrict__ mc0,
+                                                          uint8_t* __restrict__ mc1, uint8_t* __restrict__ ec,
+                                                          uint32_t* status) {
+  constexpr int T = 64;
+  __shared__ __attribute__((aligned(16))) float tile[T * T];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  int lid = blockIdx.x;
+  if (gridDim.x % 8 == 0) lid = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+  const int tiles_r = (int)(klen / T), band = lid / (8 * tiles_c), in = lid % (8 * tiles_c);
+  const int band_rows = min(8, tiles_r - 8 * band);
+  const int place0 = (8 * band + in % band_rows) * T;
+  const int64_t c0 = (int64_t)(in / band_rows) * T;
+  // the expert whose places these are; none behind the last one's
+  int first = 0, rows = 0;
+  for (int c = 0; c < sl.n; c += 64) {
+    const int i = min(c + lane, sl.n - 1);
+    const uint64_t past = __ballot(sl.k_offsets[i + 1] > place0);
+    if (past) {
+      const int e = min(c + __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(past)), sl.n - 1);
+      const int f = sl.offsets[e] + place0 - sl.k_offsets[e];
+      first = min(max(f, 0), sl.slots);
+      rows = min(max(min(sl.offsets[e + 1], sl.slots) - first, 0), T);
+      break;
+    }
+  }
+  auto swz = [](int row) { return (row & 15) ^ (((row >> 4) & 3) << 2); };
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const int q = 64 * (4 * wave + n) + lane, row = q >> 4, g = (q & 15) ^ swz(row);
+    u32x4 v = u32x4{0u, 0u, 0u, 0u};
+    if (row < rows && c0 + 4 * g < C) {
+      int src = first + row;
+      if (sl.gather) src = (int)sl.top.div((uint32_t)sl.order[src]);
+      src = min(max(src, 0), sl.rows - 1);
+      v = *reinterpret_cast<const u32x4*>(x + (int64_t)src * C + c0 + 4 * g);
+    }
+    *reinterpret_cast<u32x4*>(&tile[4 * q]) = v;
+  }
+  __syncthreads();
+
+  bool bad = false;
+  uint32_t b[16], w[NCH][3], E, s_lo, s_hi;
+  bool nonfinite;
+  if constexpr (ROWS) {
+    const int row = 16 * wave + (lane & 15), cg = lane >> 4;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(&tile[row * T + 4 * ((4 * cg + u) ^ swz(row))]);
+      b[4 * u] = v[0];
+      b[4 * u + 1] = v[1];
+      b[4 * u + 2] = v[2];
+      b[4 * u + 3] = v[3];
+    }
+    if (row < rows && c0 + 16 * cg < C) {
+      const int64_t gid = (int64_t)(first + row) * (C / 16) + c0 / 16 + cg;
+      quantize_group<16, MODE, NCH, false, P0, P1, true>(b, m, (uint64_t)gid, kr0, kr1, w, E, nonfinite, s_lo, s_hi);
+      er[gid] = (uint8_t)E;
+      store_group<16, NCH, P0, P1>(mr0, mr1, gid, w);
+      bad |= nonfinite;
+    }
+  }
+  {
+    const int rg = lane >> 4, col = 16 * wave + (lane & 15);
+#pragma unroll
+    for (int u = 0; u < 16; ++u)
+      b[u] = __float_as_uint(tile[(16 * rg + u) * T + 4 * ((col >> 2) ^ swz(16 * rg + u)) + (col & 3)]);
+    if (c0 + col < C) {
+      const int64_t gid = (c0 + col) * (klen / 16) + place0 / 16 + rg;
+      quantize_group<16, MODE, NCH, false, P0, P1, true>(b, m, (uint64_t)gid, kc0, kc1, w, E, nonfinite, s_lo, s_hi);
+      ec[gid] = (uint8_t)E;
+      store_group<16, NCH, P0, P1>(mc0, mc1, gid, w);
+      bad |= nonfinite;
+    }
+  }
+  if (status && bad) atomicOr(status, 1u);
+}
+
+template <int MODE, int NCH, int P0, int P1>
+static hipError_t launch_experts_t(const float* x, const ExpertSlots& sl, int64_t C, int64_t klen, int m,
+                                   uint64_t seed_r, uint64_t seed_c, uint8_t* mr, uint8_t* er, uint8_t* mc,
+                                   uint8_t* ec, uint32_t* status, hipStream_t s) {
+  const int64_t b0 = plane_group_bytes(16, m, 0), rgroups = (int64_t)sl.slots * (C / 16), cgroups = C * (klen / 16);
+  if (!mc) {  // the row grouping alone, gathered
+    const Gather from{sl.order, sl.top, Divisor((uint32_t)(C / 16)), (uint32_t)(C / 16), sl.rows};
+    const int64_t blocks = (rgroups + 511) / 512;  // (two groups per lane)
+    hipLaunchKernelGGL((k_quantize_rows<16, MODE, NCH, false, P0, P1, true>), dim3((unsigned)blocks), dim3(256), 0, s, x,
+                       rgroups, (uint32_t)m, (uint32_t)seed_r, (uint32_t)(seed_r >> 32), mr, mr + rgroups * b0, er,
+                       status, nullptr, from);
+    return hipGetLastError();
+  }
+  const int tiles_c = (int)((C + 63) / 64);
+  const dim3 grid((unsigned)(klen / 64 * tiles_c));
+#define FASTBFP_EXPERTS(ROWS)                                                                                            hipLaunchKernelGGL((k_quantize_experts<MODE, NCH, P0, P1, ROWS>), grid, dim3(256), 0, s, x, sl, C, klen, tiles_c,                         (uint32_t)m, (uint32_t)seed_r, (uint32_t)(seed_r >> 32), (uint32_t)seed_c,                                             (uint32_t)(seed_c >> 32), mr, mr + rgroups * b0, er, mc, mc + cgroups * b0, ec, status)
+  if (mr) FASTBFP_EXPERTS(true);
+  else FASTBFP_EXPERTS(false);
+#undef FASTBFP_EXPERTS
+  return hipGetLastError();
+}
+
+hipError_t launch_quantize_experts(const float* x, int64_t rows, int64_t C, int top, const int32_t* order,
+                                   const int32_t* offsets, const int32_t* k_offsets, int experts, int64_t slots,
+                                   int64_t klen, int m, int mode, uint64_t seed_r, uint64_t seed_c, uint8_t* mr,
+                                   uint8_t* er, uint8_t* mc, uint8_t* ec, uint32_t* status, hipStream_t s) {
+  if (slots == 0 || C == 0) return hipSuccess;
+  if (!mc && top == 0) return launch_quantize_rows(x, slots, C, 16, m, mode, seed_r, mr, er, status, s);
+  const ExpertSlots sl{order, offsets, k_offsets, experts, (int)slots, (int)rows, Divisor((uint32_t)(top > 0 ? top : 1)),
+                       top > 0};
+#define FASTBFP_EXPERTS(MODE)                                                                                          do {                                                                                                                   if (m <= 2) return launch_experts_t<MODE, 1, kPlaneFP4, kPlaneFP6>(x, sl, C, klen, m, seed_r, seed_c, mr, er, mc,                                                                        ec, status, s);                                   if (m <= 4) return launch_experts_t<MODE, 1, kPlaneFP6, kPlaneFP6>(x, sl, C, klen, m, seed_r, seed_c, mr, er, mc,                                                                        ec, status, s);                                   if (m <= 6) return launch_experts_t<MODE, 2, kPlaneFP6, kPlaneLo2>(x, sl, C, klen, m, seed_r, seed_c, mr, er, mc,                                                                        ec, status, s);                                   return launch_experts_t<MODE, 2, kPlaneFP6, kPlaneFP6>(x, sl, C, klen, m, seed_r, seed_c, mr, er, mc, ec, status,                                                            s);                                                         } while (0)
+  if (mode == kNearest) FASTBFP_EXPERTS(kNearest);
+  if (mode == kStochastic) FASTBFP_EXPERTS(kStochastic);
+  FASTBFP_EXPERTS(kTruncate);
+#undef FASTBFP_EXPERTS
 }
 
 template <int NCH, int P0, int P1 = kPlaneFP6>
