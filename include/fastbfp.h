@@ -678,6 +678,34 @@ int bfp_combine_experts_grad(const float* dout, const float* y, const float* gat
                              const int32_t* offsets, int64_t tokens, int top, int experts, int64_t N, float* dy,
                              float* dgates, void* stream);
 
+/*
+ * bfp_orthogonalize -- a step of momentum whose result is orthogonalised, the
+ * direction of a weight update (for bfp_weight_update, with alpha = -learning
+ * rate, instead of the raw gradient).  For each of `batch` matrices [rows][cols]:
+ *   momentum_out = beta momentum + grad
+ *   U = grad + beta momentum_out (nesterov = 1) or momentum_out (0)
+ *   X = U / (Frobenius norm of U + eps)
+ *   `steps` times:  S = X X^T,  X = (a I + b S + c S^2) X   (X X^T on the shorter
+ *   side: X^T X where rows > cols), (a, b, c) = (3.4445, -4.7750, 2.0315)
+ *   out = X
+ * so that U's singular vectors stay and its singular values go to about 1 (five
+ * steps: 0.7 to 1.2 for those above 0.3% of the norm).  A zero U gives zeros.
+ *   grad, out    : FP32 [batch][rows][cols], contiguous, 4-byte aligned (16 for
+ *                  full speed).  out must not overlap the other arrays.
+ *   momentum     : the same, or NULL: U = grad and momentum_out is not written.
+ *   momentum_out : may be momentum (in place).
+ *   steps        : 1 .. 16;  eps >= 0.
+ *   workspace    : bfp_orthogonalize_ws_size bytes, 256-byte aligned; overwritten.
+ * Norms are summed in 64 bits.  The products are computed to about FP32's accuracy
+ * (operands in two FP16 planes, 22 bits; FP32 sums) in an order that depends on
+ * the sizes alone.  rows and cols below 2^20 and rows * cols up to 2^29
+ * (BFP_E_UNSUPPORTED beyond).
+ */
+int bfp_orthogonalize_ws_size(int64_t batch, int64_t rows, int64_t cols, size_t* workspace_bytes);
+int bfp_orthogonalize(const float* grad, const float* momentum, float* momentum_out, float beta, int nesterov,
+                      int64_t batch, int64_t rows, int64_t cols, int steps, float eps, float* out, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,7 +26,8 @@ __all__ = ["BFPTensor", "BFPError", "quantize", "quantize_dual", "weight_update"
            "gemm_group_partials", "quantize_adaptive", "quantize_adaptive_noalloc", "adaptive_threshold", "adaptive_mantissa", "chunks", "quantized_sizes", "ROUNDING",
            "PackedBFPTensor", "packed_sizes", "quantize_packed", "dequantize_packed", "gemm_packed", "repack",
            "gemm_ws_size", "ExpertPlan", "expert_plan", "quantize_experts", "gemm_experts", "gemm_experts_grad",
-           "combine_experts", "combine_experts_grad"]
+           "combine_experts", "combine_experts_grad", "orthogonalize", "orthogonal_update",
+           "orthogonalize_ws_size"]
 
 ROUNDING = {"nearest": 0, "stochastic": 1, "truncate": 2}
 
@@ -774,3 +775,75 @@ def combine_experts_grad(dout: torch.Tensor, y: torch.Tensor, plan: ExpertPlan, 
                                           place, off, plan.tokens, plan.top, plan.experts, N, dy.data_ptr(),
                                           dgates.data_ptr(), _stream(y.device)), "bfp_combine_experts_grad")
     return dy, dgates
+
+
+# ---- the orthogonalised update ----------------------------------------------
+
+
+@functools.lru_cache(maxsize=4096)
+def _orthogonalize_ws(batch, rows, cols):
+    """Workspace bytes of bfp_orthogonalize (a function of the sizes alone)."""
+    nb = ctypes.c_size_t(0)
+    check(load().bfp_orthogonalize_ws_size(batch, rows, cols, ctypes.byref(nb)), "bfp_orthogonalize_ws_size")
+    return nb.value
+
+
+def _orthogonalize(grad, momentum, momentum_out, beta, nesterov, steps, eps, out, workspace):
+    _need_cuda(grad, "grad", torch.float32)
+    if grad.dim() < 2:
+        raise ValueError("grad must be a matrix or a batch of them")
+    rows, cols = grad.shape[-2:]
+    batch = math.prod(grad.shape[:-2])
+    o = out if out is not None else torch.empty_like(grad)
+    _need_cuda(o, "out", torch.float32)
+    if o.shape != grad.shape:
+        raise ValueError("out has the wrong shape")
+    need = _orthogonalize_ws(batch, rows, cols)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=grad.device)
+    else:
+        _need_cuda(workspace, "workspace", torch.uint8)
+        if workspace.numel() < need:
+            raise ValueError("workspace needs %d bytes" % need)
+    check(load().bfp_orthogonalize(grad.data_ptr(), momentum.data_ptr() if momentum is not None else None,
+                                   momentum_out.data_ptr() if momentum_out is not None else None, beta,
+                                   1 if nesterov else 0, batch, rows, cols, steps, eps, o.data_ptr(),
+                                   workspace.data_ptr(), workspace.numel(), _stream(grad.device)), "bfp_orthogonalize")
+    return o
+
+
+def orthogonalize_ws_size(grad: torch.Tensor) -> int:
+    """Workspace bytes of orthogonalize and orthogonal_update for a gradient of this shape."""
+    return _orthogonalize_ws(math.prod(grad.shape[:-2]), *grad.shape[-2:])
+
+
+def orthogonalize(u: torch.Tensor, steps: int = 5, eps: float = 1e-7, out: torch.Tensor | None = None,
+                  workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Each matrix of u [..., rows, cols] with its singular vectors kept and its
+    singular values taken to about 1, by ``steps`` steps of the quintic
+    Newton-Schulz iteration from u / (|u|_F + eps) (see include/fastbfp.h).
+    ``workspace``: a uint8 tensor of at least orthogonalize_ws_size bytes, to
+    keep across steps; allocated here without one."""
+    return _orthogonalize(u, None, None, 0.0, False, steps, eps, out, workspace)
+
+
+def orthogonal_update(grad: torch.Tensor, momentum: torch.Tensor, beta: float = 0.95, nesterov: bool = True,
+                      steps: int = 5, eps: float = 1e-7, out: torch.Tensor | None = None,
+                      momentum_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """A step of momentum and its orthogonalised direction: ``(update,
+    momentum_out)`` with momentum_out = beta * momentum + grad (momentum updates
+    it in place when passed) and update the orthogonalize of grad + beta *
+    momentum_out (nesterov) or of momentum_out.  weight_update(w, update, -lr)
+    takes it to the weights and their two BFP groupings."""
+    _need_cuda(grad, "grad", torch.float32)
+    _need_cuda(momentum, "momentum", torch.float32)
+    if momentum.shape != grad.shape:
+        raise ValueError("momentum must have grad's shape")
+    if momentum_out is None:
+        momentum_out = torch.empty_like(momentum)
+    else:
+        _need_cuda(momentum_out, "momentum_out", torch.float32)
+        if momentum_out.shape != momentum.shape:
+            raise ValueError("momentum_out has the wrong shape")
+    o = _orthogonalize(grad, momentum, momentum_out, beta, nesterov, steps, eps, out, workspace)
+    return o, momentum_out

@@ -61,6 +61,9 @@ SIGNATURES = {
     "bfp_gemm_experts_grad": (_I, [_P, _P, _I, _P, _P, _I, _P, _I, _I64, _I64, _I64, _I, _I, _P, _P]),
     "bfp_combine_experts": (_I, [_P, _P, _P, _P, _I64, _I, _I, _I64, _P, _P]),
     "bfp_combine_experts_grad": (_I, [_P, _P, _P, _P, _P, _I64, _I, _I, _I64, _P, _P, _P]),
+    "bfp_orthogonalize_ws_size": (_I, [_I64, _I64, _I64, ctypes.POINTER(ctypes.c_size_t)]),
+    "bfp_orthogonalize": (_I, [_P, _P, _P, ctypes.c_float, _I, _I64, _I64, _I64, _I, ctypes.c_float, _P, _P,
+                               ctypes.c_size_t, _P]),
     "bfp_adaptive_mantissa": (_I, [ctypes.c_double, ctypes.c_double, ctypes.c_double]),
 }
 ABI_VERSION = 8

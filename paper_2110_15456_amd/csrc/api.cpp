@@ -109,6 +109,16 @@ int check_combine(const float* y, const float* gates, const int32_t* place, cons
   return BFP_OK;
 }
 
+// Matrices to orthogonalise: offsets within one stay below 2^31 bytes, and so do
+// the workgroups of all.
+int check_matrices(int64_t batch, int64_t rows, int64_t cols) {
+  if (batch < 0 || rows < 0 || cols < 0) return BFP_E_ARG;
+  if (rows >= (1 << 20) || cols >= (1 << 20) || rows * cols > (int64_t(1) << 29)) return BFP_E_UNSUPPORTED;
+  const int64_t tiles = ((rows + 63) / 64) * ((cols + 63) / 64);
+  if (tiles > 0 && batch > (int64_t(1) << 26) / (16 * tiles)) return BFP_E_UNSUPPORTED;
+  return BFP_OK;
+}
+
 size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 
 // How bfp_gemm_ws runs a product: which operands it repacks into the layout
@@ -780,6 +790,39 @@ int bfp_combine_experts_grad(const float* dout, const float* y, const float* gat
   }
   return status_of(fastbfp::launch_combine_experts_grad(dout, y, gates, place, offsets, experts, tokens, top, N, dy,
                                                         dgates, static_cast<hipStream_t>(stream)));
+}
+
+int bfp_orthogonalize_ws_size(int64_t batch, int64_t rows, int64_t cols, size_t* workspace_bytes) {
+  const int st = check_matrices(batch, rows, cols);
+  if (st != BFP_OK) return st;
+  if (!workspace_bytes) return BFP_E_ARG;
+  *workspace_bytes = batch > 0 && rows > 0 && cols > 0 ? (size_t)fastbfp::orthogonalize_ws(batch, rows, cols) : 0;
+  return BFP_OK;
+}
+
+int bfp_orthogonalize(const float* grad, const float* momentum, float* momentum_out, float beta, int nesterov,
+                      int64_t batch, int64_t rows, int64_t cols, int steps, float eps, float* out, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+  const int st = check_matrices(batch, rows, cols);
+  if (st != BFP_OK) return st;
+  if (steps < 1 || steps > 16 || (nesterov != 0 && nesterov != 1) || !(eps >= 0.0f)) return BFP_E_ARG;
+  if (batch == 0 || rows == 0 || cols == 0) return BFP_OK;
+  if (!grad || !out || (momentum && !momentum_out)) return BFP_E_ARG;
+  if (!aligned(grad, 4) || !aligned(momentum, 4) || !aligned(momentum_out, 4) || !aligned(out, 4)) return BFP_E_ARG;
+  const size_t need = (size_t)fastbfp::orthogonalize_ws(batch, rows, cols);
+  if (!workspace || workspace_bytes < need || !aligned(workspace, 256)) return BFP_E_ARG;
+  const uintptr_t bytes = (uintptr_t)batch * (uintptr_t)rows * (uintptr_t)cols * 4;
+  auto apart = [&](const void* a, const void* b) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    return !a || !b || p + bytes <= q || q + bytes <= p;
+  };
+  if (!apart(out, grad) || !apart(out, momentum)) return BFP_E_ARG;
+  if (momentum && (!apart(out, momentum_out) || !apart(grad, momentum_out) ||
+                   (momentum != momentum_out && !apart(momentum, momentum_out))))
+    return BFP_E_ARG;
+  return status_of(fastbfp::launch_orthogonalize(grad, momentum, momentum ? momentum_out : nullptr, beta,
+                                                 nesterov != 0, batch, rows, cols, steps, eps, out,
+                                                 static_cast<uint8_t*>(workspace), static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -192,4 +192,10 @@ hipError_t launch_combine_experts_grad(const float* dout, const float* y, const 
                                        const int32_t* offsets, int experts, int64_t tokens, int top, int64_t N,
                                        float* dy, float* dgates, hipStream_t s);
 
+// The orthogonalised update (orthogonalize.hip).  momentum null: of grad itself.
+int64_t orthogonalize_ws(int64_t batch, int64_t rows, int64_t cols);
+hipError_t launch_orthogonalize(const float* grad, const float* momentum, float* momentum_out, float beta,
+                                bool nesterov, int64_t batch, int64_t rows, int64_t cols, int steps, float eps,
+                                float* out, uint8_t* ws, hipStream_t s);
+
 }  // namespace fastbfp
