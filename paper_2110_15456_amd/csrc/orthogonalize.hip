@@ -8,6 +8,18 @@
 // X is kept with no more rows than columns (n <= k; the transpose of U where it
 // has more), so the products are n x n x k, n x n x n and n x k x n.
 //
+// Steps are taken two at a time.  With P = a I + b S + c S^2 the second step's S is
+// P S P, so X is needed twice for both, for S = X X^T and X <- P' P X, and in between
+// there are products of symmetric n x n matrices that commute (all are polynomials
+// of S), of which one triangle is computed.  In units of n^2 multiply-adds two
+// steps alone take 6 k + 2 n and a pair 3 k + 5 n: five steps of k = 4 n, in two
+// pairs and one, 47 n instead of 65; the same at k = n.  Rounding allows no more:
+// what P S P misses of the next X X^T grows by a^2 in each step of a group.  Over
+// noise, strong directions over noise, power laws, six decades of singular values
+// and two levels of them 1 to 10^5 apart, pairs had 0.7 to 2.4 times the error of
+// evaluating the formula in FP32 (single steps 0.6 to 2.5), groups of three up to
+// 12 times and five in one 40 times and more.
+//
 // Arithmetic.  The iteration grows small singular values by up to a^5 = 485,
 // and the errors of the products with them, so they are computed to FP32
 // accuracy: every matrix is two FP16 planes, hi = fp16(x 2^s) and lo = fp16(x 2^s
@@ -31,7 +43,7 @@ namespace fastbfp {
 namespace ns {
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
-constexpr int kXScale = 15, kSScale = 15, kPScale = 14;
+constexpr int kXScale = 15, kSScale = 15, kPScale = 14, kQScale = 12;
 
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
@@ -60,8 +72,10 @@ __device__ __forceinline__ void static_for(F&& f) {
   }
 }
 
-// What a product writes.
-enum { kParts, kPlanes, kF32, kF32T };
+// What a product writes: FP32 sums of a part of K; planes of a symmetric matrix,
+// alpha sum + beta m + gamma I, of the lower triangle's tiles and mirrored; planes;
+// FP32; FP32 transposed.
+enum { kParts, kSym, kPlanes, kF32, kF32T };
 
 struct Gemm {
   const uint8_t* a;  // planes, rows x blocks_k
@@ -71,11 +85,32 @@ struct Gemm {
   int M, N, K;       // C is M x N
   int tiles_m, tiles_n;  // (kParts: tiles_m alone, the lower triangle's tiles)
   int part_slabs, parts;
-  float scale;
-  uint8_t* c;        // planes, or FP32 rows of ldc
+  float alpha;
+  uint8_t* c;        // planes, or FP32; rows of ldc values
   int64_t c_batch, c_part;
   int ldc;
+  const uint8_t* m;  // kSym: planes as c's, or null
+  float beta, gamma;
 };
+
+// 16 bytes of a plane: hi or lo of eight values.
+__device__ __forceinline__ void store_chunk(uint8_t* o, const float (&x)[8], bool lo) {
+  h8 v;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    const _Float16 h = (_Float16)x[t];
+    v[t] = lo ? (_Float16)(x[t] - (float)h) : h;
+  }
+  *reinterpret_cast<h8*>(o) = v;
+}
+
+// Tile t of a lower triangle, row by row.
+__device__ __forceinline__ void triangle_tile(int t, int& tm, int& tn) {
+  tm = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+  while (tm * (tm + 1) / 2 > t) --tm;
+  while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
+  tn = t - tm * (tm + 1) / 2;
+}
 
 // Workgroup -> (item, tile): contiguous runs of workgroups on each XCD.
 __device__ __forceinline__ int xcd_order(int bid, int n) {
@@ -101,7 +136,7 @@ template <int BM, int BN, int WGM, int WGN, bool TR, int OUT>
 __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
   constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 32, TN = WN / 32;
   constexpr int OFF_B = BM * BLOCK, STAGE = OFF_B + BN * BLOCK;
-  constexpr bool SWAP = OUT != kF32T;  // a lane's quads: columns of one row, or rows of one column
+  constexpr bool TRI = OUT == kParts || OUT == kSym;
   static_assert((BM / 8) % NW == 0 && (BN / 8) % NW == 0 && NW % 2 == 0, "loads split evenly over the waves");
   __shared__ __attribute__((aligned(128))) uint8_t stage0[STAGE];
   __shared__ __attribute__((aligned(128))) uint8_t stage1[STAGE];
@@ -110,16 +145,12 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
 
   int id = xcd_order(blockIdx.x, gridDim.x), tm, tn, part = 0;
   int64_t batch;
-  if constexpr (OUT == kParts) {
+  if constexpr (TRI) {
     const int tiles = p.tiles_m * (p.tiles_m + 1) / 2;
-    const int t = id % tiles;
+    triangle_tile(id % tiles, tm, tn);
     id /= tiles;
     part = id % p.parts;
     batch = id / p.parts;
-    tm = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
-    while (tm * (tm + 1) / 2 > t) --tm;
-    while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
-    tn = t - tm * (tm + 1) / 2;
   } else {
     // bands of four tile rows, down each band's column first: the tiles that an
     // XCD runs at once share rows of A and columns of X
@@ -181,8 +212,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
     return __builtin_bit_cast(h8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
   };
   auto mma = [&](v16& c, const h8& a, const h8& b) __attribute__((always_inline)) {
-    c = SWAP ? __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, c, 0, 0, 0)
-             : __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, c, 0, 0, 0);  // (B first: a lane's quads are columns of a row)
   };
   auto step = [&](const uint8_t* cur, uint8_t* nxt, int s) __attribute__((always_inline)) {
     // this wave's loads of slab s have landed and its reads of slab s - 1 are done
@@ -219,65 +249,101 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
   }
   if (s < nslabs) step(stage0, stage1, s);
 
-  // Epilogue.  SWAP: lane holds columns 8 q + 4 fk .. + 3 of row fr of each 32 x 32
-  // tile; otherwise rows of column fr.
+  // Epilogue.  A lane holds columns 8 q + 4 fk .. + 3 of row fr of each 32 x 32
+  // tile.  64 x 64 values at a time go through the wave's 16 KB of the stages, so
+  // that rows and, mirrored, columns leave as whole lines.  16-byte granule g of row r
+  // sits at g ^ swz(r): 16 rows of one granule, and 8 rows 8 apart, on all banks.
+  __syncthreads();
+  static_assert(WN == 64 && TM % 2 == 0 && NW * 16384 <= 2 * STAGE, "a wave's sums fit in its share of the stages");
+  float* tile = reinterpret_cast<float*>((wave < NW / 2 ? stage0 : stage1) + (wave % (NW / 2)) * 16384);
+  auto at = [](int r, int g) __attribute__((always_inline)) -> int { return r * 64 + ((g ^ ((r ^ (r >> 3)) & 15)) * 4); };
   uint8_t* C = p.c + batch * p.c_batch + part * p.c_part;
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
+  for (int half = 0; half < TM / 2; ++half) {
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        v4 v;
+      for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) v[t] = acc[i][j][4 * q + t] * p.scale;
-        const int quad = 8 * q + 4 * fk;
-        if constexpr (OUT == kF32T) {
-          // C^T: columns row .. row + 3 of row col
-          const int row = row0 + wr * WM + 32 * i + quad, col = col0 + wc * WN + 32 * j + fr;
-          float* o = reinterpret_cast<float*>(C) + (int64_t)col * p.ldc + row;
-          if (col < p.N) {
-            if ((p.ldc & 3) == 0 && row + 3 < p.M) *reinterpret_cast<v4*>(o) = v;
-            else
+        for (int q = 0; q < 4; ++q) {
+          v4 v;
 #pragma unroll
-              for (int t = 0; t < 4; ++t)
-                if (row + t < p.M) o[t] = v[t];
-          }
-        } else {
-          const int row = row0 + wr * WM + 32 * i + fr, col = col0 + wc * WN + 32 * j + quad;
-          if (row >= p.M) continue;
-          if constexpr (OUT == kParts) {
-            if (col < p.ldc) *reinterpret_cast<v4*>(reinterpret_cast<float*>(C) + (int64_t)row * p.ldc + col) = v;
-          } else if constexpr (OUT == kPlanes) {
-            if (col < p.ldc) {
-              h4 hi, lo;
+          for (int t = 0; t < 4; ++t) v[t] = acc[2 * half + i][j][4 * q + t] * p.alpha;
+          *reinterpret_cast<v4*>(&tile[at(32 * i + fr, 8 * j + 2 * q + fk)]) = v;
+        }
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the wave reads back what it wrote
+    __builtin_amdgcn_wave_barrier();
+    const int r0 = row0 + wr * WM + 64 * half, c0 = col0 + wc * WN;
+    auto row8 = [&](int r, int c, float (&x)[8]) __attribute__((always_inline)) {
+      const v4 a = *reinterpret_cast<const v4*>(&tile[at(r, c / 4)]), b = *reinterpret_cast<const v4*>(&tile[at(r, c / 4 + 1)]);
 #pragma unroll
-              for (int t = 0; t < 4; ++t) {
-                hi[t] = (_Float16)v[t];
-                lo[t] = (_Float16)(v[t] - (float)hi[t]);
-              }
-              uint8_t* o = C + ((int64_t)row * (p.ldc / KS) + col / KS) * BLOCK + (col % KS) * 2;
-              *reinterpret_cast<h4*>(o) = hi;
-              *reinterpret_cast<h4*>(o + 64) = lo;
+      for (int t = 0; t < 4; ++t) x[t] = a[t], x[4 + t] = b[t];
+    };
+    auto col8 = [&](int r, int c, float (&x)[8]) __attribute__((always_inline)) {  // rows r .. r + 7 of column c
+#pragma unroll
+      for (int t = 0; t < 8; ++t) x[t] = tile[at(r + t, c / 4) + (c & 3)];
+    };
+    if constexpr (OUT == kSym || OUT == kPlanes) {
+      const int64_t line = (int64_t)(p.ldc / KS) * BLOCK;
+      const uint8_t* m = OUT == kSym && p.m ? p.m + batch * p.c_batch : nullptr;
+      for (int mirror = 0; mirror < (OUT == kSym && tm != tn ? 2 : 1); ++mirror) {
+        const int ro = mirror ? c0 : r0, co = mirror ? r0 : c0, rows = mirror ? p.N : p.M;
+#pragma unroll 4
+        for (int it = 0; it < 16; ++it) {
+          const int r = 4 * it + (lane >> 4), blk = (lane >> 3) & 1, lo = (lane >> 2) & 1, k = lane & 3;
+          const int c = blk * KS + 8 * k;
+          if (ro + r >= rows || co + c >= p.ldc) continue;
+          float x[8];
+          if (mirror) col8(c, r, x);
+          else row8(r, c, x);
+          const int64_t o = (int64_t)(ro + r) * line + (co + c) / KS * BLOCK + k * 16;
+          if constexpr (OUT == kSym) {
+            if (m) {
+              const h8 h = *reinterpret_cast<const h8*>(m + o), l = *reinterpret_cast<const h8*>(m + o + 64);
+#pragma unroll
+              for (int t = 0; t < 8; ++t) x[t] += p.beta * ((float)h[t] + (float)l[t]);
             }
-          } else {
-            float* o = reinterpret_cast<float*>(C) + (int64_t)row * p.ldc + col;
-            if ((p.ldc & 3) == 0 && col + 3 < p.N) *reinterpret_cast<v4*>(o) = v;
-            else
 #pragma unroll
-              for (int t = 0; t < 4; ++t)
-                if (col + t < p.N) o[t] = v[t];
+            for (int t = 0; t < 8; ++t)
+              if (ro + r == co + c + t) x[t] += p.gamma;
           }
+          store_chunk(C + o + lo * 64, x, lo);
+        }
+      }
+    } else {
+      float* o = reinterpret_cast<float*>(C);
+      const int ro = OUT == kF32T ? c0 : r0, co = OUT == kF32T ? r0 : c0;
+      const int rows = OUT == kF32T ? p.N : p.M, cols = OUT == kParts ? p.ldc : OUT == kF32T ? p.M : p.N;
+      const bool vec = (p.ldc & 3) == 0 && (reinterpret_cast<uintptr_t>(C) & 15) == 0;
+#pragma unroll 4
+      for (int it = 0; it < 16; ++it) {
+        const int r = 4 * it + (lane >> 4), c = 4 * (lane & 15);
+        v4 v;
+        if constexpr (OUT == kF32T) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) v[t] = tile[at(c + t, r / 4) + (r & 3)];
+        } else {
+          v = *reinterpret_cast<const v4*>(&tile[at(r, c / 4)]);
+        }
+        if (ro + r >= rows) continue;
+        float* d = o + (int64_t)(ro + r) * p.ldc + co + c;
+        if (vec && co + c + 3 < cols) {
+          *reinterpret_cast<v4*>(d) = v;
+        } else {
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            if (co + c + t < cols) d[t] = v[t];
         }
       }
     }
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // read before the next half overwrites it
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
-// out = alpha sum_parts + beta m + gamma I of symmetric n x n matrices, of whose
-// parts (FP32, rows of ld = blocks_of(n) * 32) the lower triangle's tiles are
-// there: one 64 x 64 tile per workgroup, written twice, as it is and mirrored.
-// Columns from n to ld become zeros.
+// What kSym writes of a product whose K went in parts: out = alpha sum_parts +
+// beta m + gamma I (sums in rows of ld = blocks_of(n) * 32), one 64 x 64 tile of
+// the lower triangle per workgroup.  Columns from n to ld become zeros.
 struct Finish {
   const float* sum;
   int64_t part, batch;  // strides, values
@@ -288,24 +354,14 @@ struct Finish {
   int n, ld, tiles;
   float alpha, beta, gamma;
 };
-__device__ __forceinline__ void store_chunk(uint8_t* o, const float (&x)[8], bool lo) {
-  h8 v;
-#pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    const _Float16 h = (_Float16)x[t];
-    v[t] = lo ? (_Float16)(x[t] - (float)h) : h;
-  }
-  *reinterpret_cast<h8*>(o) = v;
-}
 __global__ __launch_bounds__(256) void k_ns_finish(Finish p) {
   constexpr int T = 64;
   __shared__ float tile[T][T + 1];
   const int tiles = p.tiles * (p.tiles + 1) / 2, t = blockIdx.x % tiles;
   const int64_t batch = blockIdx.x / tiles;
-  int tm = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
-  while (tm * (tm + 1) / 2 > t) --tm;
-  while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
-  const int tn = t - tm * (tm + 1) / 2, r0 = tm * T, c0 = tn * T;
+  int tm, tn;
+  triangle_tile(t, tm, tn);
+  const int r0 = tm * T, c0 = tn * T;
   const uint8_t* m = p.m ? p.m + batch * p.m_batch : nullptr;
   for (int q = threadIdx.x; q < T * T / 4; q += 256) {
     const int r = q / (T / 4), c = 4 * (q % (T / 4)), row = r0 + r, col = c0 + c;
@@ -433,26 +489,43 @@ using namespace ns;
 
 int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
+// Tiles of 256 x 256 or 128 x 128 (one or two workgroups on each of 256 CUs), and
+// the parts that K is taken in: what the last, part-filled round leaves idle
+// decides.  A 256 tile takes four units of work for each slab, a 128 tile one, at
+// half of the rate where two share a CU; a part costs its sums' way to memory and
+// back.
+struct Tiling {
+  int tile, parts;
+};
+Tiling tiling(int64_t batch, int64_t tiles256, int64_t tiles128, int64_t slabs, bool split) {
+  Tiling best{128, 1};
+  double least = 1e30;
+  for (const int tile : {256, 128}) {
+    const int64_t tiles = batch * (tile == 256 ? tiles256 : tiles128);
+    for (int64_t parts = 1; parts == 1 || (split && parts <= 64 && slabs / parts >= 8); ++parts) {
+      const int64_t wgs = tiles * parts, ps = (slabs + parts - 1) / parts + 6;  // (six slabs' time to start and end)
+      double cost;
+      if (tile == 256) {
+        cost = 4.0 * (double)((wgs + 255) / 256) * ps;
+      } else {
+        const int64_t full = wgs / 512, rest = wgs % 512;
+        cost = (2.06 * full + (rest == 0 ? 0.0 : rest <= 256 ? 1.2 : 2.06)) * ps;
+      }
+      if (parts > 1) cost += 12.0 + 0.02 * wgs * (tile == 256 ? 4 : 1);
+      if (cost < least) least = cost, best = Tiling{tile, (int)parts};
+    }
+  }
+  return best;
+}
+
 // The iteration of one call: sizes of its matrices and where they lie in the
 // workspace.
 struct NsPlan {
   int64_t n, k, x_bytes, s_bytes, ld, part;  // one matrix: X, S (planes), row and part of sums (values)
-  int tile, gram_parts, square_parts, norm_blocks;
-  int64_t off_x[2], off_s, off_p, off_sum, off_norm, bytes;
+  Tiling gram, square, apply;
+  int norm_blocks;
+  int64_t off_x[2], off_s[2], off_p[3], off_sum, off_norm, bytes;
 };
-
-// Parts of K so that the lower triangle's tiles fill the card (256 workgroups of
-// 256 x 256, 512 of 128 x 128), with at least eight slabs in each.
-int parts_of(int64_t tiles, int64_t slabs, int64_t room) {
-  int64_t best = 1;
-  double best_cost = 1e30;
-  for (int64_t p = 1; p <= 16 && (p == 1 || slabs / p >= 8); ++p) {
-    const int64_t rounds = (tiles * p + room - 1) / room;
-    const double cost = (double)rounds * ((slabs + p - 1) / p + 4) + 2.0 * p;
-    if (cost < best_cost) best_cost = cost, best = p;
-  }
-  return (int)best;
-}
 
 NsPlan ns_plan(int64_t batch, int64_t rows, int64_t cols) {
   NsPlan p;
@@ -462,11 +535,10 @@ NsPlan ns_plan(int64_t batch, int64_t rows, int64_t cols) {
   p.x_bytes = p.n * blocks_of(p.k) * BLOCK;
   p.s_bytes = p.n * blocks_of(p.n) * BLOCK;
   p.part = p.n * p.ld;
-  const int64_t t256 = (p.n + 255) / 256;
-  p.tile = batch * t256 * (t256 + 1) / 2 >= 200 ? 256 : 128;
-  const int64_t t = (p.n + p.tile - 1) / p.tile, tiles = batch * t * (t + 1) / 2, room = p.tile == 256 ? 256 : 512;
-  p.gram_parts = parts_of(tiles, blocks_of(p.k), room);
-  p.square_parts = parts_of(tiles, blocks_of(p.n), room);
+  const int64_t n256 = (p.n + 255) / 256, n128 = (p.n + 127) / 128;
+  p.gram = tiling(batch, n256 * (n256 + 1) / 2, n128 * (n128 + 1) / 2, blocks_of(p.k), true);
+  p.square = tiling(batch, n256 * (n256 + 1) / 2, n128 * (n128 + 1) / 2, blocks_of(p.n), true);
+  p.apply = tiling(batch, n256 * ((p.k + 255) / 256), n128 * ((p.k + 127) / 128), blocks_of(p.n), false);
   const int64_t per = (p.n * p.k + 4095) / 4096;
   p.norm_blocks = (int)(per < kNormBlocks ? per : kNormBlocks);
   int64_t at = 0;
@@ -475,12 +547,11 @@ NsPlan ns_plan(int64_t batch, int64_t rows, int64_t cols) {
     at += up(bytes, 256);
     return o;
   };
-  p.off_x[0] = take(batch * p.x_bytes);
-  p.off_x[1] = take(batch * p.x_bytes);
-  p.off_s = take(batch * p.s_bytes);
-  p.off_p = take(batch * p.s_bytes);
-  const int64_t parts = p.gram_parts > p.square_parts ? p.gram_parts : p.square_parts;
-  p.off_sum = take(batch * parts * p.part * 4);
+  for (auto& o : p.off_x) o = take(batch * p.x_bytes);
+  for (auto& o : p.off_s) o = take(batch * p.s_bytes);
+  for (auto& o : p.off_p) o = take(batch * p.s_bytes);
+  const int64_t parts = p.gram.parts > p.square.parts ? p.gram.parts : p.square.parts;
+  p.off_sum = take(parts > 1 ? batch * parts * p.part * 4 : 0);
   p.off_norm = take(batch * p.norm_blocks * 8);
   p.bytes = at;
   return p;
@@ -506,7 +577,6 @@ hipError_t launch_orthogonalize(const float* grad, const float* momentum, float*
   const NsPlan p = ns_plan(batch, rows, cols);
   const int n = (int)p.n, k = (int)p.k, mode = !momentum ? 0 : nesterov ? 2 : 1;
   uint8_t* X[2] = {ws + p.off_x[0], ws + p.off_x[1]};
-  uint8_t *S = ws + p.off_s, *P = ws + p.off_p;
   float* sum = reinterpret_cast<float*>(ws + p.off_sum);
   double* norm = reinterpret_cast<double*>(ws + p.off_norm);
   const int64_t count = rows * cols;
@@ -531,39 +601,65 @@ hipError_t launch_orthogonalize(const float* grad, const float* momentum, float*
   e = hipGetLastError();
   if (e != hipSuccess) return e;
 
-  const int t = (n + p.tile - 1) / p.tile;
-  const int64_t tri = batch * t * (t + 1) / 2;
-  // sums of a symmetric product a b^T, its K in parts
-  auto product = [&](const uint8_t* a, int64_t a_batch, const uint8_t* b, int64_t b_batch, int K, int parts) {
-    const int slabs = (int)blocks_of(K), ps = (slabs + parts - 1) / parts;
-    Gemm g{a, a_batch, b, b_batch, n, n, K, t, t, ps, (slabs + ps - 1) / ps, 1.0f, reinterpret_cast<uint8_t*>(sum),
-           p.part * 4, batch * p.part * 4, (int)p.ld};
-    return std::pair<hipError_t, int>(run_gemm<false, kParts>(g, p.tile, tri * g.parts, s), g.parts);
-  };
-  auto finish = [&](int parts, const uint8_t* m, uint8_t* o, float alpha, float b, float gamma) {
+  // out = alpha a b^T + beta m + gamma I of symmetric n x n matrices
+  auto product = [&](const uint8_t* a, const uint8_t* b, int64_t batch_bytes, int K, const Tiling& how, uint8_t* o,
+                     float alpha, const uint8_t* m, float beta_m, float gamma) {
+    const int t = (n + how.tile - 1) / how.tile, slabs = (int)blocks_of(K);
+    const int ps = (slabs + how.parts - 1) / how.parts, parts = (slabs + ps - 1) / ps;
+    const int64_t tri = batch * t * (t + 1) / 2;
+    if (parts == 1)
+      return run_gemm<false, kSym>(Gemm{a, batch_bytes, b, batch_bytes, n, n, K, t, t, ps, 1, alpha, o, p.s_bytes, 0,
+                                        (int)p.ld, m, beta_m, gamma},
+                                   how.tile, tri, s);
+    hipError_t err = run_gemm<false, kParts>(Gemm{a, batch_bytes, b, batch_bytes, n, n, K, t, t, ps, parts, 1.0f,
+                                                  reinterpret_cast<uint8_t*>(sum), p.part * 4, batch * p.part * 4,
+                                                  (int)p.ld, nullptr, 0.0f, 0.0f},
+                                             how.tile, tri * parts, s);
+    if (err != hipSuccess) return err;
     const int tiles = (n + 63) / 64;
     hipLaunchKernelGGL(k_ns_finish, dim3((unsigned)(batch * tiles * (tiles + 1) / 2)), dim3(256), 0, s,
                        Finish{sum, batch * p.part, p.part, parts, m, o, p.s_bytes, p.s_bytes, n, (int)p.ld, tiles, alpha,
-                              b, gamma});
+                              beta_m, gamma});
     return hipGetLastError();
   };
-  const int at = (p.n + 255) / 256 * ((p.k + 255) / 256) * batch >= 200 ? 256 : 128;
-  for (int i = 0; i < steps; ++i) {
-    auto [e1, parts] = product(X[i & 1], p.x_bytes, X[i & 1], p.x_bytes, k, p.gram_parts);
-    if (e1 != hipSuccess) return e1;
-    e = finish(parts, nullptr, S, ldexpf(1.0f, kSScale - 2 * kXScale), 0.0f, 0.0f);
+  uint8_t *S = ws + p.off_s[0], *T = ws + p.off_s[1];
+  uint8_t* poly[3] = {ws + p.off_p[0], ws + p.off_p[1], ws + p.off_p[2]};
+  for (int done = 0, at = 0; done < steps; at ^= 1) {
+    // a pair pays from k = n on; near it its launches decide
+    const int group = p.k < p.n + p.n / 8 || steps - done < 2 ? 1 : 2;
+    e = product(X[at], X[at], p.x_bytes, k, p.gram, S, ldexpf(1.0f, kSScale - 2 * kXScale), nullptr, 0.0f, 0.0f);
     if (e != hipSuccess) return e;
-    auto [e2, parts2] = product(S, p.s_bytes, S, p.s_bytes, n, p.square_parts);
-    if (e2 != hipSuccess) return e2;
-    e = finish(parts2, S, P, ldexpf(kC, kPScale - 2 * kSScale), ldexpf(kB, kPScale - kSScale), ldexpf(kA, kPScale));
-    if (e != hipSuccess) return e;
-    const bool last = i + 1 == steps;
-    Gemm g{P, p.s_bytes, X[i & 1], p.x_bytes, n, k, n, (n + at - 1) / at, (k + at - 1) / at, 0, 1,
-           ldexpf(1.0f, last ? -kPScale - kXScale : -kPScale), last ? reinterpret_cast<uint8_t*>(out) : X[(i + 1) & 1],
-           last ? count * 4 : p.x_bytes, 0, last ? (int)cols : (int)(blocks_of(k) * KS)};
+    const uint8_t* Q = nullptr;
+    int q_scale = 0;
+    for (int i = 0; i < group; ++i) {
+      uint8_t* P = poly[i & 1];
+      if (i > 0) {  // S <- P S P of the last step's P
+        const float one = ldexpf(1.0f, -kPScale);
+        e = product(S, poly[(i - 1) & 1], p.s_bytes, n, p.square, T, one, nullptr, 0.0f, 0.0f);
+        if (e != hipSuccess) return e;
+        e = product(T, poly[(i - 1) & 1], p.s_bytes, n, p.square, S, one, nullptr, 0.0f, 0.0f);
+        if (e != hipSuccess) return e;
+      }
+      e = product(S, S, p.s_bytes, n, p.square, P, ldexpf(kC, kPScale - 2 * kSScale), S, ldexpf(kB, kPScale - kSScale),
+                  ldexpf(kA, kPScale));
+      if (e != hipSuccess) return e;
+      if (i == 0) {
+        Q = P, q_scale = kPScale;
+      } else {  // |P' P| < 3.45^2: 2^12 of it stays below FP16's end
+        e = product(P, Q, p.s_bytes, n, p.square, poly[2], ldexpf(1.0f, kQScale - 2 * kPScale), nullptr, 0.0f, 0.0f);
+        if (e != hipSuccess) return e;
+        Q = poly[2], q_scale = kQScale;
+      }
+    }
+    done += group;
+    const bool last = done == steps;
+    const int tile = p.apply.tile;
+    const Gemm g{Q, p.s_bytes, X[at], p.x_bytes, n, k, n, (n + tile - 1) / tile, (k + tile - 1) / tile, 0, 1,
+                 ldexpf(1.0f, last ? -q_scale - kXScale : -q_scale), last ? reinterpret_cast<uint8_t*>(out) : X[at ^ 1],
+                 last ? count * 4 : p.x_bytes, 0, last ? (int)cols : (int)(blocks_of(k) * KS), nullptr, 0.0f, 0.0f};
     const int64_t wgs = batch * g.tiles_m * g.tiles_n;
-    e = !last ? run_gemm<true, kPlanes>(g, at, wgs, s) : flip ? run_gemm<true, kF32T>(g, at, wgs, s)
-                                                              : run_gemm<true, kF32>(g, at, wgs, s);
+    e = !last ? run_gemm<true, kPlanes>(g, tile, wgs, s) : flip ? run_gemm<true, kF32T>(g, tile, wgs, s)
+                                                                : run_gemm<true, kF32>(g, tile, wgs, s);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
