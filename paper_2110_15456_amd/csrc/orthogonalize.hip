@@ -72,10 +72,9 @@ __device__ __forceinline__ void static_for(F&& f) {
   }
 }
 
-// What a product writes: FP32 sums of a part of K; planes of a symmetric matrix,
-// alpha sum + beta m + gamma I, of the lower triangle's tiles and mirrored; planes;
-// FP32; FP32 transposed.
-enum { kParts, kSym, kPlanes, kF32, kF32T };
+// What a product writes: planes of a symmetric matrix, alpha sum + beta m + gamma I,
+// of the lower triangle's tiles and mirrored; planes; FP32; FP32 transposed.
+enum { kSym, kPlanes, kF32, kF32T };
 
 struct Gemm {
   const uint8_t* a;  // planes, rows x blocks_k
@@ -83,14 +82,17 @@ struct Gemm {
   const uint8_t* b;  // planes: rows of the product's columns (TR: X itself, rows of its K)
   int64_t b_batch;
   int M, N, K;       // C is M x N
-  int tiles_m, tiles_n;  // (kParts: tiles_m alone, the lower triangle's tiles)
-  int part_slabs, parts;
+  int tiles_m, tiles_n;  // (kSym: tiles_m alone, the lower triangle's tiles)
   float alpha;
   uint8_t* c;        // planes, or FP32; rows of ldc values
-  int64_t c_batch, c_part;
+  int64_t c_batch;
   int ldc;
-  const uint8_t* m;  // kSym: planes as c's, or null
+  // kSym
+  const uint8_t* m;  // planes as c's, or null
   float beta, gamma;
+  int whole;         // tiles (of all matrices) from here on are summed in parts of K
+  int parts, part_slabs;
+  float* sums;       // [tile - whole][part][BM][BN]
 };
 
 // 16 bytes of a plane: hi or lo of eight values.
@@ -112,7 +114,7 @@ __device__ __forceinline__ void triangle_tile(int t, int& tm, int& tn) {
   tn = t - tm * (tm + 1) / 2;
 }
 
-// Workgroup -> (item, tile): contiguous runs of workgroups on each XCD.
+// Workgroup -> item: contiguous runs of items on each XCD.
 __device__ __forceinline__ int xcd_order(int bid, int n) {
   const int xcd = bid % 8;
   return xcd * (n / 8) + min(xcd, n % 8) + bid / 8;
@@ -136,25 +138,33 @@ template <int BM, int BN, int WGM, int WGN, bool TR, int OUT>
 __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
   constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 32, TN = WN / 32;
   constexpr int OFF_B = BM * BLOCK, STAGE = OFF_B + BN * BLOCK;
-  constexpr bool TRI = OUT == kParts || OUT == kSym;
   static_assert((BM / 8) % NW == 0 && (BN / 8) % NW == 0 && NW % 2 == 0, "loads split evenly over the waves");
   __shared__ __attribute__((aligned(128))) uint8_t stage0[STAGE];
   __shared__ __attribute__((aligned(128))) uint8_t stage1[STAGE];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int wr = wave / WGN, wc = wave % WGN;
 
-  int id = xcd_order(blockIdx.x, gridDim.x), tm, tn, part = 0;
+  int tm, tn, slab0 = 0, nslabs = (int)blocks_of(p.K);
   int64_t batch;
-  if constexpr (TRI) {
-    const int tiles = p.tiles_m * (p.tiles_m + 1) / 2;
-    triangle_tile(id % tiles, tm, tn);
-    id /= tiles;
-    part = id % p.parts;
-    batch = id / p.parts;
+  float* sums = nullptr;  // where the sums of a part go
+  if constexpr (OUT == kSym) {
+    const int bid = blockIdx.x, tiles = p.tiles_m * (p.tiles_m + 1) / 2;
+    int t = bid;
+    if (bid < p.whole) {
+      t = xcd_order(bid, p.whole);
+    } else {
+      const int part = (bid - p.whole) % p.parts;
+      t = p.whole + (bid - p.whole) / p.parts;
+      slab0 = part * p.part_slabs;
+      nslabs = min(p.part_slabs, nslabs - slab0);
+      sums = p.sums + (int64_t)(bid - p.whole) * (BM * BN);
+    }
+    triangle_tile(t % tiles, tm, tn);
+    batch = t / tiles;
   } else {
     // bands of four tile rows, down each band's column first: the tiles that an
     // XCD runs at once share rows of A and columns of X
-    const int tiles = p.tiles_m * p.tiles_n, t = id % tiles;
+    const int id = xcd_order(blockIdx.x, gridDim.x), tiles = p.tiles_m * p.tiles_n, t = id % tiles;
     batch = id / tiles;
     const int band = t / (4 * p.tiles_n), in = t % (4 * p.tiles_n), rows = min(4, p.tiles_m - 4 * band);
     tm = 4 * band + in % rows;
@@ -167,8 +177,6 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
   const rsrc_t ra = make_rsrc(A, (uint32_t)min(BM, p.M - row0) * a_row);
   const uint8_t* B = p.b + batch * p.b_batch + (TR ? (int64_t)col0 * 4 : (int64_t)col0 * b_row);
   const rsrc_t rb = make_rsrc(B, TR ? (uint32_t)p.K * b_row - (uint32_t)col0 * 4 : (uint32_t)min(BN, p.N - col0) * b_row);
-  const int all = (int)blocks_of(p.K), slab0 = part * p.part_slabs;
-  const int nslabs = OUT == kParts ? min(p.part_slabs, all - slab0) : all;
 
   v16 acc[TM][TN];
 #pragma unroll
@@ -257,7 +265,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
   static_assert(WN == 64 && TM % 2 == 0 && NW * 16384 <= 2 * STAGE, "a wave's sums fit in its share of the stages");
   float* tile = reinterpret_cast<float*>((wave < NW / 2 ? stage0 : stage1) + (wave % (NW / 2)) * 16384);
   auto at = [](int r, int g) __attribute__((always_inline)) -> int { return r * 64 + ((g ^ ((r ^ (r >> 3)) & 15)) * 4); };
-  uint8_t* C = p.c + batch * p.c_batch + part * p.c_part;
+  uint8_t* C = p.c + batch * p.c_batch;
+  const float alpha = OUT == kSym && sums ? 1.0f : p.alpha;
 #pragma unroll
   for (int half = 0; half < TM / 2; ++half) {
 #pragma unroll
@@ -268,7 +277,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
         for (int q = 0; q < 4; ++q) {
           v4 v;
 #pragma unroll
-          for (int t = 0; t < 4; ++t) v[t] = acc[2 * half + i][j][4 * q + t] * p.alpha;
+          for (int t = 0; t < 4; ++t) v[t] = acc[2 * half + i][j][4 * q + t] * alpha;
           *reinterpret_cast<v4*>(&tile[at(32 * i + fr, 8 * j + 2 * q + fk)]) = v;
         }
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the wave reads back what it wrote
@@ -283,7 +292,14 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
 #pragma unroll
       for (int t = 0; t < 8; ++t) x[t] = tile[at(r + t, c / 4) + (c & 3)];
     };
-    if constexpr (OUT == kSym || OUT == kPlanes) {
+    if (OUT == kSym && sums) {
+      float* o = sums + (wr * WM + 64 * half) * BN + wc * WN;
+#pragma unroll 4
+      for (int it = 0; it < 16; ++it) {
+        const int r = 4 * it + (lane >> 4), c = 4 * (lane & 15);
+        *reinterpret_cast<v4*>(o + r * BN + c) = *reinterpret_cast<const v4*>(&tile[at(r, c / 4)]);
+      }
+    } else if constexpr (OUT == kSym || OUT == kPlanes) {
       const int64_t line = (int64_t)(p.ldc / KS) * BLOCK;
       const uint8_t* m = OUT == kSym && p.m ? p.m + batch * p.c_batch : nullptr;
       for (int mirror = 0; mirror < (OUT == kSym && tm != tn ? 2 : 1); ++mirror) {
@@ -313,7 +329,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
     } else {
       float* o = reinterpret_cast<float*>(C);
       const int ro = OUT == kF32T ? c0 : r0, co = OUT == kF32T ? r0 : c0;
-      const int rows = OUT == kF32T ? p.N : p.M, cols = OUT == kParts ? p.ldc : OUT == kF32T ? p.M : p.N;
+      const int rows = OUT == kF32T ? p.N : p.M, cols = OUT == kF32T ? p.M : p.N;
       const bool vec = (p.ldc & 3) == 0 && (reinterpret_cast<uintptr_t>(C) & 15) == 0;
 #pragma unroll 4
       for (int it = 0; it < 16; ++it) {
@@ -341,62 +357,48 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
   }
 }
 
-// What kSym writes of a product whose K went in parts: out = alpha sum_parts +
-// beta m + gamma I (sums in rows of ld = blocks_of(n) * 32), one 64 x 64 tile of
-// the lower triangle per workgroup.  Columns from n to ld become zeros.
-struct Finish {
-  const float* sum;
-  int64_t part, batch;  // strides, values
-  int parts;
-  const uint8_t* m;     // planes, or null
-  uint8_t* out;         // planes
-  int64_t m_batch, out_batch;
-  int n, ld, tiles;
-  float alpha, beta, gamma;
-};
-__global__ __launch_bounds__(256) void k_ns_finish(Finish p) {
-  constexpr int T = 64;
+// What kSym writes of the tiles that were summed in parts of K: a 32 x 32 piece of
+// one per workgroup, four values per thread (bound by the latency of the parts'
+// loads: 64 x 64 pieces took 22 us for 16 tiles in 16 parts).
+template <int BT>
+__global__ __launch_bounds__(256) void k_ns_finish(Gemm p) {
+  constexpr int T = 32, PIECES = (BT / T) * (BT / T);
   __shared__ float tile[T][T + 1];
-  const int tiles = p.tiles * (p.tiles + 1) / 2, t = blockIdx.x % tiles;
-  const int64_t batch = blockIdx.x / tiles;
+  const int tiles = p.tiles_m * (p.tiles_m + 1) / 2, split = blockIdx.x / PIECES, piece = blockIdx.x % PIECES;
+  const int t = p.whole + split;
+  const int64_t batch = t / tiles;
   int tm, tn;
-  triangle_tile(t, tm, tn);
-  const int r0 = tm * T, c0 = tn * T;
-  const uint8_t* m = p.m ? p.m + batch * p.m_batch : nullptr;
-  for (int q = threadIdx.x; q < T * T / 4; q += 256) {
-    const int r = q / (T / 4), c = 4 * (q % (T / 4)), row = r0 + r, col = c0 + c;
+  triangle_tile(t % tiles, tm, tn);
+  const int pr = piece / (BT / T) * T, pc = piece % (BT / T) * T, r0 = tm * BT + pr, c0 = tn * BT + pc;
+  if (r0 >= p.M || c0 >= p.ldc) return;
+  const uint8_t* m = p.m ? p.m + batch * p.c_batch : nullptr;
+  const int64_t line = (int64_t)(p.ldc / KS) * BLOCK;
+  const float* sums = p.sums + (int64_t)split * p.parts * (BT * BT) + pr * BT + pc;
+  {
+    const int r = threadIdx.x / (T / 4), c = 4 * (threadIdx.x % (T / 4)), row = r0 + r, col = c0 + c;
     v4 v = {};
-    if (row < p.n && col < p.n) {
-      const float* at = p.sum + batch * p.batch + (int64_t)row * p.ld + col;
-      for (int i = 0; i < p.parts; ++i) v += *reinterpret_cast<const v4*>(at + i * p.part);
-      v *= p.alpha;
-      if (m) {
-        const uint8_t* o = m + ((int64_t)row * (p.ld / KS) + col / KS) * BLOCK + (col % KS) * 2;
-        const h4 hi = *reinterpret_cast<const h4*>(o), lo = *reinterpret_cast<const h4*>(o + 64);
+#pragma unroll 8
+    for (int i = 0; i < p.parts; ++i) v += *reinterpret_cast<const v4*>(sums + (int64_t)i * (BT * BT) + r * BT + c);
+    v *= p.alpha;
+    if (m && row < p.M) {
+      const uint8_t* o = m + row * line + col / KS * BLOCK + (col % KS) * 2;
+      const h4 hi = *reinterpret_cast<const h4*>(o), lo = *reinterpret_cast<const h4*>(o + 64);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] += p.beta * ((float)hi[k] + (float)lo[k]);
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (row == col + k) v[k] += p.gamma;
-        if (col + k >= p.n) v[k] = 0.0f;
-      }
+      for (int k = 0; k < 4; ++k) v[k] += p.beta * ((float)hi[k] + (float)lo[k]);
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) tile[r][c + k] = v[k];
+    for (int k = 0; k < 4; ++k) tile[r][c + k] = v[k] + (row == col + k ? p.gamma : 0.0f);
   }
   __syncthreads();
-  uint8_t* out = p.out + batch * p.out_batch;
+  uint8_t* out = p.c + batch * p.c_batch;
   for (int mirror = 0; mirror < (tm == tn ? 1 : 2); ++mirror) {
     const int ro = mirror ? c0 : r0, co = mirror ? r0 : c0;
-    for (int q = threadIdx.x; q < T * 16; q += 256) {  // 16 chunks of 16 bytes a row
-      const int r = q / 16, blk = (q % 16) / 8, lo = (q % 8) / 4, k = q % 4, col = blk * KS + 8 * k;
-      if (ro + r >= p.n || co + col >= p.ld) continue;
-      float x[8];
+    const int r = threadIdx.x / 8, lo = (threadIdx.x & 4) / 4, k = threadIdx.x & 3;  // 8 chunks of 16 bytes a row
+    if (ro + r >= p.M || co >= p.ldc) continue;
+    float x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = mirror ? tile[col + i][r] : tile[r][col + i];
-      store_chunk(out + ((int64_t)(ro + r) * (p.ld / KS) + (co + col) / KS) * BLOCK + lo * 64 + k * 16, x, lo);
-    }
+    for (int i = 0; i < 8; ++i) x[i] = mirror ? tile[8 * k + i][r] : tile[r][8 * k + i];
+    store_chunk(out + (ro + r) * line + co / KS * BLOCK + lo * 64 + k * 16, x, lo);
   }
 }
 
@@ -448,7 +450,8 @@ __global__ __launch_bounds__(256) void k_ns_split(const float* __restrict__ g, c
   __shared__ double red[4];
   const int64_t matrix = blockIdx.x / per_matrix, t = blockIdx.x % per_matrix, base = matrix * ((int64_t)n * k);
   const int r0 = (int)(t / tiles_n) * T, c0 = (int)(t % tiles_n) * T;
-  double sum = (int)threadIdx.x < blocks ? part[matrix * blocks + threadIdx.x] : 0.0;
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < blocks; i += 256) sum += part[matrix * blocks + i];
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
@@ -479,7 +482,7 @@ __global__ __launch_bounds__(256) void k_ns_split(const float* __restrict__ g, c
   }
 }
 
-constexpr int kNormBlocks = 256;
+constexpr int kNormBlocks = 2048;
 
 }  // namespace ns
 
@@ -489,30 +492,31 @@ using namespace ns;
 
 int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
-// Tiles of 256 x 256 or 128 x 128 (one or two workgroups on each of 256 CUs), and
-// the parts that K is taken in: what the last, part-filled round leaves idle
-// decides.  A 256 tile takes four units of work for each slab, a 128 tile one, at
-// half of the rate where two share a CU; a part costs its sums' way to memory and
-// back.
+// Tiles of 256 x 256 or 128 x 128 (one or two workgroups on each of 256 CUs).
+// Whole rounds of tiles run as they are; those left over, where the product may be
+// split, are summed in parts of K that share out the last round.  Priced in slabs of
+// a 128 tile alone on a CU: a 256 tile's slab takes four, two 128 tiles that share a
+// CU 2.06, a tile six slabs' time to start and end, a split a second launch and its
+// sums' way to memory and back.  (n = 4096, K = 4096, 528 tiles of 128: whole 251 us,
+// all of them in three parts 239.)
 struct Tiling {
   int tile, parts;
+  int64_t whole;
 };
-Tiling tiling(int64_t batch, int64_t tiles256, int64_t tiles128, int64_t slabs, bool split) {
-  Tiling best{128, 1};
+Tiling tiling(int64_t tiles256, int64_t tiles128, int64_t slabs, bool split) {
+  Tiling best{128, 1, tiles128};
   double least = 1e30;
   for (const int tile : {256, 128}) {
-    const int64_t tiles = batch * (tile == 256 ? tiles256 : tiles128);
-    for (int64_t parts = 1; parts == 1 || (split && parts <= 64 && slabs / parts >= 8); ++parts) {
-      const int64_t wgs = tiles * parts, ps = (slabs + parts - 1) / parts + 6;  // (six slabs' time to start and end)
-      double cost;
-      if (tile == 256) {
-        cost = 4.0 * (double)((wgs + 255) / 256) * ps;
-      } else {
-        const int64_t full = wgs / 512, rest = wgs % 512;
-        cost = (2.06 * full + (rest == 0 ? 0.0 : rest <= 256 ? 1.2 : 2.06)) * ps;
-      }
-      if (parts > 1) cost += 12.0 + 0.02 * wgs * (tile == 256 ? 4 : 1);
-      if (cost < least) least = cost, best = Tiling{tile, (int)parts};
+    const int64_t tiles = tile == 256 ? tiles256 : tiles128, room = tile == 256 ? 256 : 512;
+    const double slab = tile == 256 ? 4.0 : 2.06;
+    const int64_t whole = tiles / room * room, rest = tiles - whole;
+    for (int64_t parts = 1; parts == 1 || (split && rest > 0 && parts <= 64 && slabs / parts >= 4); ++parts) {
+      const int64_t wgs = rest * parts, ps = (slabs + parts - 1) / parts;
+      const int64_t full = wgs / room, left = wgs % room;
+      const double last = left == 0 ? 0.0 : tile == 128 && left <= 256 ? 1.2 : slab;
+      double cost = (double)(whole / room) * slab * (slabs + 6) + (full * slab + last) * (ps + 6);
+      if (parts > 1) cost += 8.0 + (tile == 256 ? 0.08 : 0.02) * wgs;
+      if (cost < least) least = cost, best = Tiling{tile, (int)parts, parts > 1 ? whole : tiles};
     }
   }
   return best;
@@ -521,7 +525,7 @@ Tiling tiling(int64_t batch, int64_t tiles256, int64_t tiles128, int64_t slabs, 
 // The iteration of one call: sizes of its matrices and where they lie in the
 // workspace.
 struct NsPlan {
-  int64_t n, k, x_bytes, s_bytes, ld, part;  // one matrix: X, S (planes), row and part of sums (values)
+  int64_t n, k, x_bytes, s_bytes, ld;  // one matrix: X, S (planes), values in a row of S
   Tiling gram, square, apply;
   int norm_blocks;
   int64_t off_x[2], off_s[2], off_p[3], off_sum, off_norm, bytes;
@@ -534,11 +538,11 @@ NsPlan ns_plan(int64_t batch, int64_t rows, int64_t cols) {
   p.ld = blocks_of(p.n) * KS;
   p.x_bytes = p.n * blocks_of(p.k) * BLOCK;
   p.s_bytes = p.n * blocks_of(p.n) * BLOCK;
-  p.part = p.n * p.ld;
   const int64_t n256 = (p.n + 255) / 256, n128 = (p.n + 127) / 128;
-  p.gram = tiling(batch, n256 * (n256 + 1) / 2, n128 * (n128 + 1) / 2, blocks_of(p.k), true);
-  p.square = tiling(batch, n256 * (n256 + 1) / 2, n128 * (n128 + 1) / 2, blocks_of(p.n), true);
-  p.apply = tiling(batch, n256 * ((p.k + 255) / 256), n128 * ((p.k + 127) / 128), blocks_of(p.n), false);
+  const int64_t tri256 = batch * n256 * (n256 + 1) / 2, tri128 = batch * n128 * (n128 + 1) / 2;
+  p.gram = tiling(tri256, tri128, blocks_of(p.k), true);
+  p.square = tiling(tri256, tri128, blocks_of(p.n), true);
+  p.apply = tiling(batch * n256 * ((p.k + 255) / 256), batch * n128 * ((p.k + 127) / 128), blocks_of(p.n), false);
   const int64_t per = (p.n * p.k + 4095) / 4096;
   p.norm_blocks = (int)(per < kNormBlocks ? per : kNormBlocks);
   int64_t at = 0;
@@ -550,8 +554,12 @@ NsPlan ns_plan(int64_t batch, int64_t rows, int64_t cols) {
   for (auto& o : p.off_x) o = take(batch * p.x_bytes);
   for (auto& o : p.off_s) o = take(batch * p.s_bytes);
   for (auto& o : p.off_p) o = take(batch * p.s_bytes);
-  const int64_t parts = p.gram.parts > p.square.parts ? p.gram.parts : p.square.parts;
-  p.off_sum = take(parts > 1 ? batch * parts * p.part * 4 : 0);
+  int64_t sums = 0;
+  for (const Tiling& t : {p.gram, p.square}) {
+    const int64_t tiles = t.tile == 256 ? tri256 : tri128, bytes = (tiles - t.whole) * t.parts * t.tile * t.tile * 4;
+    sums = bytes > sums ? bytes : sums;
+  }
+  p.off_sum = take(sums);
   p.off_norm = take(batch * p.norm_blocks * 8);
   p.bytes = at;
   return p;
@@ -604,22 +612,15 @@ hipError_t launch_orthogonalize(const float* grad, const float* momentum, float*
   // out = alpha a b^T + beta m + gamma I of symmetric n x n matrices
   auto product = [&](const uint8_t* a, const uint8_t* b, int64_t batch_bytes, int K, const Tiling& how, uint8_t* o,
                      float alpha, const uint8_t* m, float beta_m, float gamma) {
-    const int t = (n + how.tile - 1) / how.tile, slabs = (int)blocks_of(K);
-    const int ps = (slabs + how.parts - 1) / how.parts, parts = (slabs + ps - 1) / ps;
-    const int64_t tri = batch * t * (t + 1) / 2;
-    if (parts == 1)
-      return run_gemm<false, kSym>(Gemm{a, batch_bytes, b, batch_bytes, n, n, K, t, t, ps, 1, alpha, o, p.s_bytes, 0,
-                                        (int)p.ld, m, beta_m, gamma},
-                                   how.tile, tri, s);
-    hipError_t err = run_gemm<false, kParts>(Gemm{a, batch_bytes, b, batch_bytes, n, n, K, t, t, ps, parts, 1.0f,
-                                                  reinterpret_cast<uint8_t*>(sum), p.part * 4, batch * p.part * 4,
-                                                  (int)p.ld, nullptr, 0.0f, 0.0f},
-                                             how.tile, tri * parts, s);
-    if (err != hipSuccess) return err;
-    const int tiles = (n + 63) / 64;
-    hipLaunchKernelGGL(k_ns_finish, dim3((unsigned)(batch * tiles * (tiles + 1) / 2)), dim3(256), 0, s,
-                       Finish{sum, batch * p.part, p.part, parts, m, o, p.s_bytes, p.s_bytes, n, (int)p.ld, tiles, alpha,
-                              beta_m, gamma});
+    const int64_t t = (n + how.tile - 1) / how.tile, tri = batch * t * (t + 1) / 2;
+    const int slabs = (int)blocks_of(K), ps = (slabs + how.parts - 1) / how.parts, parts = (slabs + ps - 1) / ps;
+    const Gemm g{a, batch_bytes, b, batch_bytes, n, n, K, (int)t, (int)t, alpha, o, p.s_bytes, (int)p.ld, m, beta_m,
+                 gamma, (int)how.whole, parts, ps, sum};
+    const hipError_t err = run_gemm<false, kSym>(g, how.tile, how.whole + (tri - how.whole) * parts, s);
+    if (err != hipSuccess || how.whole == tri) return err;
+    const int64_t pieces = (tri - how.whole) * (how.tile / 32) * (how.tile / 32);
+    if (how.tile == 256) hipLaunchKernelGGL(k_ns_finish<256>, dim3((unsigned)pieces), dim3(256), 0, s, g);
+    else hipLaunchKernelGGL(k_ns_finish<128>, dim3((unsigned)pieces), dim3(256), 0, s, g);
     return hipGetLastError();
   };
   uint8_t *S = ws + p.off_s[0], *T = ws + p.off_s[1];
@@ -654,9 +655,10 @@ hipError_t launch_orthogonalize(const float* grad, const float* momentum, float*
     done += group;
     const bool last = done == steps;
     const int tile = p.apply.tile;
-    const Gemm g{Q, p.s_bytes, X[at], p.x_bytes, n, k, n, (n + tile - 1) / tile, (k + tile - 1) / tile, 0, 1,
+    const Gemm g{Q, p.s_bytes, X[at], p.x_bytes, n, k, n, (n + tile - 1) / tile, (k + tile - 1) / tile,
                  ldexpf(1.0f, last ? -q_scale - kXScale : -q_scale), last ? reinterpret_cast<uint8_t*>(out) : X[at ^ 1],
-                 last ? count * 4 : p.x_bytes, 0, last ? (int)cols : (int)(blocks_of(k) * KS), nullptr, 0.0f, 0.0f};
+                 last ? count * 4 : p.x_bytes, last ? (int)cols : (int)(blocks_of(k) * KS), nullptr, 0.0f, 0.0f, 0, 1, 0,
+                 nullptr};
     const int64_t wgs = batch * g.tiles_m * g.tiles_n;
     e = !last ? run_gemm<true, kPlanes>(g, tile, wgs, s) : flip ? run_gemm<true, kF32T>(g, tile, wgs, s)
                                                                 : run_gemm<true, kF32>(g, tile, wgs, s);
