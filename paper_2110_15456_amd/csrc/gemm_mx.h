@@ -531,7 +531,11 @@ __global__ __launch_bounds__(CF::NT, CF::WAVES) void k_gemm_mx(const uint8_t* __
     if (sg.index == seg.n) ng = 0;  // rows of no expert: zeros
     else b_first = (int64_t)sg.index * N;
   } else if constexpr (SEG == kSegK) {
-    const int e = split_tile_of<FASTBFP_MX_GM>(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn);
+    // (every XCD takes a share of each expert's tiles: as contiguous runs of tiles of
+    // all experts, each XCD had experts of its own and waited for the one with the
+    // longest)
+    const int tiles = tiles_m * tiles_n, e = blockIdx.x / tiles;
+    tile_of_any<FASTBFP_MX_GM>(blockIdx.x % tiles, tiles, tiles_m, tiles_n, tm, tn);
     const int slabs = ng / mx::KG, end = min(max(seg.offsets[e + 1], 0) / (16 * mx::KG), slabs);
     slab0 = min(max(seg.offsets[e], 0) / (16 * mx::KG), end);
     seg_slabs = end - slab0;
@@ -1730,7 +1734,7 @@ hipError_t launch_mx_11_tile(const uint8_t* a_mant, const uint8_t* a_exp, const 
                                                         const OutBFP*, int, hipStream_t);
 
 // The products of experts of one operand-format combination (groups of 16).
-// small: 128 x 128 tiles (one chunk plane per operand).
+// small: 128 x 128 tiles.
 template <int NA, int NB, int FA, int FB>
 hipError_t launch_mx_experts_t(bool small, bool k_segments, const uint8_t* a_mant, const uint8_t* a_exp, int64_t a_ps,
                                const uint8_t* b_mant, const uint8_t* b_exp, int64_t b_ps, int M, int N, int ng,
@@ -1745,9 +1749,7 @@ hipError_t launch_mx_experts_t(bool small, bool k_segments, const uint8_t* a_man
       return launch_mx_seg<CF, true, kSegRows>(a_mant, a_exp, a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, seg, s);
     return launch_mx_seg<CF, false, kSegRows>(a_mant, a_exp, a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, seg, s);
   };
-  if constexpr (NA == 1 && NB == 1) {
-    if (small) return run(mx::Cfg<128, 128, 1, 1, FA, FB, 16>{});
-  }
+  if (small) return run(mx::Cfg<128, 128, NA, NB, FA, FB, 16>{});
   return run(typename mx_default<NA, NB, FA, FB, 16>::CF{});
 }
 #define FASTBFP_MX_EXPERTS_INSTANTIATE(NA, NB, FA, FB)                                                                \

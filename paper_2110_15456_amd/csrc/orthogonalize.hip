@@ -402,6 +402,100 @@ __global__ __launch_bounds__(256) void k_ns_finish(Gemm p) {
   }
 }
 
+// The products of symmetric matrices of n <= 96 in one launch, a workgroup for each
+// matrix with a wave for each 32 x 32 tile: S from the sums of X X^T's parts, P, and
+// for a pair of steps S P, P S P, P' and P' P; the planes of P or P' P leave.
+// Everything stays in LDS (three matrices, 110 KB at n = 96): a launch for each
+// product takes 6.9 us at n = 64 where its 12 MFMAs a wave take 0.3.
+struct Chain {
+  const float* sums;  // [matrix][part][128][128]
+  int parts, n, pair;
+  uint8_t* out;       // planes
+  int64_t out_batch;
+};
+template <int NB>
+__global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
+  constexpr int R = KS * NB, ROW = BLOCK * NB, NT = 64 * NB * NB;
+  __shared__ __attribute__((aligned(128))) uint8_t mem[3][R * ROW];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int wr = wave / NB, wc = wave % NB, fr = lane & 31, fk = lane >> 5;
+  // chunk c (16 bytes) of row r, spread over the banks within its block
+  auto at = [](int r, int c) { return r * ROW + (c & ~7) * 16 + ((c & 7) ^ (NB % 2 ? (r >> 1) & 7 : r & 7)) * 16; };
+  auto put4 = [&](uint8_t* m, int r, int c, const v4& v) {
+    h4 hi, lo;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      hi[t] = (_Float16)v[t];
+      lo[t] = (_Float16)(v[t] - (float)hi[t]);
+    }
+    const int chunk = c / KS * 8 + (c % KS) / 8;
+    *reinterpret_cast<h4*>(m + at(r, chunk) + (c & 4) * 2) = hi;
+    *reinterpret_cast<h4*>(m + at(r, chunk + 4) + (c & 4) * 2) = lo;
+  };
+  // dst = alpha a b^T + beta m + gamma I; dst is none of the others
+  auto product = [&](uint8_t* dst, const uint8_t* a, const uint8_t* b, float alpha, const uint8_t* m, float beta,
+                     float gamma) {
+    v16 acc = {};
+#pragma unroll
+    for (int h = 0; h < 2 * NB; ++h) {
+      h8 f[2][2];
+#pragma unroll
+      for (int pl = 0; pl < 2; ++pl) {
+        const int chunk = h / 2 * 8 + pl * 4 + 2 * (h & 1) + fk;
+        f[0][pl] = *reinterpret_cast<const h8*>(a + at(32 * wr + fr, chunk));
+        f[1][pl] = *reinterpret_cast<const h8*>(b + at(32 * wc + fr, chunk));
+      }
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[1][0], f[0][1], acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[1][1], f[0][0], acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[1][0], f[0][0], acc, 0, 0, 0);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int r = 32 * wr + fr, c = 32 * wc + 8 * q + 4 * fk, chunk = c / KS * 8 + (c % KS) / 8;
+      v4 v;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) v[t] = acc[4 * q + t] * alpha;
+      if (m) {
+        const h4 hi = *reinterpret_cast<const h4*>(m + at(r, chunk) + (c & 4) * 2);
+        const h4 lo = *reinterpret_cast<const h4*>(m + at(r, chunk + 4) + (c & 4) * 2);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) v[t] += beta * ((float)hi[t] + (float)lo[t]);
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (r == c + t && r < p.n) v[t] += gamma;
+      put4(dst, r, c, v);
+    }
+    __syncthreads();
+  };
+  uint8_t *S = mem[0], *P = mem[1], *T = mem[2];
+  const float* sums = p.sums + (int64_t)blockIdx.x * p.parts * (128 * 128);
+  for (int q = tid; q < R * R / 4; q += NT) {
+    const int r = q / (R / 4), c = 4 * (q % (R / 4));
+    v4 v = {};
+#pragma unroll 8
+    for (int i = 0; i < p.parts; ++i) v += *reinterpret_cast<const v4*>(sums + (int64_t)i * (128 * 128) + r * 128 + c);
+    put4(S, r, c, v * ldexpf(1.0f, kSScale - 2 * kXScale));
+  }
+  __syncthreads();
+  const float one = ldexpf(1.0f, -kPScale), sq = ldexpf(kC, kPScale - 2 * kSScale), li = ldexpf(kB, kPScale - kSScale);
+  const float id = ldexpf(kA, kPScale);
+  product(P, S, S, sq, S, li, id);
+  const uint8_t* Q = P;
+  if (p.pair) {
+    product(T, S, P, one, nullptr, 0.0f, 0.0f);
+    product(S, T, P, one, nullptr, 0.0f, 0.0f);
+    product(T, S, S, sq, S, li, id);
+    product(S, T, P, ldexpf(1.0f, kQScale - 2 * kPScale), nullptr, 0.0f, 0.0f);
+    Q = S;
+  }
+  uint8_t* out = p.out + blockIdx.x * p.out_batch;
+  for (int q = tid; q < p.n * NB * 8; q += NT) {
+    const int r = q / (NB * 8), c = q % (NB * 8);
+    *reinterpret_cast<h8*>(out + (int64_t)r * ROW + c * 16) = *reinterpret_cast<const h8*>(Q + at(r, c));
+  }
+}
+
 // U of one value: the new momentum (written where there is one) and what is
 // orthogonalised.
 __device__ __forceinline__ float update_of(float g, float m_new, float beta, int mode) {
@@ -450,23 +544,23 @@ __global__ __launch_bounds__(256) void k_ns_split(const float* __restrict__ g, c
   __shared__ double red[4];
   const int64_t matrix = blockIdx.x / per_matrix, t = blockIdx.x % per_matrix, base = matrix * ((int64_t)n * k);
   const int r0 = (int)(t / tiles_n) * T, c0 = (int)(t % tiles_n) * T;
+  // the tile of U: rows of U are X's columns where it is transposed
+  const int rows = FLIP ? k : n, cols = FLIP ? n : k, ur = FLIP ? c0 : r0, uc = FLIP ? r0 : c0;
+#pragma unroll
+  for (int i = 0; i < T * T / 256; ++i) {
+    const int q = threadIdx.x + 256 * i, r = q / T, c = q % T;
+    float u = 0.0f;
+    if (ur + r < rows && uc + c < cols) {
+      const int64_t at = base + (int64_t)(ur + r) * cols + uc + c;
+      u = update_of(g[at], mode ? m_new[at] : 0.0f, beta, mode);
+    }
+    tile[r][c] = u;
+  }
   double sum = 0.0;
   for (int i = threadIdx.x; i < blocks; i += 256) sum += part[matrix * blocks + i];
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
-  // the tile of U: rows of U are X's columns where it is transposed
-  const int rows = FLIP ? k : n, cols = FLIP ? n : k, ur = FLIP ? c0 : r0, uc = FLIP ? r0 : c0;
-#pragma unroll 4
-  for (int q = threadIdx.x; q < T * T; q += 256) {
-    const int r = q / T, c = q % T;
-    float u = 0.0f;
-    if (ur + r < rows && uc + c < cols) {
-      const int64_t i = base + (int64_t)(ur + r) * cols + uc + c;
-      u = update_of(g[i], mode ? m_new[i] : 0.0f, beta, mode);
-    }
-    tile[r][c] = u;
-  }
   __syncthreads();
   const double norm = sqrt((red[0] + red[1]) + (red[2] + red[3]));
   const float inv = (float)((double)(1 << kXScale) / (norm + (double)eps));
@@ -483,6 +577,7 @@ __global__ __launch_bounds__(256) void k_ns_split(const float* __restrict__ g, c
 }
 
 constexpr int kNormBlocks = 2048;
+constexpr int kChainMost = 96;  // rows of the matrices that k_ns_chain takes
 
 }  // namespace ns
 
@@ -542,6 +637,11 @@ NsPlan ns_plan(int64_t batch, int64_t rows, int64_t cols) {
   const int64_t tri256 = batch * n256 * (n256 + 1) / 2, tri128 = batch * n128 * (n128 + 1) / 2;
   p.gram = tiling(tri256, tri128, blocks_of(p.k), true);
   p.square = tiling(tri256, tri128, blocks_of(p.n), true);
+  if (p.n <= kChainMost) {  // one tile a matrix, its sums left to the chain
+    const int64_t slabs = blocks_of(p.k), fill = 512 / batch, most = slabs / 4 < 16 ? slabs / 4 : 16;
+    p.gram = Tiling{128, (int)(fill < 1 || most < 1 ? 1 : fill < most ? fill : most), 0};
+    p.square = Tiling{128, 1, tri128};
+  }
   p.apply = tiling(batch * n256 * ((p.k + 255) / 256), batch * n128 * ((p.k + 127) / 128), blocks_of(p.n), false);
   const int64_t per = (p.n * p.k + 4095) / 4096;
   p.norm_blocks = (int)(per < kNormBlocks ? per : kNormBlocks);
@@ -626,13 +726,27 @@ hipError_t launch_orthogonalize(const float* grad, const float* momentum, float*
   uint8_t *S = ws + p.off_s[0], *T = ws + p.off_s[1];
   uint8_t* poly[3] = {ws + p.off_p[0], ws + p.off_p[1], ws + p.off_p[2]};
   for (int done = 0, at = 0; done < steps; at ^= 1) {
-    // a pair pays from k = n on; near it its launches decide
-    const int group = p.k < p.n + p.n / 8 || steps - done < 2 ? 1 : 2;
-    e = product(X[at], X[at], p.x_bytes, k, p.gram, S, ldexpf(1.0f, kSScale - 2 * kXScale), nullptr, 0.0f, 0.0f);
-    if (e != hipSuccess) return e;
+    // a pair pays from k = n on; near it its launches decide, which the chain does not have
+    const int group = (p.k < p.n + p.n / 8 && n > kChainMost) || steps - done < 2 ? 1 : 2;
     const uint8_t* Q = nullptr;
     int q_scale = 0;
-    for (int i = 0; i < group; ++i) {
+    if (n <= kChainMost) {
+      const int slabs = (int)blocks_of(k), ps = (slabs + p.gram.parts - 1) / p.gram.parts, parts = (slabs + ps - 1) / ps;
+      e = run_gemm<false, kSym>(Gemm{X[at], p.x_bytes, X[at], p.x_bytes, n, n, k, 1, 1, 1.0f, nullptr, 0, (int)p.ld,
+                                     nullptr, 0.0f, 0.0f, 0, parts, ps, sum},
+                                128, batch * parts, s);
+      if (e != hipSuccess) return e;
+      const Chain c{sum, parts, n, group == 2, poly[0], p.s_bytes};
+      if (n <= 32) hipLaunchKernelGGL(k_ns_chain<1>, dim3((unsigned)batch), dim3(64), 0, s, c);
+      else if (n <= 64) hipLaunchKernelGGL(k_ns_chain<2>, dim3((unsigned)batch), dim3(256), 0, s, c);
+      else hipLaunchKernelGGL(k_ns_chain<3>, dim3((unsigned)batch), dim3(576), 0, s, c);
+      Q = poly[0], q_scale = group == 2 ? kQScale : kPScale;
+    } else {
+      e = product(X[at], X[at], p.x_bytes, k, p.gram, S, ldexpf(1.0f, kSScale - 2 * kXScale), nullptr, 0.0f, 0.0f);
+    }
+    if (e == hipSuccess) e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    for (int i = 0; i < group && n > kChainMost; ++i) {
       uint8_t* P = poly[i & 1];
       if (i > 0) {  // S <- P S P of the last step's P
         const float one = ldexpf(1.0f, -kPScale);
