@@ -20,6 +20,8 @@
 // 2^-254 adds nothing); rows past the end read zeros (the buffer resource ends
 // at the last row).
 #pragma once
+#include <type_traits>
+
 #include "bfp_quant.h"
 #include "segments.h"
 
@@ -29,6 +31,7 @@ namespace direct {
 
 typedef __amdgpu_buffer_rsrc_t rsrc_t;
 constexpr int kMaxWaves = 8;
+constexpr int kExpertWaves = 4;  // of a workgroup of the experts' kernel
 constexpr int kMaxRowTiles = 65535;  // row tiles are the grid's y, which holds no more
 
 __device__ __forceinline__ rsrc_t make_rsrc(const uint8_t* p, uint32_t bytes) {
@@ -182,47 +185,89 @@ template <int NP, int K0, int K1> struct Frag {
   uint32_t e;
 };
 
-}  // namespace direct
-
-// NA / NB, FA / FB, G: as mx::Cfg (planes read; FP4 codes, or split at 2 bits).
-// BOUT: C is written as BFP (N a multiple of 16).  SEG = kSegRows: the products
-// of experts (segments.h; a tile stays within one segment, B holds N rows for
-// each).
-template <int NA, int NB, int FA, int FB, int G, int RM, int RN, bool BOUT, int SEG = kSegNone>
-__global__ __launch_bounds__(64 * direct::kMaxWaves) void k_gemm_direct(
-    const uint8_t* __restrict__ a_mant, const uint8_t* __restrict__ a_exp, int64_t a_ps,
-    const uint8_t* __restrict__ b_mant, const uint8_t* __restrict__ b_exp, int64_t b_ps, int M, int N, int ng,
-    float scale, float* __restrict__ C, int64_t ldc, direct::Out out, typename SegArg<SEG>::type seg) {
-  using namespace direct;
+// One superstep of a wave: every row tile of A against every one of B.
+template <int NA, int NB, int FA, int FB, int G, int RM, int RN, class FragA, class FragB>
+__device__ __forceinline__ void superstep(v4f (&acc)[RM][RN], const FragA (&fa)[RM], const FragB (&fb)[RN]) {
   constexpr int KA0 = (NA == 1 && FA) ? kPlaneFP4 : kPlaneFP6, KB0 = (NB == 1 && FB) ? kPlaneFP4 : kPlaneFP6;
   constexpr int KA1 = FA ? kPlaneLo2 : kPlaneFP6, KB1 = FB ? kPlaneLo2 : kPlaneFP6;
   constexpr bool SA = NA == 2 && FA, SB = NB == 2 && FB;  // split at 2 bits
+#pragma unroll
+  for (int u = 0; u < (G == 16 ? 4 : 2); ++u) {
+#pragma unroll
+    for (int i = 0; i < RM; ++i) {
+      const auto& x = fa[i];
+      const uint32_t ea = (x.e >> (8 * u)) & 0xFFu;
+#pragma unroll
+      for (int j = 0; j < RN; ++j) {
+        const auto& y = fb[j];
+        const uint32_t eb = (y.e >> (8 * u)) & 0xFFu;
+        v4f& c = acc[i][j];
+        // The chunk weights on the scale bytes and the pairing of planes
+        // are those of gemm_mx.h.
+        if constexpr (G == 32) {
+          constexpr int wa0 = NA == 1 ? 0 : SA ? 2 : 4, wa1 = SA ? 2 : 0;
+          constexpr int wb0 = NB == 1 ? 0 : SB ? 2 : 4, wb1 = SB ? 2 : 0;
+          mma<KA0, KB0>(c, x.p0.pair(u), y.p0.pair(u), ea + wa0, eb + wb0);
+          if constexpr (NA == 2) mma<KA1, KB0>(c, x.p1.pair(u), y.p0.pair(u), ea + wa1, eb + wb0);
+          if constexpr (NB == 2) mma<KA0, KB1>(c, x.p0.pair(u), y.p1.pair(u), ea + wa0, eb + wb1);
+          if constexpr (NA == 2 && NB == 2) mma<KA1, KB1>(c, x.p1.pair(u), y.p1.pair(u), ea + wa1, eb + wb1);
+        } else if constexpr (SA) {
+          // A's [q >> 2 | q & 3] block against each plane of B repeated
+          const v8i av = join(x.p0, x.p1, u);
+          constexpr int wb0 = NB == 1 ? 0 : SB ? 2 : 4, wb1 = SB ? 2 : 0;
+          mma<kPlaneFP6, KB0>(c, av, y.p0.template half<true>(u), ea + 2, eb + wb0);
+          if constexpr (NB == 2) mma<kPlaneFP6, KB1>(c, av, y.p1.template half<true>(u), ea + 2, eb + wb1);
+        } else if constexpr (SB) {
+          const v8i bv = join(y.p0, y.p1, u);
+          constexpr int wa0 = NA == 1 ? 0 : 4;
+          mma<KA0, kPlaneFP6>(c, x.p0.template half<true>(u), bv, ea + wa0, eb + 2);
+          if constexpr (NA == 2) mma<KA1, kPlaneFP6>(c, x.p1.template half<true>(u), bv, ea, eb + 2);
+        } else if constexpr (NA == 2 && NB == 2) {
+          // split at 4 bits on both sides: the two cross products share one MFMA
+          mma<KA0, KB0>(c, x.p0.template half<false>(u), y.p0.template half<false>(u), ea + 4, eb + 4);
+          mma<KA1, KB1>(c, x.p1.template half<false>(u), y.p1.template half<false>(u), ea, eb);
+          mma<kPlaneFP6, kPlaneFP6>(c, join(x.p0, x.p1, u), join(y.p1, y.p0, u), ea + 4, eb);
+        } else {
+          constexpr int wa0 = NA == 1 ? 0 : 4, wb0 = NB == 1 ? 0 : 4;
+          mma<KA0, KB0>(c, x.p0.template half<false>(u), y.p0.template half<false>(u), ea + wa0, eb + wb0);
+          if constexpr (NA == 2)
+            mma<KA1, KB0>(c, x.p1.template half<false>(u), y.p0.template half<false>(u), ea, eb + wb0);
+          if constexpr (NB == 2)
+            mma<KA0, KB1>(c, x.p0.template half<false>(u), y.p1.template half<false>(u), ea + wa0, eb);
+        }
+      }
+    }
+  }
+}
+
+}  // namespace direct
+
+// NA / NB, FA / FB, G: as mx::Cfg (planes read; FP4 codes, or split at 2 bits).
+// BOUT: C is written as BFP (N a multiple of 16).
+template <int NA, int NB, int FA, int FB, int G, int RM, int RN, bool BOUT>
+__global__ __launch_bounds__(64 * direct::kMaxWaves) void k_gemm_direct(
+    const uint8_t* __restrict__ a_mant, const uint8_t* __restrict__ a_exp, int64_t a_ps,
+    const uint8_t* __restrict__ b_mant, const uint8_t* __restrict__ b_exp, int64_t b_ps, int M, int N, int ng,
+    float scale, float* __restrict__ C, int64_t ldc, direct::Out out) {
+  using namespace direct;
+  constexpr int KA0 = (NA == 1 && FA) ? kPlaneFP4 : kPlaneFP6, KB0 = (NB == 1 && FB) ? kPlaneFP4 : kPlaneFP6;
+  constexpr int KA1 = FA ? kPlaneLo2 : kPlaneFP6, KB1 = FB ? kPlaneLo2 : kPlaneFP6;
   constexpr int SROW = 16 * RN + 4;                       // LDS row stride in floats (padding spreads the banks)
   __shared__ __attribute__((aligned(16))) float part[kMaxWaves][16 * RM * SROW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nw = blockDim.x >> 6;
   const int lr = lane & 15, lb = lane >> 4;
-  int row0 = blockIdx.y * (16 * RM);
-  const int col0 = blockIdx.x * (16 * RN);
-  int64_t b_row0 = col0;
-  if constexpr (SEG == kSegRows) {
-    const Segment sg = find_segment<16 * RM>(seg, blockIdx.y);
-    if (sg.index < 0) return;  // (the grid is sized for the most tiles there can be)
-    row0 = sg.first;
-    M = sg.end;
-    if (sg.index == seg.n) ng = 0;  // rows of no expert: zeros
-    else b_row0 += (int64_t)sg.index * N;
-  }
+  const int row0 = blockIdx.y * (16 * RM), col0 = blockIdx.x * (16 * RN);
   const int a_rows = min(16 * RM, M - row0), b_rows = min(16 * RN, N - col0);
   const int ng_e = ng * 16 / G;
   constexpr int UA0 = KA0 == kPlaneFP6 ? 12 : 8, UB0 = KB0 == kPlaneFP6 ? 12 : 8;  // bytes per unit
   constexpr int UA1 = KA1 == kPlaneFP6 ? 12 : 8, UB1 = KB1 == kPlaneFP6 ? 12 : 8;
   const rsrc_t ra0 = make_rsrc(a_mant + (int64_t)row0 * ng * UA0, (uint32_t)a_rows * ng * UA0);
-  const rsrc_t rb0 = make_rsrc(b_mant + b_row0 * ng * UB0, (uint32_t)b_rows * ng * UB0);
+  const rsrc_t rb0 = make_rsrc(b_mant + (int64_t)col0 * ng * UB0, (uint32_t)b_rows * ng * UB0);
   const rsrc_t ra1 = make_rsrc(a_mant + a_ps + (int64_t)row0 * ng * UA1, NA == 2 ? (uint32_t)a_rows * ng * UA1 : 0u);
-  const rsrc_t rb1 = make_rsrc(b_mant + b_ps + b_row0 * ng * UB1, NB == 2 ? (uint32_t)b_rows * ng * UB1 : 0u);
+  const rsrc_t rb1 = make_rsrc(b_mant + b_ps + (int64_t)col0 * ng * UB1, NB == 2 ? (uint32_t)b_rows * ng * UB1 : 0u);
   const rsrc_t rea = make_rsrc(a_exp + (int64_t)row0 * ng_e, (uint32_t)a_rows * ng_e);
-  const rsrc_t reb = make_rsrc(b_exp + b_row0 * ng_e, (uint32_t)b_rows * ng_e);
+  const rsrc_t reb = make_rsrc(b_exp + (int64_t)col0 * ng_e, (uint32_t)b_rows * ng_e);
   constexpr int EA = G == 16 ? 4 : 2;  // exponent bytes per lane and superstep
   const bool dw = ng_e % EA == 0 && (reinterpret_cast<uintptr_t>(a_exp) % EA) == 0 &&
                   (reinterpret_cast<uintptr_t>(b_exp) % EA) == 0;
@@ -254,53 +299,7 @@ __global__ __launch_bounds__(64 * direct::kMaxWaves) void k_gemm_direct(
       if constexpr (NA == 2) fa[i].p1.load(ra1, (r * ng + u0) * UA1);
       fa[i].e = load_exps<G>(rea, G == 16 ? r * ng_e + u0 : r * ng_e + u0 / 2, ng - u0, dw);
     }
-#pragma unroll
-    for (int u = 0; u < (G == 16 ? 4 : 2); ++u) {
-#pragma unroll
-      for (int i = 0; i < RM; ++i) {
-        const auto& x = fa[i];
-        const uint32_t ea = (x.e >> (8 * u)) & 0xFFu;
-#pragma unroll
-        for (int j = 0; j < RN; ++j) {
-          const auto& y = fb[j];
-          const uint32_t eb = (y.e >> (8 * u)) & 0xFFu;
-          v4f& c = acc[i][j];
-          // The chunk weights on the scale bytes and the pairing of planes
-          // are those of gemm_mx.h.
-          if constexpr (G == 32) {
-            constexpr int wa0 = NA == 1 ? 0 : SA ? 2 : 4, wa1 = SA ? 2 : 0;
-            constexpr int wb0 = NB == 1 ? 0 : SB ? 2 : 4, wb1 = SB ? 2 : 0;
-            mma<KA0, KB0>(c, x.p0.pair(u), y.p0.pair(u), ea + wa0, eb + wb0);
-            if constexpr (NA == 2) mma<KA1, KB0>(c, x.p1.pair(u), y.p0.pair(u), ea + wa1, eb + wb0);
-            if constexpr (NB == 2) mma<KA0, KB1>(c, x.p0.pair(u), y.p1.pair(u), ea + wa0, eb + wb1);
-            if constexpr (NA == 2 && NB == 2) mma<KA1, KB1>(c, x.p1.pair(u), y.p1.pair(u), ea + wa1, eb + wb1);
-          } else if constexpr (SA) {
-            // A's [q >> 2 | q & 3] block against each plane of B repeated
-            const v8i av = join(x.p0, x.p1, u);
-            constexpr int wb0 = NB == 1 ? 0 : SB ? 2 : 4, wb1 = SB ? 2 : 0;
-            mma<kPlaneFP6, KB0>(c, av, y.p0.template half<true>(u), ea + 2, eb + wb0);
-            if constexpr (NB == 2) mma<kPlaneFP6, KB1>(c, av, y.p1.template half<true>(u), ea + 2, eb + wb1);
-          } else if constexpr (SB) {
-            const v8i bv = join(y.p0, y.p1, u);
-            constexpr int wa0 = NA == 1 ? 0 : 4;
-            mma<KA0, kPlaneFP6>(c, x.p0.template half<true>(u), bv, ea + wa0, eb + 2);
-            if constexpr (NA == 2) mma<KA1, kPlaneFP6>(c, x.p1.template half<true>(u), bv, ea, eb + 2);
-          } else if constexpr (NA == 2 && NB == 2) {
-            // split at 4 bits on both sides: the two cross products share one MFMA
-            mma<KA0, KB0>(c, x.p0.template half<false>(u), y.p0.template half<false>(u), ea + 4, eb + 4);
-            mma<KA1, KB1>(c, x.p1.template half<false>(u), y.p1.template half<false>(u), ea, eb);
-            mma<kPlaneFP6, kPlaneFP6>(c, join(x.p0, x.p1, u), join(y.p1, y.p0, u), ea + 4, eb);
-          } else {
-            constexpr int wa0 = NA == 1 ? 0 : 4, wb0 = NB == 1 ? 0 : 4;
-            mma<KA0, KB0>(c, x.p0.template half<false>(u), y.p0.template half<false>(u), ea + wa0, eb + wb0);
-            if constexpr (NA == 2)
-              mma<KA1, KB0>(c, x.p1.template half<false>(u), y.p0.template half<false>(u), ea, eb + wb0);
-            if constexpr (NB == 2)
-              mma<KA0, KB1>(c, x.p0.template half<false>(u), y.p1.template half<false>(u), ea + wa0, eb);
-          }
-        }
-      }
-    }
+    superstep<NA, NB, FA, FB, G, RM, RN>(acc, fa, fb);
   }
 #pragma unroll
   for (int i = 0; i < RM; ++i)
@@ -360,10 +359,10 @@ hipError_t launch_direct_t(int rm, int rn, const uint8_t* a_mant, const uint8_t*
   if (rm == RM && rn == RN) {                                                                                         \
     if (out)                                                                                                          \
       hipLaunchKernelGGL((k_gemm_direct<NA, NB, FA, FB, G, RM, RN, true>), grid, dim3(64 * nw), 0, s, a_mant, a_exp,  \
-                         a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, *out, NoSegments{});                                   \
+                         a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, *out);                                                 \
     else                                                                                                              \
       hipLaunchKernelGGL((k_gemm_direct<NA, NB, FA, FB, G, RM, RN, false>), grid, dim3(64 * nw), 0, s, a_mant, a_exp, \
-                         a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, direct::Out{}, NoSegments{});           \
+                         a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, direct::Out{});                          \
     return hipGetLastError();                                                                                         \
   }
   FASTBFP_DIRECT_LAUNCH(1, 1)
@@ -373,32 +372,287 @@ hipError_t launch_direct_t(int rm, int rn, const uint8_t* a_mant, const uint8_t*
   return hipErrorInvalidValue;
 }
 
-// The products of experts (groups of 16); the tiles as above.
-template <int NA, int NB, int FA, int FB>
-hipError_t launch_direct_experts_t(int rm, int rn, const uint8_t* a_mant, const uint8_t* a_exp, int64_t a_ps,
-                                   const uint8_t* b_mant, const uint8_t* b_exp, int64_t b_ps, int M, int N, int ng,
-                                   float scale, float* C, int64_t ldc, const Segments& seg, hipStream_t s) {
-  const int nss = (ng + 15) / 16;
-  const int nw = nss < 1 ? 1 : nss > direct::kMaxWaves ? direct::kMaxWaves : nss;
-  const int64_t tiles = most_segment_tiles(seg, 16 * rm);
-  if (tiles > direct::kMaxRowTiles) return hipErrorInvalidValue;  // (the plan does not plan it)
-  const dim3 grid((unsigned)((N + 16 * rn - 1) / (16 * rn)), (unsigned)tiles);
-#define FASTBFP_DIRECT_LAUNCH(RM, RN)                                                                               \
-  if (rm == RM && rn == RN) {                                                                                       \
-    hipLaunchKernelGGL((k_gemm_direct<NA, NB, FA, FB, 16, RM, RN, false, kSegRows>), grid, dim3(64 * nw), 0, s,     \
-                       a_mant, a_exp, a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, direct::Out{}, seg);      \
-    return hipGetLastError();                                                                                       \
+namespace direct {
+
+// Sixteen rows of one plane in a pair of K supersteps (32 units: 384 bytes of a row
+// of FP6 codes, 256 of FP4 or Lo2), a wave's loads of 1 KB.  Chunk c = 64 i + lane (16
+// bytes) is part c % CPR of row c / CPR, so that neighbouring lanes read neighbouring
+// bytes; in LDS a row takes CPR + 1 chunks, an odd number, so that the 16 rows that
+// a fragment reads at one place lie on all banks.
+template <int KIND> struct Rows16 {
+  static constexpr int UNIT = KIND == kPlaneFP6 ? 12 : 8, CPR = 2 * UNIT, NI = CPR / 4, STRIDE = (CPR + 1) * 16;
+  static constexpr int BYTES = 16 * STRIDE;
+  v4i d[NI];
+  static __device__ __forceinline__ int chunk_row(int i, int lane) { return (64 * i + lane) / CPR; }
+  // first: byte offset of the first row's pair.  STREAM: past the caches (whole lines).
+  template <bool STREAM>
+  __device__ __forceinline__ void load(rsrc_t r, uint32_t first, uint32_t row_bytes, int lane) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int row = chunk_row(i, lane);
+      d[i] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(
+          r, first + (uint32_t)row * row_bytes + (uint32_t)(64 * i + lane - row * CPR) * 16u, 0,
+          STREAM ? kStreamPolicy : 0));
+    }
   }
-  FASTBFP_DIRECT_LAUNCH(1, 1)
-  FASTBFP_DIRECT_LAUNCH(1, 2)
-  FASTBFP_DIRECT_LAUNCH(2, 2)
-  FASTBFP_DIRECT_LAUNCH(4, 2)
-#undef FASTBFP_DIRECT_LAUNCH
+  __device__ __forceinline__ void put(uint8_t* lds, int lane) const {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      *reinterpret_cast<v4i*>(lds + 16 * (64 * i + lane + chunk_row(i, lane))) = d[i];
+  }
+  // superstep s of the pair
+  static __device__ __forceinline__ void get(const uint8_t* lds, int lane, int s, Units<KIND>& u) {
+    const uint8_t* p = lds + (lane & 15) * STRIDE + (16 * s + 4 * (lane >> 4)) * UNIT;
+#pragma unroll
+    for (int i = 0; i < UNIT / 4; ++i) {
+      const v4i v = *reinterpret_cast<const v4i*>(p + 16 * i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) u.d[4 * i + k] = v[k];
+    }
+  }
+};
+
+// The 32 exponents of each of ROWS rows' pairs, a lane for each row: from the
+// aligned words that hold them (the resource begins at a word, shift bytes before
+// the first row's first exponent), funnelled into place.
+template <int ROWS> struct Exps32 {
+  uint32_t w[9];
+  uint32_t by;
+  __device__ __forceinline__ void load(rsrc_t r, uint32_t shift, int ng, int pair, bool words, int lane) {
+    if (lane >= ROWS) return;
+    const uint32_t o = shift + (uint32_t)lane * (uint32_t)ng + (uint32_t)pair * 32u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const v4i v = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(r, (o & ~3u) + 16u * h, 0, 0));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[4 * h + k] = (uint32_t)v[k];
+    }
+    by = o & 3u;
+    w[8] = words ? 0u : (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, (o & ~3u) + 32u, 0, 0);
+  }
+  __device__ __forceinline__ void put(uint8_t* lds, int lane) const {
+    if (lane >= ROWS) return;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      v4i v;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = (int)__builtin_amdgcn_alignbyte(w[4 * h + k + 1], w[4 * h + k], by);
+      *reinterpret_cast<v4i*>(lds + 32 * lane + 16 * h) = v;
+    }
+  }
+};
+// Of row lane % 16 of the sixteen at lds: units 16 s + 4 (lane / 16) .. + 3 of the
+// pair, zero past the last.
+__device__ __forceinline__ uint32_t get_exps(const uint8_t* lds, int lane, int s, int units_left) {
+  const uint32_t e = *reinterpret_cast<const uint32_t*>(lds + 32 * (lane & 15) + 16 * s + 4 * (lane >> 4));
+  return units_left >= 4 ? e : units_left <= 0 ? 0u : e & ((1u << (8 * units_left)) - 1u);
+}
+
+}  // namespace direct
+
+// The products of experts (segments.h; groups of 16): a workgroup takes one tile of
+// rows, which stays within one segment, and shares of its columns: kw of its four
+// waves split K for one tile of 16 RN columns (1, 2 or 4; their sums meet in LDS).
+//
+// What bounds it is the bytes of the weights, each read once for every 16 RM tokens
+// of its expert.  Fragments loaded straight into their registers are 16-byte pieces
+// of 16 rows, and a tile's waves, all splitting K, met at two barriers every second
+// superstep: 16 tokens' 32 choices of 8 experts' 4096 x 16384 weights (m = 4, 436 MB)
+// took 95 us, with the next loads in flight too.  A loop that only reads them takes
+// 67 us in pieces of 192 bytes of a row and 55 in pieces of 384, whole lines past the
+// caches (7.2 TB/s).  So a wave loads pairs of supersteps of whole rows' pieces in
+// order, a pair ahead in registers, and turns them into fragments through its own
+// part of LDS, sixteen rows of B at a time; where the columns are enough for every
+// wave (kw = 1) there is no barrier.
+template <int NA, int NB, int FA, int FB, int RM, int RN>
+__global__ __launch_bounds__(64 * direct::kExpertWaves, 2) void k_gemm_direct_experts(
+    const uint8_t* __restrict__ a_mant, const uint8_t* __restrict__ a_exp, int64_t a_ps,
+    const uint8_t* __restrict__ b_mant, const uint8_t* __restrict__ b_exp, int64_t b_ps, int N, int ng, float scale,
+    float* __restrict__ C, int64_t ldc, int kw, Segments seg) {
+  using namespace direct;
+  constexpr int KA0 = (NA == 1 && FA) ? kPlaneFP4 : kPlaneFP6, KB0 = (NB == 1 && FB) ? kPlaneFP4 : kPlaneFP6;
+  constexpr int KA1 = FA ? kPlaneLo2 : kPlaneFP6, KB1 = FB ? kPlaneLo2 : kPlaneFP6;
+  typedef Rows16<KA0> A0;
+  typedef Rows16<KA1> A1;
+  typedef Rows16<KB0> B0;
+  typedef Rows16<KB1> B1;
+  constexpr int SROW = 16 * RN + 4;
+  // a wave's LDS: sixteen rows of A or B, and all exponents; at a tile's end its sums
+  constexpr int AB = A0::BYTES + (NA == 2 ? A1::BYTES : 0), BB = B0::BYTES + (NB == 2 ? B1::BYTES : 0);
+  constexpr int OFF_AE = AB > BB ? AB : BB, OFF_BE = OFF_AE + 512 * RM, USED = OFF_BE + 512 * RN;
+  constexpr int SUMS = 16 * RM * SROW * 4, WAVE = USED > SUMS ? USED : SUMS;
+  static_assert(2 * WAVE * kExpertWaves <= 160 * 1024, "two workgroups on a CU");
+  __shared__ __attribute__((aligned(16))) uint8_t mem[kExpertWaves * WAVE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 15, lb = lane >> 4, wn = wave / kw, wk = wave % kw, nwn = kExpertWaves / kw;
+  uint8_t* mine = mem + wave * WAVE;
+  const Segment sg = find_segment<16 * RM>(seg, blockIdx.y);
+  if (sg.index < 0) return;  // (the grid is sized for the most tiles there can be)
+  const bool none = sg.index == seg.n;  // rows of no expert: zeros
+  const int row0 = sg.first, M = sg.end, a_rows = min(16 * RM, M - row0);
+  const uint32_t ra_b = (uint32_t)ng * A0::UNIT, ra1_b = (uint32_t)ng * A1::UNIT;  // bytes of a row
+  const uint32_t rb_b = (uint32_t)ng * B0::UNIT, rb1_b = (uint32_t)ng * B1::UNIT;
+  const rsrc_t ra0 = make_rsrc(a_mant + (int64_t)row0 * ra_b, (uint32_t)a_rows * ra_b);
+  const rsrc_t ra1 = make_rsrc(a_mant + a_ps + (int64_t)row0 * ra1_b, NA == 2 ? (uint32_t)a_rows * ra1_b : 0u);
+  // exponents: the aligned words from the first row's first to the last row's last
+  auto exps_rsrc = [&](const uint8_t* e, int rows, uint32_t& shift) __attribute__((always_inline)) -> rsrc_t {
+    shift = (uint32_t)(reinterpret_cast<uintptr_t>(e) & 3);
+    return make_rsrc(e - shift, (shift + (uint32_t)rows * (uint32_t)ng + 3u) & ~3u);
+  };
+  const bool words = ng % 4 == 0 && (reinterpret_cast<uintptr_t>(a_exp) & 3) == 0 &&
+                     (reinterpret_cast<uintptr_t>(b_exp) & 3) == 0;  // every row's pairs begin with a word
+  uint32_t sa;
+  const rsrc_t rea = exps_rsrc(a_exp + (int64_t)row0 * ng, a_rows, sa);
+  const int pairs = none ? 0 : (ng + 31) / 32, per = (pairs + kw - 1) / kw;
+  const int p0 = wk * per, p1 = min(pairs, p0 + per);  // this wave's pairs of every tile
+  const int tiles = (N + 16 * RN - 1) / (16 * RN), groups = (tiles + nwn - 1) / nwn;  // of a tile for each kw waves
+  auto works = [&](int g) { return g < groups && g * nwn + wn < tiles && p0 < p1; };
+
+  // one pair of supersteps in registers, as loaded
+  A0 a0[RM];
+  A1 a1[RM];
+  B0 b0[RN];
+  B1 b1[RN];
+  Exps32<16 * RM> ea;
+  Exps32<16 * RN> eb;
+  auto load = [&](int g, int pair) __attribute__((always_inline)) {
+    const int col0 = (g * nwn + wn) * (16 * RN), rows = min(16 * RN, N - col0);
+    const int64_t b_row = (int64_t)sg.index * N + col0;
+    const rsrc_t rb0 = make_rsrc(b_mant + b_row * rb_b, (uint32_t)rows * rb_b);
+    const rsrc_t rb1 = make_rsrc(b_mant + b_ps + b_row * rb1_b, NB == 2 ? (uint32_t)rows * rb1_b : 0u);
+    uint32_t sb;
+    const rsrc_t reb = exps_rsrc(b_exp + b_row * ng, rows, sb);
+#pragma unroll
+    for (int j = 0; j < RN; ++j) {
+      b0[j].template load<true>(rb0, 16u * j * rb_b + (uint32_t)pair * (32 * B0::UNIT), rb_b, lane);
+      if constexpr (NB == 2) b1[j].template load<true>(rb1, 16u * j * rb1_b + (uint32_t)pair * (32 * B1::UNIT), rb1_b, lane);
+    }
+    eb.load(reb, sb, ng, pair, words, lane);
+#pragma unroll
+    for (int i = 0; i < RM; ++i) {
+      a0[i].template load<false>(ra0, 16u * i * ra_b + (uint32_t)pair * (32 * A0::UNIT), ra_b, lane);
+      if constexpr (NA == 2) a1[i].template load<false>(ra1, 16u * i * ra1_b + (uint32_t)pair * (32 * A1::UNIT), ra1_b, lane);
+    }
+    ea.load(rea, sa, ng, pair, words, lane);
+  };
+  v4f acc[RN][RM][1];
+  // barriers that wait for LDS alone: the next pair's loads stay in flight
+  auto lds_barrier = []() __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  const bool vec = (ldc & 3) == 0 && (reinterpret_cast<uintptr_t>(C) & 15) == 0;
+  auto store4 = [&](int row, int col, const v4f& v) __attribute__((always_inline)) {
+    if (row >= M || col >= N) return;
+    float* p = C + (int64_t)row * ldc + col;
+    if (vec && col + 3 < N) {
+      *reinterpret_cast<float4*>(p) = make_float4(v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (col + t < N) p[t] = v[t] * scale;
+    }
+  };
+  int g = blockIdx.x;
+  if (works(g)) load(g, p0);
+  for (; g < groups; g += gridDim.x) {
+#pragma unroll
+    for (int j = 0; j < RN; ++j)
+#pragma unroll
+      for (int i = 0; i < RM; ++i) acc[j][i][0] = v4f{0.f, 0.f, 0.f, 0.f};
+    if (works(g)) {
+      for (int p = p0; p < p1; ++p) {
+        const bool same = p + 1 < p1;
+        const int left = ng - (p * 32 + 4 * lb);
+        // registers -> LDS -> fragments, sixteen rows at a time
+        ea.put(mine + OFF_AE, lane);
+        eb.put(mine + OFF_BE, lane);
+        Frag<NA, KA0, KA1> fa[2][RM];
+#pragma unroll
+        for (int i = 0; i < RM; ++i) {
+          a0[i].put(mine, lane);
+          if constexpr (NA == 2) a1[i].put(mine + A0::BYTES, lane);
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            A0::get(mine, lane, s, fa[s][i].p0);
+            if constexpr (NA == 2) A1::get(mine + A0::BYTES, lane, s, fa[s][i].p1);
+            fa[s][i].e = get_exps(mine + OFF_AE + 512 * i, lane, s, left - 16 * s);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < RN; ++j) {
+          b0[j].put(mine, lane);
+          if constexpr (NB == 2) b1[j].put(mine + B0::BYTES, lane);
+          if (j + 1 == RN && (same || works(g + (int)gridDim.x))) load(same ? g : g + (int)gridDim.x, same ? p + 1 : p0);
+          Frag<NB, KB0, KB1> fb[1];
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            B0::get(mine, lane, s, fb[0].p0);
+            if constexpr (NB == 2) B1::get(mine + B0::BYTES, lane, s, fb[0].p1);
+            fb[0].e = get_exps(mine + OFF_BE + 512 * j, lane, s, left - 16 * s);
+            superstep<NA, NB, FA, FB, 16, RM, 1>(acc[j], fa[s], fb);
+          }
+        }
+      }
+    }
+    const int col0 = (g * nwn + wn) * (16 * RN);
+    if (kw == 1) {
+#pragma unroll
+      for (int i = 0; i < RM; ++i)
+#pragma unroll
+        for (int j = 0; j < RN; ++j) store4(row0 + 16 * i + lr, col0 + 16 * j + 4 * lb, acc[j][i][0]);
+    } else {
+      // the sums of a tile's waves, added in their order, four columns per lane
+      float* part = reinterpret_cast<float*>(mine);
+#pragma unroll
+      for (int i = 0; i < RM; ++i)
+#pragma unroll
+        for (int j = 0; j < RN; ++j)
+          *reinterpret_cast<v4f*>(&part[(16 * i + lr) * SROW + 16 * j + 4 * lb]) = acc[j][i][0];
+      lds_barrier();
+      for (int q = wk * 64 + lane; q < 16 * RM * 4 * RN; q += 64 * kw) {
+        const int r = q / (4 * RN), k = 4 * (q % (4 * RN));
+        const uint8_t* at = mem + wn * kw * WAVE + (r * SROW + k) * 4;
+        v4f v = *reinterpret_cast<const v4f*>(at);
+        for (int w = 1; w < kw; ++w) v += *reinterpret_cast<const v4f*>(at + w * WAVE);
+        store4(row0 + r, col0 + k, v);
+      }
+      lds_barrier();
+    }
+  }
+}
+
+// Columns of a tile of 16 rm rows: 32, and 16 where an operand's rows take two planes
+// or there are 32 of A (the registers hold no more).
+constexpr int direct_experts_cols(int na, int nb, int rm) { return na == 1 && nb == 1 && rm == 1 ? 32 : 16; }
+
+// The products of experts on tiles of 16 rm rows (rm = 2: one plane of A), kw waves to
+// a tile, `each` groups of tiles to a workgroup.
+template <int NA, int NB, int FA, int FB>
+hipError_t launch_direct_experts_t(int rm, int kw, int each, const uint8_t* a_mant, const uint8_t* a_exp, int64_t a_ps,
+                                   const uint8_t* b_mant, const uint8_t* b_exp, int64_t b_ps, int N, int ng,
+                                   float scale, float* C, int64_t ldc, const Segments& seg, hipStream_t s) {
+  const int64_t rows = most_segment_tiles(seg, 16 * rm);
+  if (rows > direct::kMaxRowTiles) return hipErrorInvalidValue;  // (the plan does not plan it)
+  auto run = [&](auto rm_c) {
+    constexpr int RM = decltype(rm_c)::value, COLS = direct_experts_cols(NA, NB, RM);
+    const int64_t tiles = (N + COLS - 1) / COLS, nwn = direct::kExpertWaves / kw, groups = (tiles + nwn - 1) / nwn;
+    hipLaunchKernelGGL((k_gemm_direct_experts<NA, NB, FA, FB, RM, COLS / 16>),
+                       dim3((unsigned)((groups + each - 1) / each), (unsigned)rows), dim3(64 * direct::kExpertWaves), 0, s,
+                       a_mant, a_exp, a_ps, b_mant, b_exp, b_ps, N, ng, scale, C, ldc, kw, seg);
+    return hipGetLastError();
+  };
+  if (rm == 1) return run(std::integral_constant<int, 1>{});
+  if constexpr (NA == 1) {
+    if (rm == 2) return run(std::integral_constant<int, 2>{});
+  }
   return hipErrorInvalidValue;
 }
-#define FASTBFP_DIRECT_EXPERTS_INSTANTIATE(NA, NB, FA, FB)                                                          \
-  template hipError_t launch_direct_experts_t<NA, NB, FA, FB>(int, int, const uint8_t*, const uint8_t*, int64_t,    \
-                                                              const uint8_t*, const uint8_t*, int64_t, int, int, int, \
+#define FASTBFP_DIRECT_EXPERTS_INSTANTIATE(NA, NB, FA, FB)                                                           \
+  template hipError_t launch_direct_experts_t<NA, NB, FA, FB>(int, int, int, const uint8_t*, const uint8_t*, int64_t, \
+                                                              const uint8_t*, const uint8_t*, int64_t, int, int,     \
                                                               float, float*, int64_t, const Segments&, hipStream_t);
 #define FASTBFP_DIRECT_EXPERTS_DECLARE(NA, NB, FA, FB) extern FASTBFP_DIRECT_EXPERTS_INSTANTIATE(NA, NB, FA, FB)
 #define FASTBFP_DIRECT_EXPERTS_ALL(DO, NA, NB) DO(NA, NB, 0, 0) DO(NA, NB, 0, 1) DO(NA, NB, 1, 0) DO(NA, NB, 1, 1)

@@ -55,10 +55,10 @@ hipError_t run_tiled(const Operands& p, bool small, bool k_segments, float* C, i
   });
 }
 
-hipError_t run_direct(const Operands& p, int rm, int rn, float* C, int64_t ldc, const Segments& seg, hipStream_t s) {
+hipError_t run_direct(const Operands& p, int rm, int kw, int each, float* C, int64_t ldc, const Segments& seg, hipStream_t s) {
   return with_operands(p, [&](auto na, auto nb, auto fa, auto fb) {
     return launch_direct_experts_t<decltype(na)::value, decltype(nb)::value, decltype(fa)::value, decltype(fb)::value>(
-        rm, rn, p.a_mant, p.a_exp, p.a_ps, p.b_mant, p.b_exp, p.b_ps, p.M, p.N, p.ng, p.scale, C, ldc, seg, s);
+        rm, kw, each, p.a_mant, p.a_exp, p.a_ps, p.b_mant, p.b_exp, p.b_ps, p.N, p.ng, p.scale, C, ldc, seg, s);
   });
 }
 
@@ -74,8 +74,17 @@ hipError_t launch_gemm_experts(const uint8_t* a_mant, const uint8_t* a_exp, int 
                    fmt_flag(a_m, na), fmt_flag(b_m, nb), ldexpf(1.0f, scale_log2)};
   const Segments seg{offsets, experts, (int)slots};
   const int64_t mean = slots / experts;
-  if (mean <= 16 && most_segment_tiles(seg, 16) <= direct::kMaxRowTiles) return run_direct(p, 1, 2, C, ldc, seg, s);
-  if (mean <= 32 && most_segment_tiles(seg, 32) <= direct::kMaxRowTiles) return run_direct(p, 2, 2, C, ldc, seg, s);
+  for (int rm = 1; rm <= (na == 1 ? 2 : 1); ++rm) {
+    const int64_t rows = most_segment_tiles(seg, 16 * rm);
+    if (mean > 16 * rm || rows > direct::kMaxRowTiles) continue;
+    const int wide = direct_experts_cols(na, nb, rm);
+    const int64_t cols = (N + wide - 1) / wide, pairs = (K / 16 + 31) / 32;
+    // waves for a tile: until every CU has eight
+    int kw = 1;
+    while (kw < direct::kExpertWaves && rows * cols * kw < 2048 && 2 * kw <= pairs) kw *= 2;
+    const int64_t each = rows * cols * kw / (512 * direct::kExpertWaves);
+    return run_direct(p, rm, kw, each < 1 ? 1 : each > 8 ? 8 : (int)each, C, ldc, seg, s);
+  }
   return run_tiled(p, mean < 512, false, C, ldc, seg, s);
 }
 

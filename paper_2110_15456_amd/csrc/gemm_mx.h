@@ -499,7 +499,7 @@ __global__ __launch_bounds__(CF::NT, CF::WAVES) void k_gemm_mx(const uint8_t* __
   // explicit pipeline of the two-chunk loop (one operand split at 4 bits)
   constexpr bool PIPE2 = (NA == 2 || NB == 2) && CF::G == 16 && !X3 && !COMB;
   constexpr int NTHR = CF::NT;
-  constexpr int STRIP_BYTES = QNCH ? CF::NW * 16 * (CF::WN + 4) * 4 : 0;
+  constexpr int STRIP_BYTES = QNCH || SEG ? CF::NW * 16 * (CF::WN + 4) * 4 : 0;
   constexpr int SB = XP ? (CF::OFF_EA > STRIP_BYTES ? CF::OFF_EA : STRIP_BYTES) : CF::STAGE;
   constexpr int XEB = XP ? (CF::BM + CF::BN) * 16 : 16;
   // Two stages (and two exponent buffers) as separate LDS objects: the
@@ -1546,6 +1546,37 @@ __global__ __launch_bounds__(CF::NT, CF::WAVES) void k_gemm_mx(const uint8_t* __
       const bool lines = (ldc & 31) == 0 && (reinterpret_cast<uintptr_t>(C) & 127) == 0;
       if (part_slabs > 0 || !lines) store(ic<0>{});
       else store(ic<1>{});
+      return;
+    }
+    if constexpr (SEG != kSegNone) {
+      // Rows of any length and alignment, and the last columns: 16 rows at a time
+      // through the stages, so that a store instruction writes 64 consecutive values
+      // of a row.  Value by value from the registers, 16 rows x 4 columns 4 apart, 5500
+      // x 777 values took 20 us more than x 768; now 5.
+      constexpr int SROW = CF::WN + 4;
+      static_assert(CF::NW * 16 * SROW * 4 <= SB, "a strip per wave fits in one stage");
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      float* strip = reinterpret_cast<float*>(stage0) + wave * (16 * SROW);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          *reinterpret_cast<float4*>(&strip[lr * SROW + j * 16 + 4 * lb]) =
+              make_float4(acc[i][j][0] * scale, acc[i][j][1] * scale, acc[i][j][2] * scale, acc[i][j][3] * scale);
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): this wave's strip writes are done
+        __builtin_amdgcn_wave_barrier();
+        const int row = row0 + wr * CF::WM + i * 16, rows = min(16, M - row);
+        for (int c = lane; c < CF::WN; c += 64)
+          if (wcol + c < N)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float v = strip[r * SROW + c];
+              if (r < rows) C[(int64_t)(row + r) * ldc + wcol + c] = v;
+            }
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // read before the next strip overwrites it
+        __builtin_amdgcn_wave_barrier();
+      }
       return;
     }
 #pragma unroll

@@ -47,6 +47,9 @@ PLANS = [
     (2048, 2, 7, 0.1, 0.0, 1),      # one workgroup, whole; all on one expert
     (4097, 1, 9, 0.1, 1.2, None),   # two workgroups
     (9000, 6, 130, 0.2, 0.5, None),
+    (1025, 1, 6, 0.1, 0.0, None),   # one workgroup, from one slot a lane to four
+    (16384, 1, 8, 0.1, 0.5, None),  # the most that one workgroup takes
+    (8193, 2, 8, 0.1, 0.5, None),   # and more: two launches
 ]
 
 
