@@ -1,6 +1,8 @@
 // gemm_experts.hip -- dispatch of the products of experts over the operand
 // formats, and the choice of their kernel and tile (kernels: gemm_mx.h,
 // gemm_direct.h with SEG).
+#include <math.h>
+
 #include "gemm_direct.h"
 #include "gemm_mx.h"
 
@@ -62,6 +64,62 @@ hipError_t run_direct(const Operands& p, int rm, int kw, int each, float* C, int
   });
 }
 
+// What a product takes, in us, on the tiles there are.  The routing is device data,
+// so the tiles of rows are those that slots spread over all experts would have, each
+// expert's last one half full.  Fitted to graph replays of ten calls at 4 to 1024
+// slots an expert: 8 experts of 2048 x 2048 and 4096 x 4096, 64 of 1024 x 1024, 16 of
+// 576 x 1152; the kernel taken is within 15% of the fastest on most.  What decided,
+// us (few tokens on 16 and 32 rows, tiles of 128 x 128, large tiles):
+//   8 x 2048 x 2048 (4,4)    4 slots   7.4   9.1   17   32     (6,6)  21     -   31  37
+//                           24        11.3   9.6   18   31            37     -   32  37
+//                           64        22    22     20   32           109     -   33  38
+//                          512       170   142     46   41           685     -   97  84
+//   64 x 1024 x 1024 (4,4)  64        61    45     19   25           245     -   42  47
+//                          128       122    90     33   27           372     -   60  50
+//                          256       186   140     47   53           640     -   96  80
+struct Price {
+  double few[2], small, big;  // few[0]: 16 rows, few[1]: 32
+};
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Rounds of 128 x 128 tiles, and of the formats' large ones.
+void price_tiles(const Operands& p, double rows128, double rows256, double slabs, Price& out) {
+  const bool one = p.na == 1 && p.nb == 1, both4 = one && p.fa && p.fb, split2 = p.na == 2 && p.nb == 2;
+  const double n128 = (double)ceil_div(p.N, 128), n256 = (double)ceil_div(p.N, 256);
+  if (one) {
+    // two workgroups of 128 x 128 share a CU, and take a quarter longer than alone
+    const double w = rows128 * n128, full = floor(w / 512.0), rest = w - 512.0 * full;
+    const double two = 1.25 * (4.7 + 1.19 * slabs), alone = 1.25 * (2.4 + 0.93 * slabs);
+    out.small = (both4 ? 0.76 : 1.0) * (full * two + (rest <= 0.5 ? 0.0 : rest <= 256.0 ? alone : two));
+    out.big = (both4 ? 0.92 : 1.0) * ceil(rows256 * n256 / 256.0) * (10.9 + 1.97 * slabs);
+    return;
+  }
+  // the large tile of two planes on one side: 256 rows of the other
+  const double wide = p.na == 1 ? rows256 * n128 : split2 && p.fa && p.fb ? rows256 * n128 : split2 ? rows128 * n128
+                                                                                             : rows128 * n256;
+  out.small = ceil(rows128 * n128 / 256.0) * (split2 ? 4.0 + 2.0 * slabs : 5.0 + 1.45 * slabs);
+  out.big = ceil(wide / 256.0) * (split2 ? 7.0 + 2.2 * slabs : 8.0 + 1.8 * slabs);
+}
+
+// Tiles of T rows that `slots` slots of `experts` experts have.
+double tiles_of_rows(double slots, double experts, int T) {
+  const double busy = slots < experts ? slots : experts;
+  return busy * (slots / busy / T < 0.5 ? 1.0 : slots / busy / T + 0.5);
+}
+
+Price price(const Operands& p, int experts, int64_t slots, int64_t K) {
+  Price out{};
+  const double s = (double)slots, slabs = (double)ceil_div(K / 16, mx::KG) * (K % 128 ? 1.15 : 1.0);
+  price_tiles(p, tiles_of_rows(s, experts, 128), tiles_of_rows(s, experts, 256), slabs, out);
+  // the few-token kernels: the weights, once for every tile of rows, in bytes per us
+  const double bytes = (double)p.N * (double)K *
+                       ((p.nb == 1 ? (p.fb ? 4.0 : 6.0) : p.fb ? 10.0 : 12.0) / 8.0 + 1.0 / 16.0);
+  const double rate = p.na + p.nb == 2 ? 5.0e6 : p.na + p.nb == 3 ? 3.2e6 : p.fa && p.fb ? 2.4e6 : 2.1e6;
+  out.few[0] = 3.0 + tiles_of_rows(s, experts, 16) * bytes / rate;
+  out.few[1] = p.na == 1 ? 3.0 + tiles_of_rows(s, experts, 32) * bytes / (0.72 * rate) : 1e30;
+  return out;
+}
+
 }  // namespace
 
 hipError_t launch_gemm_experts(const uint8_t* a_mant, const uint8_t* a_exp, int a_m, int na, const uint8_t* b_mant,
@@ -73,19 +131,20 @@ hipError_t launch_gemm_experts(const uint8_t* a_mant, const uint8_t* a_exp, int 
                    experts * N * (K / 16) * plane_group_bytes(16, b_m, 0), (int)slots, (int)N, (int)(K / 16), na, nb,
                    fmt_flag(a_m, na), fmt_flag(b_m, nb), ldexpf(1.0f, scale_log2)};
   const Segments seg{offsets, experts, (int)slots};
-  const int64_t mean = slots / experts;
-  for (int rm = 1; rm <= (na == 1 ? 2 : 1); ++rm) {
+  const Price us = price(p, experts, slots, K);
+  const double tiled = us.small < us.big ? us.small : us.big;
+  for (int rm = 1; rm <= 2; ++rm) {
     const int64_t rows = most_segment_tiles(seg, 16 * rm);
-    if (mean > 16 * rm || rows > direct::kMaxRowTiles) continue;
+    if (us.few[rm - 1] > tiled || us.few[rm - 1] > us.few[2 - rm] || rows > direct::kMaxRowTiles) continue;
     const int wide = direct_experts_cols(na, nb, rm);
-    const int64_t cols = (N + wide - 1) / wide, pairs = (K / 16 + 31) / 32;
+    const int64_t cols = ceil_div(N, wide), pairs = ceil_div(K / 16, 32);
     // waves for a tile: until every CU has eight
     int kw = 1;
     while (kw < direct::kExpertWaves && rows * cols * kw < 2048 && 2 * kw <= pairs) kw *= 2;
     const int64_t each = rows * cols * kw / (512 * direct::kExpertWaves);
-    return run_direct(p, rm, kw, each < 1 ? 1 : each > 8 ? 8 : (int)each, C, ldc, seg, s);
+    return run_direct(p, rm, kw, each < 1 ? 1 : each > 4 ? 4 : (int)each, C, ldc, seg, s);
   }
-  return run_tiled(p, mean < 512, false, C, ldc, seg, s);
+  return run_tiled(p, us.small <= us.big, false, C, ldc, seg, s);
 }
 
 hipError_t launch_gemm_experts_grad(const uint8_t* a_mant, const uint8_t* a_exp, int a_m, int na, const uint8_t* b_mant,
@@ -96,8 +155,11 @@ hipError_t launch_gemm_experts_grad(const uint8_t* a_mant, const uint8_t* a_exp,
                    N * (klen / 16) * plane_group_bytes(16, b_m, 0), (int)M, (int)N, (int)(klen / 16), na, nb,
                    fmt_flag(a_m, na), fmt_flag(b_m, nb), ldexpf(1.0f, scale_log2)};
   const Segments seg{k_offsets, experts, (int)klen};
-  const int64_t tiles = (M + 255) / 256 * ((N + 255) / 256) * experts;
-  return run_tiled(p, tiles < 256, true, C, N, seg, s);
+  // (the tiles of every expert, at the mean length of K)
+  Price us{};
+  price_tiles(p, (double)(experts * ceil_div(M, 128)), (double)(experts * ceil_div(M, 256)),
+              (double)klen / 128.0 / experts, us);
+  return run_tiled(p, us.small <= us.big, true, C, N, seg, s);
 }
 
 }  // namespace fastbfp
