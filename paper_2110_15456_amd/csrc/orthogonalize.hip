@@ -402,11 +402,12 @@ __global__ __launch_bounds__(256) void k_ns_finish(Gemm p) {
   }
 }
 
-// The products of symmetric matrices of n <= 96 in one launch, a workgroup for each
+// The products of symmetric matrices of n <= 128 in one launch, a workgroup for each
 // matrix with a wave for each 32 x 32 tile: S from the sums of X X^T's parts, P, and
 // for a pair of steps S P, P S P, P' and P' P; the planes of P or P' P leave.
-// Everything stays in LDS (three matrices, 110 KB at n = 96): a launch for each
-// product takes 6.9 us at n = 64 where its 12 MFMAs a wave take 0.3.
+// Everything stays in LDS, in two matrices (128 KB at n = 128), as each product takes
+// the place of an operand that it is the last to read: a launch for each product
+// takes 6.9 us at n = 64 where its 12 MFMAs a wave take 0.3.
 struct Chain {
   const float* sums;  // [matrix][part][128][128]
   int parts, n, pair;
@@ -416,7 +417,7 @@ struct Chain {
 template <int NB>
 __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
   constexpr int R = KS * NB, ROW = BLOCK * NB, NT = 64 * NB * NB;
-  __shared__ __attribute__((aligned(128))) uint8_t mem[3][R * ROW];
+  __shared__ __attribute__((aligned(128))) uint8_t mem[2][R * ROW];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int wr = wave / NB, wc = wave % NB, fr = lane & 31, fk = lane >> 5;
   // chunk c (16 bytes) of row r, spread over the banks within its block
@@ -432,7 +433,7 @@ __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
     *reinterpret_cast<h4*>(m + at(r, chunk) + (c & 4) * 2) = hi;
     *reinterpret_cast<h4*>(m + at(r, chunk + 4) + (c & 4) * 2) = lo;
   };
-  // dst = alpha a b^T + beta m + gamma I; dst is none of the others
+  // dst = alpha a b^T + beta m + gamma I; dst may be any of the others
   auto product = [&](uint8_t* dst, const uint8_t* a, const uint8_t* b, float alpha, const uint8_t* m, float beta,
                      float gamma) {
     v16 acc = {};
@@ -449,10 +450,11 @@ __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
       acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[1][1], f[0][0], acc, 0, 0, 0);
       acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[1][0], f[0][0], acc, 0, 0, 0);
     }
+    v4 out[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int r = 32 * wr + fr, c = 32 * wc + 8 * q + 4 * fk, chunk = c / KS * 8 + (c % KS) / 8;
-      v4 v;
+      v4& v = out[q];
 #pragma unroll
       for (int t = 0; t < 4; ++t) v[t] = acc[4 * q + t] * alpha;
       if (m) {
@@ -464,11 +466,13 @@ __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
 #pragma unroll
       for (int t = 0; t < 4; ++t)
         if (r == c + t && r < p.n) v[t] += gamma;
-      put4(dst, r, c, v);
     }
+    __syncthreads();  // every wave has read
+#pragma unroll
+    for (int q = 0; q < 4; ++q) put4(dst, 32 * wr + fr, 32 * wc + 8 * q + 4 * fk, out[q]);
     __syncthreads();
   };
-  uint8_t *S = mem[0], *P = mem[1], *T = mem[2];
+  uint8_t *S = mem[0], *P = mem[1];
   const float* sums = p.sums + (int64_t)blockIdx.x * p.parts * (128 * 128);
   for (int q = tid; q < R * R / 4; q += NT) {
     const int r = q / (R / 4), c = 4 * (q % (R / 4));
@@ -483,10 +487,10 @@ __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
   product(P, S, S, sq, S, li, id);
   const uint8_t* Q = P;
   if (p.pair) {
-    product(T, S, P, one, nullptr, 0.0f, 0.0f);
-    product(S, T, P, one, nullptr, 0.0f, 0.0f);
-    product(T, S, S, sq, S, li, id);
-    product(S, T, P, ldexpf(1.0f, kQScale - 2 * kPScale), nullptr, 0.0f, 0.0f);
+    product(S, S, P, one, nullptr, 0.0f, 0.0f);  // S P
+    product(S, S, P, one, nullptr, 0.0f, 0.0f);  // P S P
+    product(S, S, S, sq, S, li, id);             // P'
+    product(S, S, P, ldexpf(1.0f, kQScale - 2 * kPScale), nullptr, 0.0f, 0.0f);
     Q = S;
   }
   uint8_t* out = p.out + blockIdx.x * p.out_batch;
@@ -577,7 +581,7 @@ __global__ __launch_bounds__(256) void k_ns_split(const float* __restrict__ g, c
 }
 
 constexpr int kNormBlocks = 2048;
-constexpr int kChainMost = 96;  // rows of the matrices that k_ns_chain takes
+constexpr int kChainMost = 128;  // rows of the matrices that k_ns_chain takes
 
 }  // namespace ns
 
@@ -739,7 +743,8 @@ hipError_t launch_orthogonalize(const float* grad, const float* momentum, float*
       const Chain c{sum, parts, n, group == 2, poly[0], p.s_bytes};
       if (n <= 32) hipLaunchKernelGGL(k_ns_chain<1>, dim3((unsigned)batch), dim3(64), 0, s, c);
       else if (n <= 64) hipLaunchKernelGGL(k_ns_chain<2>, dim3((unsigned)batch), dim3(256), 0, s, c);
-      else hipLaunchKernelGGL(k_ns_chain<3>, dim3((unsigned)batch), dim3(576), 0, s, c);
+      else if (n <= 96) hipLaunchKernelGGL(k_ns_chain<3>, dim3((unsigned)batch), dim3(576), 0, s, c);
+      else hipLaunchKernelGGL(k_ns_chain<4>, dim3((unsigned)batch), dim3(1024), 0, s, c);
       Q = poly[0], q_scale = group == 2 ? kQScale : kPScale;
     } else {
       e = product(X[at], X[at], p.x_bytes, k, p.gram, S, ldexpf(1.0f, kSScale - 2 * kXScale), nullptr, 0.0f, 0.0f);
