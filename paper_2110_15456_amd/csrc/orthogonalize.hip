@@ -567,7 +567,9 @@ __global__ __launch_bounds__(256) void k_ns_split(const float* __restrict__ g, c
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
   __syncthreads();
   const double norm = sqrt((red[0] + red[1]) + (red[2] + red[3]));
-  const float inv = (float)((double)(1 << kXScale) / (norm + (double)eps));
+  // the factor as a fraction and a power of two, which may lie outside FP32's range
+  int power;
+  const float part_of = (float)frexp((double)(1 << kXScale) / (norm + (double)eps), &power);
   const int64_t ld = blocks_of(k);
   uint8_t* out = x + matrix * (n * ld * BLOCK);
   for (int q = threadIdx.x; q < T * 16; q += 256) {
@@ -575,7 +577,7 @@ __global__ __launch_bounds__(256) void k_ns_split(const float* __restrict__ g, c
     if (r0 + r >= n || c0 + col >= ld * KS) continue;
     float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = inv * (FLIP ? tile[col + i][r] : tile[r][col + i]);
+    for (int i = 0; i < 8; ++i) v[i] = part_of * ldexpf(FLIP ? tile[col + i][r] : tile[r][col + i], power);
     store_chunk(out + ((int64_t)(r0 + r) * ld + (c0 + col) / KS) * BLOCK + lo * 64 + kk * 16, v, lo);
   }
 }

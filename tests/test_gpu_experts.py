@@ -249,6 +249,20 @@ def test_weight_gradients(tokens, top, experts, drop, skew, busy, M, N):
                 assert not G[e].any()
 
 
+def test_no_tokens():
+    """An empty batch: nothing to write but the weights' gradients, zeros."""
+    announce("expert layer without tokens")
+    p = fb.expert_plan(torch.zeros((0, 2), dtype=torch.int64, device="cuda"), 3)
+    x = torch.zeros((0, 32), device="cuda")
+    tr, tc = fb.quantize_experts(x, p, gather=True)
+    W = fb.quantize(torch.randn((3 * 8, 32), device="cuda"))
+    y = fb.gemm_experts(tr, W, p)
+    assert tuple(y.shape) == (0, 8) and tuple(fb.combine_experts(y, p).shape) == (0, 8)
+    _, dt = fb.quantize_experts(torch.zeros((0, 16), device="cuda"), p)
+    out = torch.full((3, 16, 32), 7.0, device="cuda")
+    assert not bool(fb.gemm_experts_grad(dt, tc, p, out=out).any())
+
+
 def test_gradients_against_differences():
     """Of small whole numbers, which BFP at 8 bits holds exactly, so that the layer
     is linear and every sum exact: <dX, d> is the forward's change along d, and

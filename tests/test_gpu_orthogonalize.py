@@ -109,6 +109,16 @@ def test_scale_zeros_and_poison():
     assert not bool(out[1].any()) and not bool(out[2].isfinite().all()) and not bool(out[3].isfinite().all())
 
 
+@pytest.mark.parametrize("power", [-124, -60, 100])
+def test_far_scales(power):
+    """Gradients whose norm, or the factor that normalises them, is near the ends of
+    FP32's range (the smallest entries here are still normal numbers)."""
+    announce("orthogonalize at 2^%d" % power)
+    u = torch.randn((40, 60), generator=torch.Generator().manual_seed(9))
+    u = torch.where(u.abs() < 0.25, torch.ones_like(u), u).cuda()
+    assert torch.equal(fb.orthogonalize(u * 2.0 ** power, eps=0.0), fb.orthogonalize(u, eps=0.0))
+
+
 def test_transposed_and_unaligned():
     """The update of the transpose is the update's transpose (the same products), and
     rows that start off a 16-byte boundary give the same bits."""
