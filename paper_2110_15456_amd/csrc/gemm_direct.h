@@ -185,62 +185,59 @@ template <int NP, int K0, int K1> struct Frag {
   uint32_t e;
 };
 
-// One superstep of a wave: every row tile of A against every one of B.
-template <int NA, int NB, int FA, int FB, int G, int RM, int RN, class FragA, class FragB>
-__device__ __forceinline__ void superstep(v4f (&acc)[RM][RN], const FragA (&fa)[RM], const FragB (&fb)[RN]) {
-  constexpr int KA0 = (NA == 1 && FA) ? kPlaneFP4 : kPlaneFP6, KB0 = (NB == 1 && FB) ? kPlaneFP4 : kPlaneFP6;
-  constexpr int KA1 = FA ? kPlaneLo2 : kPlaneFP6, KB1 = FB ? kPlaneLo2 : kPlaneFP6;
-  constexpr bool SA = NA == 2 && FA, SB = NB == 2 && FB;  // split at 2 bits
-#pragma unroll
-  for (int u = 0; u < (G == 16 ? 4 : 2); ++u) {
-#pragma unroll
-    for (int i = 0; i < RM; ++i) {
-      const auto& x = fa[i];
-      const uint32_t ea = (x.e >> (8 * u)) & 0xFFu;
-#pragma unroll
-      for (int j = 0; j < RN; ++j) {
-        const auto& y = fb[j];
-        const uint32_t eb = (y.e >> (8 * u)) & 0xFFu;
-        v4f& c = acc[i][j];
-        // The chunk weights on the scale bytes and the pairing of planes
-        // are those of gemm_mx.h.
-        if constexpr (G == 32) {
-          constexpr int wa0 = NA == 1 ? 0 : SA ? 2 : 4, wa1 = SA ? 2 : 0;
-          constexpr int wb0 = NB == 1 ? 0 : SB ? 2 : 4, wb1 = SB ? 2 : 0;
-          mma<KA0, KB0>(c, x.p0.pair(u), y.p0.pair(u), ea + wa0, eb + wb0);
-          if constexpr (NA == 2) mma<KA1, KB0>(c, x.p1.pair(u), y.p0.pair(u), ea + wa1, eb + wb0);
-          if constexpr (NB == 2) mma<KA0, KB1>(c, x.p0.pair(u), y.p1.pair(u), ea + wa0, eb + wb1);
-          if constexpr (NA == 2 && NB == 2) mma<KA1, KB1>(c, x.p1.pair(u), y.p1.pair(u), ea + wa1, eb + wb1);
-        } else if constexpr (SA) {
-          // A's [q >> 2 | q & 3] block against each plane of B repeated
-          const v8i av = join(x.p0, x.p1, u);
-          constexpr int wb0 = NB == 1 ? 0 : SB ? 2 : 4, wb1 = SB ? 2 : 0;
-          mma<kPlaneFP6, KB0>(c, av, y.p0.template half<true>(u), ea + 2, eb + wb0);
-          if constexpr (NB == 2) mma<kPlaneFP6, KB1>(c, av, y.p1.template half<true>(u), ea + 2, eb + wb1);
-        } else if constexpr (SB) {
-          const v8i bv = join(y.p0, y.p1, u);
-          constexpr int wa0 = NA == 1 ? 0 : 4;
-          mma<KA0, kPlaneFP6>(c, x.p0.template half<true>(u), bv, ea + wa0, eb + 2);
-          if constexpr (NA == 2) mma<KA1, kPlaneFP6>(c, x.p1.template half<true>(u), bv, ea, eb + 2);
-        } else if constexpr (NA == 2 && NB == 2) {
-          // split at 4 bits on both sides: the two cross products share one MFMA
-          mma<KA0, KB0>(c, x.p0.template half<false>(u), y.p0.template half<false>(u), ea + 4, eb + 4);
-          mma<KA1, KB1>(c, x.p1.template half<false>(u), y.p1.template half<false>(u), ea, eb);
-          mma<kPlaneFP6, kPlaneFP6>(c, join(x.p0, x.p1, u), join(y.p1, y.p0, u), ea + 4, eb);
-        } else {
-          constexpr int wa0 = NA == 1 ? 0 : 4, wb0 = NB == 1 ? 0 : 4;
-          mma<KA0, KB0>(c, x.p0.template half<false>(u), y.p0.template half<false>(u), ea + wa0, eb + wb0);
-          if constexpr (NA == 2)
-            mma<KA1, KB0>(c, x.p1.template half<false>(u), y.p0.template half<false>(u), ea, eb + wb0);
-          if constexpr (NB == 2)
-            mma<KA0, KB1>(c, x.p0.template half<false>(u), y.p1.template half<false>(u), ea + wa0, eb);
-        }
-      }
-    }
-  }
-}
-
 }  // namespace direct
+
+// One superstep of a wave: ROWS row tiles of A, FRAG_A, against COLS of B, FRAG_B,
+// into ACC.  The chunk weights on the scale bytes and the pairing of planes are those
+// of gemm_mx.h: an operand split at 2 bits is the block [q >> 2 | q & 3] against each
+// plane of the other repeated; split at 4 bits on both sides, the two cross
+// products share one MFMA.  (A macro: of a function, however inlined, the compiler
+// merges the reads of the fragments before they are registers, and keeps them in
+// memory in half of the kernels.)
+#define FASTBFP_DIRECT_SUPERSTEP(ACC, FRAG_A, FRAG_B, ROWS, COLS) \
+    _Pragma("unroll")                                                                                           \
+    for (int u = 0; u < (G == 16 ? 4 : 2); ++u) {                                                               \
+    _Pragma("unroll")                                                                                           \
+      for (int i = 0; i < ROWS; ++i) {                                                                          \
+        const auto& x = FRAG_A[i];                                                                              \
+        const uint32_t ea = (x.e >> (8 * u)) & 0xFFu;                                                           \
+    _Pragma("unroll")                                                                                           \
+        for (int j = 0; j < COLS; ++j) {                                                                        \
+          const auto& y = FRAG_B[j];                                                                            \
+          const uint32_t eb = (y.e >> (8 * u)) & 0xFFu;                                                         \
+          v4f& c = ACC[i][j];                                                                                   \
+          if constexpr (G == 32) {                                                                              \
+            constexpr int wa0 = NA == 1 ? 0 : SA ? 2 : 4, wa1 = SA ? 2 : 0;                                     \
+            constexpr int wb0 = NB == 1 ? 0 : SB ? 2 : 4, wb1 = SB ? 2 : 0;                                     \
+            mma<KA0, KB0>(c, x.p0.pair(u), y.p0.pair(u), ea + wa0, eb + wb0);                                   \
+            if constexpr (NA == 2) mma<KA1, KB0>(c, x.p1.pair(u), y.p0.pair(u), ea + wa1, eb + wb0);            \
+            if constexpr (NB == 2) mma<KA0, KB1>(c, x.p0.pair(u), y.p1.pair(u), ea + wa0, eb + wb1);            \
+            if constexpr (NA == 2 && NB == 2) mma<KA1, KB1>(c, x.p1.pair(u), y.p1.pair(u), ea + wa1, eb + wb1); \
+          } else if constexpr (SA) {                                                                            \
+            const v8i av = join(x.p0, x.p1, u);                                                                 \
+            constexpr int wb0 = NB == 1 ? 0 : SB ? 2 : 4, wb1 = SB ? 2 : 0;                                     \
+            mma<kPlaneFP6, KB0>(c, av, y.p0.template half<true>(u), ea + 2, eb + wb0);                          \
+            if constexpr (NB == 2) mma<kPlaneFP6, KB1>(c, av, y.p1.template half<true>(u), ea + 2, eb + wb1);   \
+          } else if constexpr (SB) {                                                                            \
+            const v8i bv = join(y.p0, y.p1, u);                                                                 \
+            constexpr int wa0 = NA == 1 ? 0 : 4;                                                                \
+            mma<KA0, kPlaneFP6>(c, x.p0.template half<true>(u), bv, ea + wa0, eb + 2);                          \
+            if constexpr (NA == 2) mma<KA1, kPlaneFP6>(c, x.p1.template half<true>(u), bv, ea, eb + 2);         \
+          } else if constexpr (NA == 2 && NB == 2) {                                                            \
+            mma<KA0, KB0>(c, x.p0.template half<false>(u), y.p0.template half<false>(u), ea + 4, eb + 4);       \
+            mma<KA1, KB1>(c, x.p1.template half<false>(u), y.p1.template half<false>(u), ea, eb);               \
+            mma<kPlaneFP6, kPlaneFP6>(c, join(x.p0, x.p1, u), join(y.p1, y.p0, u), ea + 4, eb);                 \
+          } else {                                                                                              \
+            constexpr int wa0 = NA == 1 ? 0 : 4, wb0 = NB == 1 ? 0 : 4;                                         \
+            mma<KA0, KB0>(c, x.p0.template half<false>(u), y.p0.template half<false>(u), ea + wa0, eb + wb0);   \
+            if constexpr (NA == 2)                                                                              \
+              mma<KA1, KB0>(c, x.p1.template half<false>(u), y.p0.template half<false>(u), ea, eb + wb0);       \
+            if constexpr (NB == 2)                                                                              \
+              mma<KA0, KB1>(c, x.p0.template half<false>(u), y.p1.template half<false>(u), ea + wa0, eb);       \
+          }                                                                                                     \
+        }                                                                                                       \
+      }                                                                                                         \
+    }
 
 // NA / NB, FA / FB, G: as mx::Cfg (planes read; FP4 codes, or split at 2 bits).
 // BOUT: C is written as BFP (N a multiple of 16).
@@ -252,6 +249,7 @@ __global__ __launch_bounds__(64 * direct::kMaxWaves) void k_gemm_direct(
   using namespace direct;
   constexpr int KA0 = (NA == 1 && FA) ? kPlaneFP4 : kPlaneFP6, KB0 = (NB == 1 && FB) ? kPlaneFP4 : kPlaneFP6;
   constexpr int KA1 = FA ? kPlaneLo2 : kPlaneFP6, KB1 = FB ? kPlaneLo2 : kPlaneFP6;
+  constexpr bool SA = NA == 2 && FA, SB = NB == 2 && FB;  // split at 2 bits
   constexpr int SROW = 16 * RN + 4;                       // LDS row stride in floats (padding spreads the banks)
   __shared__ __attribute__((aligned(16))) float part[kMaxWaves][16 * RM * SROW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -299,7 +297,7 @@ __global__ __launch_bounds__(64 * direct::kMaxWaves) void k_gemm_direct(
       if constexpr (NA == 2) fa[i].p1.load(ra1, (r * ng + u0) * UA1);
       fa[i].e = load_exps<G>(rea, G == 16 ? r * ng_e + u0 : r * ng_e + u0 / 2, ng - u0, dw);
     }
-    superstep<NA, NB, FA, FB, G, RM, RN>(acc, fa, fb);
+    FASTBFP_DIRECT_SUPERSTEP(acc, fa, fb, RM, RN)
   }
 #pragma unroll
   for (int i = 0; i < RM; ++i)
@@ -472,6 +470,8 @@ __global__ __launch_bounds__(64 * direct::kExpertWaves, 2) void k_gemm_direct_ex
   using namespace direct;
   constexpr int KA0 = (NA == 1 && FA) ? kPlaneFP4 : kPlaneFP6, KB0 = (NB == 1 && FB) ? kPlaneFP4 : kPlaneFP6;
   constexpr int KA1 = FA ? kPlaneLo2 : kPlaneFP6, KB1 = FB ? kPlaneLo2 : kPlaneFP6;
+  constexpr bool SA = NA == 2 && FA, SB = NB == 2 && FB;
+  constexpr int G = 16;
   typedef Rows16<KA0> A0;
   typedef Rows16<KA1> A1;
   typedef Rows16<KB0> B0;
@@ -582,17 +582,17 @@ __global__ __launch_bounds__(64 * direct::kExpertWaves, 2) void k_gemm_direct_ex
           }
         }
 #pragma unroll
-        for (int j = 0; j < RN; ++j) {
-          b0[j].put(mine, lane);
-          if constexpr (NB == 2) b1[j].put(mine + B0::BYTES, lane);
-          if (j + 1 == RN && (same || works(g + (int)gridDim.x))) load(same ? g : g + (int)gridDim.x, same ? p + 1 : p0);
+        for (int jb = 0; jb < RN; ++jb) {
+          b0[jb].put(mine, lane);
+          if constexpr (NB == 2) b1[jb].put(mine + B0::BYTES, lane);
+          if (jb + 1 == RN && (same || works(g + (int)gridDim.x))) load(same ? g : g + (int)gridDim.x, same ? p + 1 : p0);
           Frag<NB, KB0, KB1> fb[1];
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
             B0::get(mine, lane, s, fb[0].p0);
             if constexpr (NB == 2) B1::get(mine + B0::BYTES, lane, s, fb[0].p1);
-            fb[0].e = get_exps(mine + OFF_BE + 512 * j, lane, s, left - 16 * s);
-            superstep<NA, NB, FA, FB, 16, RM, 1>(acc[j], fa[s], fb);
+            fb[0].e = get_exps(mine + OFF_BE + 512 * jb, lane, s, left - 16 * s);
+            FASTBFP_DIRECT_SUPERSTEP(acc[jb], fa[s], fb, RM, 1)
           }
         }
       }

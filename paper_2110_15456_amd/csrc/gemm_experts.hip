@@ -66,17 +66,17 @@ hipError_t run_direct(const Operands& p, int rm, int kw, int each, float* C, int
 
 // What a product takes, in us, on the tiles there are.  The routing is device data,
 // so the tiles of rows are those that slots spread over all experts would have, each
-// expert's last one half full.  Fitted to graph replays of ten calls at 4 to 1024
+// expert's last one half full.  Fitted to graph replays of ten calls at 1 to 1024
 // slots an expert: 8 experts of 2048 x 2048 and 4096 x 4096, 64 of 1024 x 1024, 16 of
 // 576 x 1152; the kernel taken is within 15% of the fastest on most.  What decided,
 // us (few tokens on 16 and 32 rows, tiles of 128 x 128, large tiles):
-//   8 x 2048 x 2048 (4,4)    4 slots   7.4   9.1   17   32     (6,6)  21     -   31  37
-//                           24        11.3   9.6   18   31            37     -   32  37
-//                           64        22    22     20   32           109     -   33  38
-//                          512       170   142     46   41           685     -   97  84
-//   64 x 1024 x 1024 (4,4)  64        61    45     19   25           245     -   42  47
-//                          128       122    90     33   27           372     -   60  50
-//                          256       186   140     47   53           640     -   96  80
+//   8 x 2048 x 2048 (4,4)    4 slots   7.2   9.0   18   32     (6,6)  12     -   31  37
+//                           24        11.4   9.6   19   31            18     -   31  37
+//                           64        22    22     19   32            40     -   34  38
+//                          512       170   142     46   41             -     -   97  84
+//   64 x 1024 x 1024 (4,4)  64        60    50     18   25            79     -   42  47
+//                          128       122    90     33   27             -     -   60  50
+//                          256       186   140     47   53             -     -   96  80
 struct Price {
   double few[2], small, big;  // few[0]: 16 rows, few[1]: 32
 };
@@ -114,9 +114,9 @@ Price price(const Operands& p, int experts, int64_t slots, int64_t K) {
   // the few-token kernels: the weights, once for every tile of rows, in bytes per us
   const double bytes = (double)p.N * (double)K *
                        ((p.nb == 1 ? (p.fb ? 4.0 : 6.0) : p.fb ? 10.0 : 12.0) / 8.0 + 1.0 / 16.0);
-  const double rate = p.na + p.nb == 2 ? 5.0e6 : p.na + p.nb == 3 ? 3.2e6 : p.fa && p.fb ? 2.4e6 : 2.1e6;
+  constexpr double rate = 5.0e6;
   out.few[0] = 3.0 + tiles_of_rows(s, experts, 16) * bytes / rate;
-  out.few[1] = p.na == 1 ? 3.0 + tiles_of_rows(s, experts, 32) * bytes / (0.72 * rate) : 1e30;
+  out.few[1] = p.na == 1 ? 3.0 + tiles_of_rows(s, experts, 32) * bytes / (0.85 * rate) : 1e30;
   return out;
 }
 
