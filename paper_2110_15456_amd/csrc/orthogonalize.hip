@@ -135,7 +135,7 @@ __device__ __forceinline__ int xcd_order(int bid, int n) {
 // fragments for 96 (48) MFMAs of 32x32x16, i.e. the LDS is busy half of the time
 // that the matrix cores are.
 template <int BM, int BN, int WGM, int WGN, bool TR, int OUT>
-__global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
+__global__ __launch_bounds__(64 * WGM * WGN, BM == 64 ? 4 : 2) void k_ns_gemm(Gemm p) {
   constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 32, TN = WN / 32;
   constexpr int OFF_B = BM * BLOCK, STAGE = OFF_B + BN * BLOCK;
   static_assert((BM / 8) % NW == 0 && (BN / 8) % NW == 0 && NW % 2 == 0, "loads split evenly over the waves");
@@ -261,28 +261,36 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
   // tile.  64 x 64 values at a time go through the wave's 16 KB of the stages, so
   // that rows and, mirrored, columns leave as whole lines.  16-byte granule g of row r
   // sits at g ^ swz(r): 16 rows of one granule, and 8 rows 8 apart, on all banks.
+  // (On the 64 tile the four waves' 32 x 32 are one such piece, of which each
+  // writes a quarter.)
   __syncthreads();
-  static_assert(WN == 64 && TM % 2 == 0 && NW * 16384 <= 2 * STAGE, "a wave's sums fit in its share of the stages");
-  float* tile = reinterpret_cast<float*>((wave < NW / 2 ? stage0 : stage1) + (wave % (NW / 2)) * 16384);
+  constexpr bool JOIN = BM == 64;
+  static_assert(JOIN ? BN == 64 && NW == 4 && STAGE == 16384
+                     : WN == 64 && TM % 2 == 0 && NW * 16384 <= 2 * STAGE, "the sums fit in the stages");
+  constexpr int HI = JOIN ? 1 : 2, ITS = JOIN ? 4 : 16;  // 32-row pieces of a wave's share, its lines / 4
+  float* tile = reinterpret_cast<float*>(JOIN ? stage0
+                                              : (wave < NW / 2 ? stage0 : stage1) + (wave % (NW / 2)) * 16384);
+  const int pr = JOIN ? wr * 32 : 0, pg = JOIN ? wc * 8 : 0, it0 = JOIN ? wave * ITS : 0;
   auto at = [](int r, int g) __attribute__((always_inline)) -> int { return r * 64 + ((g ^ ((r ^ (r >> 3)) & 15)) * 4); };
   uint8_t* C = p.c + batch * p.c_batch;
   const float alpha = OUT == kSym && sums ? 1.0f : p.alpha;
 #pragma unroll
-  for (int half = 0; half < TM / 2; ++half) {
+  for (int half = 0; half < (JOIN ? 1 : TM / 2); ++half) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < HI; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           v4 v;
 #pragma unroll
-          for (int t = 0; t < 4; ++t) v[t] = acc[2 * half + i][j][4 * q + t] * alpha;
-          *reinterpret_cast<v4*>(&tile[at(32 * i + fr, 8 * j + 2 * q + fk)]) = v;
+          for (int t = 0; t < 4; ++t) v[t] = acc[HI * half + i][j][4 * q + t] * alpha;
+          *reinterpret_cast<v4*>(&tile[at(pr + 32 * i + fr, pg + 8 * j + 2 * q + fk)]) = v;
         }
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the wave reads back what it wrote
-    __builtin_amdgcn_wave_barrier();
-    const int r0 = row0 + wr * WM + 64 * half, c0 = col0 + wc * WN;
+    if constexpr (JOIN) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
+    const int r0 = JOIN ? row0 : row0 + wr * WM + 64 * half, c0 = JOIN ? col0 : col0 + wc * WN;
     auto row8 = [&](int r, int c, float (&x)[8]) __attribute__((always_inline)) {
       const v4 a = *reinterpret_cast<const v4*>(&tile[at(r, c / 4)]), b = *reinterpret_cast<const v4*>(&tile[at(r, c / 4 + 1)]);
 #pragma unroll
@@ -293,9 +301,9 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
       for (int t = 0; t < 8; ++t) x[t] = tile[at(r + t, c / 4) + (c & 3)];
     };
     if (OUT == kSym && sums) {
-      float* o = sums + (wr * WM + 64 * half) * BN + wc * WN;
+      float* o = sums + (r0 - row0) * BN + (c0 - col0);
 #pragma unroll 4
-      for (int it = 0; it < 16; ++it) {
+      for (int it = it0; it < it0 + ITS; ++it) {
         const int r = 4 * it + (lane >> 4), c = 4 * (lane & 15);
         *reinterpret_cast<v4*>(o + r * BN + c) = *reinterpret_cast<const v4*>(&tile[at(r, c / 4)]);
       }
@@ -305,7 +313,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
       for (int mirror = 0; mirror < (OUT == kSym && tm != tn ? 2 : 1); ++mirror) {
         const int ro = mirror ? c0 : r0, co = mirror ? r0 : c0, rows = mirror ? p.N : p.M;
 #pragma unroll 4
-        for (int it = 0; it < 16; ++it) {
+        for (int it = it0; it < it0 + ITS; ++it) {
           const int r = 4 * it + (lane >> 4), blk = (lane >> 3) & 1, lo = (lane >> 2) & 1, k = lane & 3;
           const int c = blk * KS + 8 * k;
           if (ro + r >= rows || co + c >= p.ldc) continue;
@@ -332,7 +340,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_ns_gemm(Gemm p) {
       const int rows = OUT == kF32T ? p.N : p.M, cols = OUT == kF32T ? p.M : p.N;
       const bool vec = (p.ldc & 3) == 0 && (reinterpret_cast<uintptr_t>(C) & 15) == 0;
 #pragma unroll 4
-      for (int it = 0; it < 16; ++it) {
+      for (int it = it0; it < it0 + ITS; ++it) {
         const int r = 4 * it + (lane >> 4), c = 4 * (lane & 15);
         v4 v;
         if constexpr (OUT == kF32T) {
@@ -593,31 +601,42 @@ using namespace ns;
 
 int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
-// Tiles of 256 x 256 or 128 x 128 (one or two workgroups on each of 256 CUs).
+// Tiles of 256, 128 or 64 squared, of which a CU takes one, two or four at once.
 // Whole rounds of tiles run as they are; those left over, where the product may be
-// split, are summed in parts of K that share out the last round.  Priced in slabs of
-// a 128 tile alone on a CU: a 256 tile's slab takes four, two 128 tiles that share a
-// CU 2.06, a tile six slabs' time to start and end, a split a second launch and its
-// sums' way to memory and back.  (n = 4096, K = 4096, 528 tiles of 128: whole 251 us,
-// all of them in three parts 239.)
+// split, are summed in parts of K that share out the last round.  Priced in us: a slab
+// of a tile that has its CU for itself, what each further tile there adds, the start
+// and end of a tile, and a split's second launch and its sums' way to memory and back.
+// (S S^T of n = 256: 14.8 us on 128 tiles, 8.3 on 64; n = 4096: 290 on 64, 206 on 128
+// with the last 16 of 528 tiles in parts, 251 without; Q X of 4096 x 16384: 1940, 1600
+// and 1450 on 64, 128 and 256.)
 struct Tiling {
   int tile, parts;
   int64_t whole;
 };
-Tiling tiling(int64_t tiles256, int64_t tiles128, int64_t slabs, bool split) {
-  Tiling best{128, 1, tiles128};
+Tiling tiling(const int64_t (&count)[3], int64_t slabs, bool split) {
+  struct Price {
+    int tile, per_cu;
+    double slab, more, ends, part_ends, sums;
+  };
+  constexpr Price prices[3] = {{256, 1, 2.8, 0.0, 10.0, 8.0, 0.045},
+                               {128, 2, 1.0, 0.45, 6.5, 2.0, 0.0125},
+                               {64, 4, 0.5, 0.14, 4.5, 2.3, 0.003}};
+  Tiling best{128, 1, count[1]};
   double least = 1e30;
-  for (const int tile : {256, 128}) {
-    const int64_t tiles = tile == 256 ? tiles256 : tiles128, room = tile == 256 ? 256 : 512;
-    const double slab = tile == 256 ? 4.0 : 2.06;
-    const int64_t whole = tiles / room * room, rest = tiles - whole;
+  for (int i = 0; i < 3; ++i) {
+    const Price& p = prices[i];
+    const int64_t tiles = count[i], room = 256 * p.per_cu, whole = tiles / room * room, rest = tiles - whole;
+    // workgroups of so many slabs, in rounds
+    auto rounds = [&](int64_t wgs, int64_t s) {
+      const int64_t left = wgs % room, deep = (left + 255) / 256;
+      return (double)(wgs / room) * (s * (p.slab + (p.per_cu - 1) * p.more) + p.ends / 2) +
+             (left ? s * (p.slab + (deep - 1) * p.more) : 0.0);
+    };
     for (int64_t parts = 1; parts == 1 || (split && rest > 0 && parts <= 64 && slabs / parts >= 4); ++parts) {
-      const int64_t wgs = rest * parts, ps = (slabs + parts - 1) / parts;
-      const int64_t full = wgs / room, left = wgs % room;
-      const double last = left == 0 ? 0.0 : tile == 128 && left <= 256 ? 1.2 : slab;
-      double cost = (double)(whole / room) * slab * (slabs + 6) + (full * slab + last) * (ps + 6);
-      if (parts > 1) cost += 8.0 + (tile == 256 ? 0.08 : 0.02) * wgs;
-      if (cost < least) least = cost, best = Tiling{tile, (int)parts, parts > 1 ? whole : tiles};
+      const int64_t ps = (slabs + parts - 1) / parts, wgs = rest * parts;
+      const double cost = parts == 1 ? rounds(tiles, slabs) + p.ends
+                                     : rounds(whole, slabs) + rounds(wgs, ps) + p.part_ends + 6.5 + p.sums * wgs;
+      if (cost < least) least = cost, best = Tiling{p.tile, (int)parts, parts > 1 ? whole : tiles};
     }
   }
   return best;
@@ -639,16 +658,17 @@ NsPlan ns_plan(int64_t batch, int64_t rows, int64_t cols) {
   p.ld = blocks_of(p.n) * KS;
   p.x_bytes = p.n * blocks_of(p.k) * BLOCK;
   p.s_bytes = p.n * blocks_of(p.n) * BLOCK;
-  const int64_t n256 = (p.n + 255) / 256, n128 = (p.n + 127) / 128;
-  const int64_t tri256 = batch * n256 * (n256 + 1) / 2, tri128 = batch * n128 * (n128 + 1) / 2;
-  p.gram = tiling(tri256, tri128, blocks_of(p.k), true);
-  p.square = tiling(tri256, tri128, blocks_of(p.n), true);
+  // tiles of edge t in a matrix, and in the lower triangles of all
+  auto count = [&](int64_t t) { return (p.n + t - 1) / t * ((p.k + t - 1) / t) * batch; };
+  auto tri = [&](int64_t t) { return batch * ((p.n + t - 1) / t) * ((p.n + t - 1) / t + 1) / 2; };
+  p.gram = tiling({tri(256), tri(128), tri(64)}, blocks_of(p.k), true);
+  p.square = tiling({tri(256), tri(128), tri(64)}, blocks_of(p.n), true);
   if (p.n <= kChainMost) {  // one tile a matrix, its sums left to the chain
     const int64_t slabs = blocks_of(p.k), fill = 512 / batch, most = slabs / 4 < 16 ? slabs / 4 : 16;
     p.gram = Tiling{128, (int)(fill < 1 || most < 1 ? 1 : fill < most ? fill : most), 0};
-    p.square = Tiling{128, 1, tri128};
+    p.square = Tiling{128, 1, tri(128)};
   }
-  p.apply = tiling(batch * n256 * ((p.k + 255) / 256), batch * n128 * ((p.k + 127) / 128), blocks_of(p.n), false);
+  p.apply = tiling({count(256), count(128), count(64)}, blocks_of(p.n), false);
   const int64_t per = (p.n * p.k + 4095) / 4096;
   p.norm_blocks = (int)(per < kNormBlocks ? per : kNormBlocks);
   int64_t at = 0;
@@ -662,7 +682,7 @@ NsPlan ns_plan(int64_t batch, int64_t rows, int64_t cols) {
   for (auto& o : p.off_p) o = take(batch * p.s_bytes);
   int64_t sums = 0;
   for (const Tiling& t : {p.gram, p.square}) {
-    const int64_t tiles = t.tile == 256 ? tri256 : tri128, bytes = (tiles - t.whole) * t.parts * t.tile * t.tile * 4;
+    const int64_t bytes = (tri(t.tile) - t.whole) * t.parts * t.tile * t.tile * 4;
     sums = bytes > sums ? bytes : sums;
   }
   p.off_sum = take(sums);
@@ -675,8 +695,10 @@ template <bool TR, int OUT>
 hipError_t run_gemm(const Gemm& g, int tile, int64_t wgs, hipStream_t s) {
   if (tile == 256)
     hipLaunchKernelGGL((k_ns_gemm<256, 256, 2, 4, TR, OUT>), dim3((unsigned)wgs), dim3(512), 0, s, g);
-  else
+  else if (tile == 128)
     hipLaunchKernelGGL((k_ns_gemm<128, 128, 2, 2, TR, OUT>), dim3((unsigned)wgs), dim3(256), 0, s, g);
+  else
+    hipLaunchKernelGGL((k_ns_gemm<64, 64, 2, 2, TR, OUT>), dim3((unsigned)wgs), dim3(256), 0, s, g);
   return hipGetLastError();
 }
 
@@ -726,6 +748,7 @@ hipError_t launch_orthogonalize(const float* grad, const float* momentum, float*
     if (err != hipSuccess || how.whole == tri) return err;
     const int64_t pieces = (tri - how.whole) * (how.tile / 32) * (how.tile / 32);
     if (how.tile == 256) hipLaunchKernelGGL(k_ns_finish<256>, dim3((unsigned)pieces), dim3(256), 0, s, g);
+    else if (how.tile == 64) hipLaunchKernelGGL(k_ns_finish<64>, dim3((unsigned)pieces), dim3(256), 0, s, g);
     else hipLaunchKernelGGL(k_ns_finish<128>, dim3((unsigned)pieces), dim3(256), 0, s, g);
     return hipGetLastError();
   };
