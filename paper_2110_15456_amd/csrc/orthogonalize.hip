@@ -131,16 +131,29 @@ __device__ __forceinline__ int xcd_order(int bid, int n) {
 // the four rows x 32 columns of two lane groups of a transposed read do.  Rows past
 // the end read zeros (the buffer resources end at the last row).
 //
-// A wave's tile is 128 x 64 (64 x 64 on the small tile): per slab 24 (16) KB of
-// fragments for 96 (48) MFMAs of 32x32x16, i.e. the LDS is busy half of the time
-// that the matrix cores are.
-template <int BM, int BN, int WGM, int WGN, bool TR, int OUT>
-__global__ __launch_bounds__(64 * WGM * WGN, BM == 64 ? 4 : 2) void k_ns_gemm(Gemm p) {
+// A wave's tile is 128 x 64, 64 x 64 or, on the 64 tile, 32 x 32: per slab 24 (16, 8)
+// KB of fragments for 48 (24, 6) MFMAs of 32x32x16, i.e. the LDS is busy a half (two
+// thirds, four thirds) of the time that the matrix cores are.
+//
+// ST stages: two, or four for few 64 tiles of few slabs, where the loads' latency is
+// what a slab takes (0.5 us) and nearly all of them can be on the way at once: the
+// update of 256 x 256 went from 135 to 126 us, of 384 x 1536 from 190 to 177; with 16
+// and more slabs, and on the 128 tile, it gained nothing.
+//
+// Large products are bound by power: the clock falls to 1.7 .. 1.85 GHz (of 2.4) with
+// the matrix cores busy 60 to 65 % of the cycles.  Q X of 4096 x 16384 takes 1.36 to
+// 1.47 ms, i.e. 1.12 to 1.21 PFLOP/s of FP16; a library's FP16 product of 8192^3
+// reached 1.15 on the same card.  Reading a slab's first fragments before the last one's
+// barrier changed nothing.
+template <int BM, int BN, int WGM, int WGN, bool TR, int OUT, int ST>
+__global__ __launch_bounds__(64 * WGM * WGN, BM == 64 && ST == 2 ? 4 : 2) void k_ns_gemm(Gemm p) {
   constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 32, TN = WN / 32;
   constexpr int OFF_B = BM * BLOCK, STAGE = OFF_B + BN * BLOCK;
   static_assert((BM / 8) % NW == 0 && (BN / 8) % NW == 0 && NW % 2 == 0, "loads split evenly over the waves");
   __shared__ __attribute__((aligned(128))) uint8_t stage0[STAGE];
   __shared__ __attribute__((aligned(128))) uint8_t stage1[STAGE];
+  __shared__ __attribute__((aligned(128))) uint8_t stage2[ST == 4 ? STAGE : 16];
+  __shared__ __attribute__((aligned(128))) uint8_t stage3[ST == 4 ? STAGE : 16];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int wr = wave / WGN, wc = wave % WGN;
 
@@ -223,12 +236,17 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 64 ? 4 : 2) void k_ns_gemm(Ge
     c = __builtin_amdgcn_mfma_f32_32x32x16_f16(b, a, c, 0, 0, 0);  // (B first: a lane's quads are columns of a row)
   };
   auto step = [&](const uint8_t* cur, uint8_t* nxt, int s) __attribute__((always_inline)) {
-    // this wave's loads of slab s have landed and its reads of slab s - 1 are done
-    __builtin_amdgcn_s_waitcnt(0);
+    // this wave's loads of slab s have landed (those of the ST - 2 after it may be on
+    // the way) and its reads of slab s - 1 are done
+    constexpr int YOUNGER = (ST - 2) * ((BM + BN) / 8 / NW);
+    if (ST > 2 && s + ST - 1 <= nslabs)
+      __builtin_amdgcn_s_waitcnt((YOUNGER & 15) | ((YOUNGER >> 4) << 14) | (7 << 4));  // vmcnt(YOUNGER) lgkmcnt(0)
+    else
+      __builtin_amdgcn_s_waitcnt(0);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (s + 1 < nslabs) issue(nxt, s + 1);
+    if (s + ST - 1 < nslabs) issue(nxt, s + ST - 1);
     static_for<2>([&](auto hc) __attribute__((always_inline)) {
       constexpr int h = decltype(hc)::value;
       h8 b[TN][2];
@@ -251,11 +269,25 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 64 ? 4 : 2) void k_ns_gemm(Ge
   };
   issue(stage0, 0);
   int s = 0;
-  for (; s + 2 <= nslabs; s += 2) {
-    step(stage0, stage1, s);
-    step(stage1, stage0, s + 1);
+  if constexpr (ST == 2) {
+    for (; s + 2 <= nslabs; s += 2) {
+      step(stage0, stage1, s);
+      step(stage1, stage0, s + 1);
+    }
+    if (s < nslabs) step(stage0, stage1, s);
+  } else {
+    if (nslabs > 1) issue(stage1, 1);
+    if (nslabs > 2) issue(stage2, 2);
+    for (; s + 4 <= nslabs; s += 4) {
+      step(stage0, stage3, s);
+      step(stage1, stage0, s + 1);
+      step(stage2, stage1, s + 2);
+      step(stage3, stage2, s + 3);
+    }
+    if (s < nslabs) step(stage0, stage3, s);
+    if (s + 1 < nslabs) step(stage1, stage0, s + 1);
+    if (s + 2 < nslabs) step(stage2, stage1, s + 2);
   }
-  if (s < nslabs) step(stage0, stage1, s);
 
   // Epilogue.  A lane holds columns 8 q + 4 fk .. + 3 of row fr of each 32 x 32
   // tile.  64 x 64 values at a time go through the wave's 16 KB of the stages, so
@@ -694,11 +726,13 @@ NsPlan ns_plan(int64_t batch, int64_t rows, int64_t cols) {
 template <bool TR, int OUT>
 hipError_t run_gemm(const Gemm& g, int tile, int64_t wgs, hipStream_t s) {
   if (tile == 256)
-    hipLaunchKernelGGL((k_ns_gemm<256, 256, 2, 4, TR, OUT>), dim3((unsigned)wgs), dim3(512), 0, s, g);
+    hipLaunchKernelGGL((k_ns_gemm<256, 256, 2, 4, TR, OUT, 2>), dim3((unsigned)wgs), dim3(512), 0, s, g);
   else if (tile == 128)
-    hipLaunchKernelGGL((k_ns_gemm<128, 128, 2, 2, TR, OUT>), dim3((unsigned)wgs), dim3(256), 0, s, g);
+    hipLaunchKernelGGL((k_ns_gemm<128, 128, 2, 2, TR, OUT, 2>), dim3((unsigned)wgs), dim3(256), 0, s, g);
+  else if (wgs <= 512 && (g.parts > 1 ? g.part_slabs : blocks_of(g.K)) <= 12)
+    hipLaunchKernelGGL((k_ns_gemm<64, 64, 2, 2, TR, OUT, 4>), dim3((unsigned)wgs), dim3(256), 0, s, g);
   else
-    hipLaunchKernelGGL((k_ns_gemm<64, 64, 2, 2, TR, OUT>), dim3((unsigned)wgs), dim3(256), 0, s, g);
+    hipLaunchKernelGGL((k_ns_gemm<64, 64, 2, 2, TR, OUT, 2>), dim3((unsigned)wgs), dim3(256), 0, s, g);
   return hipGetLastError();
 }
 
