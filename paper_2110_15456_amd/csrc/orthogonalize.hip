@@ -514,12 +514,19 @@ __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
   };
   uint8_t *S = mem[0], *P = mem[1];
   const float* sums = p.sums + (int64_t)blockIdx.x * p.parts * (128 * 128);
-  for (int q = tid; q < R * R / 4; q += NT) {
-    const int r = q / (R / 4), c = 4 * (q % (R / 4));
-    v4 v = {};
-#pragma unroll 8
-    for (int i = 0; i < p.parts; ++i) v += *reinterpret_cast<const v4*>(sums + (int64_t)i * (128 * 128) + r * 128 + c);
-    put4(S, r, c, v * ldexpf(1.0f, kSScale - 2 * kXScale));
+  constexpr int EACH = R * R / 4 / NT;
+  v4 sum[EACH] = {};
+#pragma unroll 4
+  for (int i = 0; i < p.parts; ++i)
+#pragma unroll
+    for (int u = 0; u < EACH; ++u) {
+      const int q = tid + u * NT, r = q / (R / 4), c = 4 * (q % (R / 4));
+      sum[u] += *reinterpret_cast<const v4*>(sums + (int64_t)i * (128 * 128) + r * 128 + c);
+    }
+#pragma unroll
+  for (int u = 0; u < EACH; ++u) {
+    const int q = tid + u * NT;
+    put4(S, q / (R / 4), 4 * (q % (R / 4)), sum[u] * ldexpf(1.0f, kSScale - 2 * kXScale));
   }
   __syncthreads();
   const float one = ldexpf(1.0f, -kPScale), sq = ldexpf(kC, kPScale - 2 * kSScale), li = ldexpf(kB, kPScale - kSScale);
@@ -590,18 +597,25 @@ __global__ __launch_bounds__(256) void k_ns_split(const float* __restrict__ g, c
   const int r0 = (int)(t / tiles_n) * T, c0 = (int)(t % tiles_n) * T;
   // the tile of U: rows of U are X's columns where it is transposed
   const int rows = FLIP ? k : n, cols = FLIP ? n : k, ur = FLIP ? c0 : r0, uc = FLIP ? r0 : c0;
+  // (every load before the first is waited for: values past the edge are read at it)
+  constexpr int EACH = T * T / 256;
+  const int ic = threadIdx.x % T, ir = threadIdx.x / T;
+  float gv[EACH], mv[EACH];
+  const int64_t from = base + min(uc + ic, cols - 1);
 #pragma unroll
-  for (int i = 0; i < T * T / 256; ++i) {
-    const int q = threadIdx.x + 256 * i, r = q / T, c = q % T;
-    float u = 0.0f;
-    if (ur + r < rows && uc + c < cols) {
-      const int64_t at = base + (int64_t)(ur + r) * cols + uc + c;
-      u = update_of(g[at], mode ? m_new[at] : 0.0f, beta, mode);
-    }
-    tile[r][c] = u;
+  for (int i = 0; i < EACH; ++i) gv[i] = g[from + (int64_t)min(ur + ir + 4 * i, rows - 1) * cols];
+  if (mode) {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) mv[i] = m_new[from + (int64_t)min(ur + ir + 4 * i, rows - 1) * cols];
+  } else {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) mv[i] = 0.0f;
   }
   double sum = 0.0;
   for (int i = threadIdx.x; i < blocks; i += 256) sum += part[matrix * blocks + i];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i)
+    tile[ir + 4 * i][ic] = ur + ir + 4 * i < rows && uc + ic < cols ? update_of(gv[i], mv[i], beta, mode) : 0.0f;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
