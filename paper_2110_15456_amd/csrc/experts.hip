@@ -193,7 +193,8 @@ hipError_t launch_expert_plan(const void* ids, bool ids64, int64_t slots, int ex
 // add nothing.  Every row of y is read once and every row of out written once:
 // bound by HBM.  A thread takes four columns of a token (V = 4), so that a wave
 // reads 1 KB of a row at a time; rows that are not 16-byte aligned go value by
-// value (V = 1).
+// value (V = 1).  8192 tokens of 4 slots, 4096 columns: 106 us, 5.8 TB/s (a copy of
+// 1 GB reaches 5.1); 16 tokens of 2: 2.9 us, a launch.
 namespace {
 
 template <int V> struct vec;
@@ -225,7 +226,8 @@ __global__ __launch_bounds__(256) void k_combine(const float* __restrict__ y, co
 // there are enough slots to fill the card, so that the slots of a token, which
 // follow one another, read its row of dout from the same L1; four otherwise.
 // The products are added lane by lane in the order of the columns, then over the
-// lanes and waves in a fixed tree.
+// lanes and waves in a fixed tree.  Bound by HBM: y read and dy written once, 211 us
+// or 5.5 TB/s for 8192 tokens of 4 slots and 4096 columns.
 template <int V, int WPS>
 __global__ __launch_bounds__(256) void k_combine_grad(const float* __restrict__ dout, const float* __restrict__ y,
                                                       const float* __restrict__ gates,

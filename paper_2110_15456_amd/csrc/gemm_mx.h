@@ -1551,8 +1551,8 @@ __global__ __launch_bounds__(CF::NT, CF::WAVES) void k_gemm_mx(const uint8_t* __
     if constexpr (SEG != kSegNone) {
       // Rows of any length and alignment, and the last columns: 16 rows at a time
       // through the stages, so that a store instruction writes 64 consecutive values
-      // of a row.  Value by value from the registers, 16 rows x 4 columns 4 apart, 5500
-      // x 777 values took 20 us more than x 768; now 5.
+      // of a row.  (Value by value from the registers, 16 rows x 4 columns 4 apart, the
+      // product of 5500 x 777 x 1056 took 67 us, not 63.)
       constexpr int SROW = CF::WN + 4;
       static_assert(CF::NW * 16 * SROW * 4 <= SB, "a strip per wave fits in one stage");
       __builtin_amdgcn_s_waitcnt(0);

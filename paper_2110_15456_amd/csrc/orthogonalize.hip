@@ -449,14 +449,14 @@ __global__ __launch_bounds__(256) void k_ns_finish(Gemm p) {
 // the place of an operand that it is the last to read: a launch for each product
 // takes 6.9 us at n = 64 where its 12 MFMAs a wave take 0.3.
 struct Chain {
-  const float* sums;  // [matrix][part][128][128]
+  const float* sums;  // [matrix][part][tile][tile], of 64 (NB <= 2) or 128
   int parts, n, pair;
   uint8_t* out;       // planes
   int64_t out_batch;
 };
 template <int NB>
 __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
-  constexpr int R = KS * NB, ROW = BLOCK * NB, NT = 64 * NB * NB;
+  constexpr int R = KS * NB, ROW = BLOCK * NB, NT = 64 * NB * NB, T = NB <= 2 ? 64 : 128;
   __shared__ __attribute__((aligned(128))) uint8_t mem[2][R * ROW];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int wr = wave / NB, wc = wave % NB, fr = lane & 31, fk = lane >> 5;
@@ -513,7 +513,7 @@ __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
     __syncthreads();
   };
   uint8_t *S = mem[0], *P = mem[1];
-  const float* sums = p.sums + (int64_t)blockIdx.x * p.parts * (128 * 128);
+  const float* sums = p.sums + (int64_t)blockIdx.x * p.parts * (T * T);
   constexpr int EACH = R * R / 4 / NT;
   v4 sum[EACH] = {};
 #pragma unroll 4
@@ -521,7 +521,7 @@ __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
 #pragma unroll
     for (int u = 0; u < EACH; ++u) {
       const int q = tid + u * NT, r = q / (R / 4), c = 4 * (q % (R / 4));
-      sum[u] += *reinterpret_cast<const v4*>(sums + (int64_t)i * (128 * 128) + r * 128 + c);
+      sum[u] += *reinterpret_cast<const v4*>(sums + (int64_t)i * (T * T) + r * T + c);
     }
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
@@ -711,7 +711,7 @@ NsPlan ns_plan(int64_t batch, int64_t rows, int64_t cols) {
   p.square = tiling({tri(256), tri(128), tri(64)}, blocks_of(p.n), true);
   if (p.n <= kChainMost) {  // one tile a matrix, its sums left to the chain
     const int64_t slabs = blocks_of(p.k), fill = 512 / batch, most = slabs / 4 < 16 ? slabs / 4 : 16;
-    p.gram = Tiling{128, (int)(fill < 1 || most < 1 ? 1 : fill < most ? fill : most), 0};
+    p.gram = Tiling{p.n <= 64 ? 64 : 128, (int)(fill < 1 || most < 1 ? 1 : fill < most ? fill : most), 0};
     p.square = Tiling{128, 1, tri(128)};
   }
   p.apply = tiling({count(256), count(128), count(64)}, blocks_of(p.n), false);
@@ -811,7 +811,7 @@ hipError_t launch_orthogonalize(const float* grad, const float* momentum, float*
       const int slabs = (int)blocks_of(k), ps = (slabs + p.gram.parts - 1) / p.gram.parts, parts = (slabs + ps - 1) / ps;
       e = run_gemm<false, kSym>(Gemm{X[at], p.x_bytes, X[at], p.x_bytes, n, n, k, 1, 1, 1.0f, nullptr, 0, (int)p.ld,
                                      nullptr, 0.0f, 0.0f, 0, parts, ps, sum},
-                                128, batch * parts, s);
+                                p.gram.tile, batch * parts, s);
       if (e != hipSuccess) return e;
       const Chain c{sum, parts, n, group == 2, poly[0], p.s_bytes};
       if (n <= 32) hipLaunchKernelGGL(k_ns_chain<1>, dim3((unsigned)batch), dim3(64), 0, s, c);

