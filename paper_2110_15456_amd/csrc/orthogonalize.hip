@@ -449,14 +449,14 @@ __global__ __launch_bounds__(256) void k_ns_finish(Gemm p) {
 // the place of an operand that it is the last to read: a launch for each product
 // takes 6.9 us at n = 64 where its 12 MFMAs a wave take 0.3.
 struct Chain {
-  const float* sums;  // [matrix][part][tile][tile], of 64 (NB <= 2) or 128
+  const float* sums;  // [matrix][tile of the lower triangle][part][64][64]
   int parts, n, pair;
   uint8_t* out;       // planes
   int64_t out_batch;
 };
 template <int NB>
 __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
-  constexpr int R = KS * NB, ROW = BLOCK * NB, NT = 64 * NB * NB, T = NB <= 2 ? 64 : 128;
+  constexpr int R = KS * NB, ROW = BLOCK * NB, NT = 64 * NB * NB, T = 64;
   __shared__ __attribute__((aligned(128))) uint8_t mem[2][R * ROW];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int wr = wave / NB, wc = wave % NB, fr = lane & 31, fk = lane >> 5;
@@ -513,20 +513,32 @@ __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
     __syncthreads();
   };
   uint8_t *S = mem[0], *P = mem[1];
-  const float* sums = p.sums + (int64_t)blockIdx.x * p.parts * (T * T);
-  constexpr int EACH = R * R / 4 / NT;
+  // the triangle's tiles, four values of a row at a time; those below the diagonal mirrored
+  constexpr int QUADS = (NB <= 2 ? 1 : 3) * T * T / 4, EACH = (QUADS + NT - 1) / NT;
+  const float* sums = p.sums + (int64_t)blockIdx.x * (QUADS * 4) * p.parts;
   v4 sum[EACH] = {};
 #pragma unroll 4
   for (int i = 0; i < p.parts; ++i)
 #pragma unroll
     for (int u = 0; u < EACH; ++u) {
-      const int q = tid + u * NT, r = q / (R / 4), c = 4 * (q % (R / 4));
-      sum[u] += *reinterpret_cast<const v4*>(sums + (int64_t)i * (T * T) + r * T + c);
+      const int q = min(tid + u * NT, QUADS - 1), t = q / (T * T / 4);
+      sum[u] += *reinterpret_cast<const v4*>(sums + ((int64_t)t * p.parts + i) * (T * T) + 4 * (q % (T * T / 4)));
     }
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
-    const int q = tid + u * NT;
-    put4(S, q / (R / 4), 4 * (q % (R / 4)), sum[u] * ldexpf(1.0f, kSScale - 2 * kXScale));
+    const int q = tid + u * NT, t = q / (T * T / 4), in = q % (T * T / 4);
+    const int r = in / (T / 4) + (t > 0 ? T : 0), c = 4 * (in % (T / 4)) + (t == 2 ? T : 0);
+    if (q >= QUADS || r >= R || c >= R) continue;
+    const v4 v = sum[u] * ldexpf(1.0f, kSScale - 2 * kXScale);
+    put4(S, r, c, v);
+    if (t != 1) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const _Float16 hi = (_Float16)v[j];
+      uint8_t* o = S + (r & 7) * 2;
+      *reinterpret_cast<_Float16*>(o + at(c + j, r / KS * 8 + (r % KS) / 8)) = hi;
+      *reinterpret_cast<_Float16*>(o + at(c + j, r / KS * 8 + (r % KS) / 8 + 4)) = (_Float16)(v[j] - (float)hi);
+    }
   }
   __syncthreads();
   const float one = ldexpf(1.0f, -kPScale), sq = ldexpf(kC, kPScale - 2 * kSScale), li = ldexpf(kB, kPScale - kSScale);
@@ -709,10 +721,10 @@ NsPlan ns_plan(int64_t batch, int64_t rows, int64_t cols) {
   auto tri = [&](int64_t t) { return batch * ((p.n + t - 1) / t) * ((p.n + t - 1) / t + 1) / 2; };
   p.gram = tiling({tri(256), tri(128), tri(64)}, blocks_of(p.k), true);
   p.square = tiling({tri(256), tri(128), tri(64)}, blocks_of(p.n), true);
-  if (p.n <= kChainMost) {  // one tile a matrix, its sums left to the chain
-    const int64_t slabs = blocks_of(p.k), fill = 512 / batch, most = slabs / 4 < 16 ? slabs / 4 : 16;
-    p.gram = Tiling{p.n <= 64 ? 64 : 128, (int)(fill < 1 || most < 1 ? 1 : fill < most ? fill : most), 0};
-    p.square = Tiling{128, 1, tri(128)};
+  if (p.n <= kChainMost) {  // tiles of 64, their sums left to the chain
+    const int64_t slabs = blocks_of(p.k), fill = 512 / tri(64), most = slabs / 4 < 16 ? slabs / 4 : 16;
+    p.gram = Tiling{64, (int)(fill < 1 || most < 1 ? 1 : fill < most ? fill : most), 0};
+    p.square = Tiling{64, 1, tri(64)};
   }
   p.apply = tiling({count(256), count(128), count(64)}, blocks_of(p.n), false);
   const int64_t per = (p.n * p.k + 4095) / 4096;
@@ -809,9 +821,10 @@ hipError_t launch_orthogonalize(const float* grad, const float* momentum, float*
     int q_scale = 0;
     if (n <= kChainMost) {
       const int slabs = (int)blocks_of(k), ps = (slabs + p.gram.parts - 1) / p.gram.parts, parts = (slabs + ps - 1) / ps;
-      e = run_gemm<false, kSym>(Gemm{X[at], p.x_bytes, X[at], p.x_bytes, n, n, k, 1, 1, 1.0f, nullptr, 0, (int)p.ld,
-                                     nullptr, 0.0f, 0.0f, 0, parts, ps, sum},
-                                p.gram.tile, batch * parts, s);
+      const int64_t t = (n + 63) / 64, tri = batch * t * (t + 1) / 2;
+      e = run_gemm<false, kSym>(Gemm{X[at], p.x_bytes, X[at], p.x_bytes, n, n, k, (int)t, (int)t, 1.0f, nullptr, 0,
+                                     (int)p.ld, nullptr, 0.0f, 0.0f, 0, parts, ps, sum},
+                                64, tri * parts, s);
       if (e != hipSuccess) return e;
       const Chain c{sum, parts, n, group == 2, poly[0], p.s_bytes};
       if (n <= 32) hipLaunchKernelGGL(k_ns_chain<1>, dim3((unsigned)batch), dim3(64), 0, s, c);
