@@ -3,7 +3,8 @@
  * FAST (Zhang, McDanel, Kung, "FAST: DNN Training Under Variable Precision
  * Block Floating Point with Stochastic Rounding", HPCA 2022).
  *
- * Two operations sit behind this boundary:
+ * Two operations sit behind this boundary, and what training and serving put
+ * around them (the expert layer's products, the orthogonalised update):
  *   bfp_quantize  FP32 -> BFP conversion (section III-A; converter of
  *                 section V-C): one shared exponent per group of g values,
  *                 sign-magnitude mantissas of m bits, nearest, stochastic or
@@ -689,7 +690,8 @@ int bfp_combine_experts_grad(const float* dout, const float* y, const float* gat
  *   side: X^T X where rows > cols), (a, b, c) = (3.4445, -4.7750, 2.0315)
  *   out = X
  * so that U's singular vectors stay and its singular values go to about 1 (five
- * steps: 0.7 to 1.2 for those above 0.3% of the norm).  A zero U gives zeros.
+ * steps: 0.7 to 1.2 for those above 0.3% of the norm).  A zero U gives zeros where
+ * eps > 0.
  *   grad, out    : FP32 [batch][rows][cols], contiguous, 4-byte aligned (16 for
  *                  full speed).  out must not overlap the other arrays.
  *   momentum     : the same, or NULL: U = grad and momentum_out is not written.

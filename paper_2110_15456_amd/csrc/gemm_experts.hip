@@ -67,9 +67,10 @@ hipError_t run_direct(const Operands& p, int rm, int kw, int each, float* C, int
 // What a product takes, in us, on the tiles there are.  The routing is device data,
 // so the tiles of rows are those that slots spread over all experts would have, each
 // expert's last one half full.  Fitted to graph replays of ten calls at 1 to 1024
-// slots an expert: 8 experts of 2048 x 2048 and 4096 x 4096, 64 of 1024 x 1024, 16 of
-// 576 x 1152; the kernel taken is within 15% of the fastest on most.  What decided,
-// us (few tokens on 16 and 32 rows, tiles of 128 x 128, large tiles):
+// slots an expert, 4 to 128 experts of 256 x 256 to 4096 x 4096: over 288 products of up
+// to 160 slots an expert the kernel taken is 3% slower than the fastest in the mean
+// and 43% at worst.  What decided, us (few tokens on 16 and 32 rows, tiles of 128 x 128,
+// large tiles):
 //   8 x 2048 x 2048 (4,4)    4 slots   7.2   9.0   18   32     (6,6)  12     -   31  37
 //                           24        11.4   9.6   19   31            18     -   31  37
 //                           64        22    22     19   32            40     -   34  38
@@ -111,12 +112,16 @@ Price price(const Operands& p, int experts, int64_t slots, int64_t K) {
   Price out{};
   const double s = (double)slots, slabs = (double)ceil_div(K / 16, mx::KG) * (K % 128 ? 1.15 : 1.0);
   price_tiles(p, tiles_of_rows(s, experts, 128), tiles_of_rows(s, experts, 256), slabs, out);
-  // the few-token kernels: the weights, once for every tile of rows, in bytes per us
-  const double bytes = (double)p.N * (double)K *
-                       ((p.nb == 1 ? (p.fb ? 4.0 : 6.0) : p.fb ? 10.0 : 12.0) / 8.0 + 1.0 / 16.0);
-  constexpr double rate = 5.0e6;
-  out.few[0] = 3.0 + tiles_of_rows(s, experts, 16) * bytes / rate;
-  out.few[1] = p.na == 1 ? 3.0 + tiles_of_rows(s, experts, 32) * bytes / (0.85 * rate) : 1e30;
+  // the few-token kernels: the weights, once for every tile of rows, and from the caches
+  // the rows, once for every 16 columns, at rates in bytes per us
+  auto bytes_of = [](int planes, bool narrow) {
+    return (planes == 1 ? (narrow ? 4.0 : 6.0) : narrow ? 10.0 : 12.0) / 8.0 + 1.0 / 16.0;
+  };
+  const double values = (double)p.N * (double)K;
+  const double weights = values * bytes_of(p.nb, p.fb), rows = s / 16.0 * values * bytes_of(p.na, p.fa);
+  constexpr double rate = 5.5e6, rows_rate = 8.3e6;
+  out.few[0] = 3.0 + tiles_of_rows(s, experts, 16) * weights / rate + rows / rows_rate;
+  out.few[1] = p.na == 1 ? 3.0 + 1.3 * (tiles_of_rows(s, experts, 32) * weights / rate + rows / rows_rate) : 1e30;
   return out;
 }
 
