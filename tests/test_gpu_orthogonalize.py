@@ -20,7 +20,7 @@ A, B, C = 3.4445, -4.7750, 2.0315
 
 
 def plain(u, steps=5, eps=1e-7):
-    """The iteration on one matrix, in its type, on the CPU."""
+    """The iteration on one matrix, in its type."""
     x = u / (u.norm() + eps)
     flip = x.shape[0] > x.shape[1]
     x = x.t() if flip else x
@@ -34,7 +34,7 @@ def check(out, u, steps=5):
     want = plain(u.double(), steps)
     low = plain(u.float(), steps).double()
     norm = float(want.norm())
-    assert float((out.cpu().double() - want).norm()) <= 4 * float((low - want).norm()) + 2.0 ** -22 * norm
+    assert float((out.to(want.device).double() - want).norm()) <= 4 * float((low - want).norm()) + 2.0 ** -22 * norm
     return want
 
 
@@ -58,6 +58,23 @@ def test_against_formula(rows, cols, kind):
     if kind == "noise" and min(rows, cols) * 4 <= max(rows, cols):  # (well away from zero singular values)
         s = torch.linalg.svdvals(want)
         assert 0.6 < float(s.min()) and float(s.max()) < 1.25
+
+
+@pytest.mark.parametrize("shape", [(40, 300, 500), (1, 2304, 6000), (1, 6000, 2304), (2, 2300, 5000), (1, 2050, 2050),
+                                   (1, 4100, 4200)])
+@pytest.mark.parametrize("kind", ["noise", "strong"])
+def test_large(shape, kind):
+    """Many tiles: whole rounds of them, parts of K, large tiles with ragged ends.
+    (The formula on the GPU, by torch's products of 64 and 32 bits.)"""
+    announce("orthogonalize %d x %d x %d, %s" % (*shape, kind))
+    g = torch.Generator(device="cuda").manual_seed(shape[1])
+    u = 1e-4 * torch.randn(shape, generator=g, device="cuda")
+    if kind == "strong":
+        u += 1e-2 * (torch.randn((*shape[:2], 2), generator=g, device="cuda") @
+                     torch.randn((shape[0], 2, shape[2]), generator=g, device="cuda"))
+    out = fb.orthogonalize(u)
+    for i in sorted({0, shape[0] // 2, shape[0] - 1}):
+        check(out[i], u[i])
 
 
 @pytest.mark.parametrize("steps", [1, 2, 3, 8])
