@@ -831,8 +831,8 @@ def orthogonal_update(grad: torch.Tensor, momentum: torch.Tensor, beta: float = 
                       steps: int = 5, eps: float = 1e-7, out: torch.Tensor | None = None,
                       momentum_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """A step of momentum and its orthogonalised direction: ``(update,
-    momentum_out)`` with momentum_out = beta * momentum + grad (momentum updates
-    it in place when passed) and update the orthogonalize of grad + beta *
+    momentum_out)`` with momentum_out = beta * momentum + grad (momentum itself
+    may be passed for it: in place) and update the orthogonalize of grad + beta *
     momentum_out (nesterov) or of momentum_out.  weight_update(w, update, -lr)
     takes it to the weights and their two BFP groupings."""
     _need_cuda(grad, "grad", torch.float32)
