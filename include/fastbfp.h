@@ -664,6 +664,8 @@ int bfp_gemm_experts_grad(const uint8_t* a_mant, const uint8_t* a_exp, int a_m_b
  * in FP32, in the order of j; dropped choices add nothing.
  *   y          : FP32 [tokens * top][N], in the experts' order; out FP32 [tokens][N].
  *   gates      : FP32 [tokens][top], or NULL for ones.
+ *   out must not overlap y, gates, place or offsets (BFP_E_ARG): rows of y are read
+ *   in the tokens' order, by workgroups that run in any.
  */
 int bfp_combine_experts(const float* y, const float* gates, const int32_t* place, const int32_t* offsets,
                         int64_t tokens, int top, int experts, int64_t N, float* out, void* stream);
@@ -673,7 +675,7 @@ int bfp_combine_experts(const float* y, const float* gates, const int32_t* place
  * top][n] and dgates[i] = sum over n of dout[i / top][n] y[place[i]][n] for every
  * slot i, zeros for dropped ones.
  *   dgates     : FP32 [tokens][top], or NULL.  gates as above.
- *   dy must not overlap y or dout.
+ *   dy and dgates must not overlap each other or what is read (BFP_E_ARG).
  */
 int bfp_combine_experts_grad(const float* dout, const float* y, const float* gates, const int32_t* place,
                              const int32_t* offsets, int64_t tokens, int top, int experts, int64_t N, float* dy,

@@ -743,7 +743,7 @@ def combine_experts(y: torch.Tensor, plan: ExpertPlan, gates: torch.Tensor | Non
     """The experts' outputs y [slots, N] (in their order) back at their tokens:
     FP32 [tokens, N], the sum over a token's choices of gates [tokens, top] (None:
     ones, e.g. for the gradient of the tokens) times the slot's row of y.  Dropped
-    choices add nothing."""
+    choices add nothing.  ``out`` must not overlap y: the rows change places."""
     N = _combine_args(y, plan, gates)
     o = out if out is not None else torch.empty((plan.tokens, N), dtype=torch.float32, device=y.device)
     _need_cuda(o, "out", torch.float32)

@@ -95,6 +95,19 @@ int check_routing(int64_t tokens, int64_t top, int experts) {
   return BFP_OK;
 }
 
+// Whether the `an` bytes at a and the `bn` bytes at b share any (null: nothing there).
+bool overlap(const void* a, uint64_t an, const void* b, uint64_t bn) {
+  const uint64_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+  return a && b && (p < q ? q - p < an && bn > 0 : p - q < bn && an > 0);
+}
+
+// Whether a weighted sum's output shares bytes with what its kernel reads.
+bool overlaps_combine_inputs(const void* o, uint64_t bytes, const float* y, const float* gates, const int32_t* place,
+                             const int32_t* offsets, uint64_t slots, int experts, uint64_t N) {
+  return overlap(o, bytes, y, slots * N * 4) || overlap(o, bytes, gates, slots * 4) ||
+         overlap(o, bytes, place, slots * 4) || overlap(o, bytes, offsets, (uint64_t)(experts + 1) * 4);
+}
+
 int check_combine(const float* y, const float* gates, const int32_t* place, const int32_t* offsets, int64_t tokens,
                   int top, int experts, int64_t N, const float* out) {
   const int st = check_routing(tokens, top, experts);
@@ -771,6 +784,9 @@ int bfp_combine_experts(const float* y, const float* gates, const int32_t* place
   const int st = check_combine(y, gates, place, offsets, tokens, top, experts, N, out);
   if (st != BFP_OK || tokens == 0 || N == 0) return st;
   if ((tokens * N + 255) / 256 > 0x7fffffff) return BFP_E_UNSUPPORTED;
+  if (overlaps_combine_inputs(out, (uint64_t)(tokens * N) * 4, y, gates, place, offsets, (uint64_t)tokens * top,
+                              experts, (uint64_t)N))
+    return BFP_E_ARG;
   return status_of(fastbfp::launch_combine_experts(y, gates, place, offsets, experts, tokens, top, N, out,
                                                    static_cast<hipStream_t>(stream)));
 }
@@ -781,13 +797,14 @@ int bfp_combine_experts_grad(const float* dout, const float* y, const float* gat
   const int st = check_combine(y, gates, place, offsets, tokens, top, experts, N, dy);
   if (st != BFP_OK || tokens == 0) return st;
   if (!aligned(dgates, 4)) return BFP_E_ARG;
-  if (N > 0) {
-    if (!dout || !aligned(dout, 4)) return BFP_E_ARG;
-    const uintptr_t bytes = (uintptr_t)tokens * (uintptr_t)N * 4, all = bytes * (uintptr_t)top;
-    const uintptr_t o = reinterpret_cast<uintptr_t>(dy), a = reinterpret_cast<uintptr_t>(y);
-    const uintptr_t d = reinterpret_cast<uintptr_t>(dout);
-    if ((a < o + all && o < a + all) || (d < o + all && o < d + bytes)) return BFP_E_ARG;  // dy overlaps y or dout
-  }
+  if (N > 0 && (!dout || !aligned(dout, 4))) return BFP_E_ARG;
+  const uint64_t slots = (uint64_t)tokens * top, n = (uint64_t)N, dout_bytes = (uint64_t)tokens * n * 4;
+  const uint64_t dy_bytes = slots * n * 4, dgates_bytes = slots * 4;
+  if (overlaps_combine_inputs(dy, dy_bytes, y, gates, place, offsets, slots, experts, n) ||
+      overlaps_combine_inputs(dgates, dgates_bytes, y, gates, place, offsets, slots, experts, n) ||
+      overlap(dy, dy_bytes, dout, dout_bytes) || overlap(dgates, dgates_bytes, dout, dout_bytes) ||
+      overlap(dy, dy_bytes, dgates, dgates_bytes))
+    return BFP_E_ARG;
   return status_of(fastbfp::launch_combine_experts_grad(dout, y, gates, place, offsets, experts, tokens, top, N, dy,
                                                         dgates, static_cast<hipStream_t>(stream)));
 }
