@@ -372,6 +372,16 @@ hipError_t launch_direct_t(int rm, int rn, const uint8_t* a_mant, const uint8_t*
 
 namespace direct {
 
+// Between a wave's writes to LDS and reads of them by its other lanes, and between
+// those and the next writes: neither may pass it.  (The LDS serves a wave in order,
+// so it emits no instruction; without it only the compiler's failure to tell the lanes'
+// addresses apart keeps the order.)
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // Sixteen rows of one plane in a pair of K supersteps (32 units: 384 bytes of a row
 // of FP6 codes, 256 of FP4 or Lo2), a wave's loads of 1 KB.  Chunk c = 64 i + lane (16
 // bytes) is part c % CPR of row c / CPR, so that neighbouring lanes read neighbouring
@@ -567,13 +577,16 @@ __global__ __launch_bounds__(64 * direct::kExpertWaves, 2) void k_gemm_direct_ex
         const bool same = p + 1 < p1;
         const int left = ng - (p * 32 + 4 * lb);
         // registers -> LDS -> fragments, sixteen rows at a time
+        wave_lds_order();
         ea.put(mine + OFF_AE, lane);
         eb.put(mine + OFF_BE, lane);
         Frag<NA, KA0, KA1> fa[2][RM];
 #pragma unroll
         for (int i = 0; i < RM; ++i) {
+          if (i > 0) wave_lds_order();
           a0[i].put(mine, lane);
           if constexpr (NA == 2) a1[i].put(mine + A0::BYTES, lane);
+          wave_lds_order();
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
             A0::get(mine, lane, s, fa[s][i].p0);
@@ -583,8 +596,10 @@ __global__ __launch_bounds__(64 * direct::kExpertWaves, 2) void k_gemm_direct_ex
         }
 #pragma unroll
         for (int jb = 0; jb < RN; ++jb) {
+          wave_lds_order();
           b0[jb].put(mine, lane);
           if constexpr (NB == 2) b1[jb].put(mine + B0::BYTES, lane);
+          wave_lds_order();
           if (jb + 1 == RN && (same || works(g + (int)gridDim.x))) load(same ? g : g + (int)gridDim.x, same ? p + 1 : p0);
           Frag<NB, KB0, KB1> fb[1];
 #pragma unroll
@@ -606,6 +621,7 @@ __global__ __launch_bounds__(64 * direct::kExpertWaves, 2) void k_gemm_direct_ex
     } else {
       // the sums of a tile's waves, added in their order, four columns per lane
       float* part = reinterpret_cast<float*>(mine);
+      wave_lds_order();
 #pragma unroll
       for (int i = 0; i < RM; ++i)
 #pragma unroll
