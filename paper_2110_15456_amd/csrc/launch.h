@@ -164,7 +164,8 @@ hipError_t launch_gemm_general(const uint8_t* a_mant, const uint8_t* a_exp, int 
 // j.  Places of the token grouping: the least multiple of 128 that every routing
 // of `slots` slots over `experts` experts fits.
 constexpr int kMaxExperts = 512;  // (the counts of a workgroup of the plan: 35 KB of LDS)
-constexpr int kPlanBlock = 4096;  // slots a workgroup of the plan takes
+constexpr int kPlanBlock = 4096;  // slots a workgroup of the plan takes in a round
+constexpr int kPlanMost = 256;    // its workgroups: one for each CU
 int64_t expert_places(int64_t slots, int experts);
 // int32 words of the plan's workspace (the counts of its workgroups; 0 for one).
 int64_t expert_plan_ws(int64_t slots, int experts);
