@@ -619,8 +619,10 @@ int bfp_expert_plan(const void* ids, int ids_bits, int64_t tokens, int top, int 
  *                gather = 0: the slots in the experts' order (rows = tokens *
  *                top).
  *   C          : a multiple of 16 (BFP_E_SHAPE otherwise), below 2^22.
- *   m_bits, round_mode, status_word : as bfp_quantize; seed_r and seed_c are the
- *                seeds of the two outputs, gid a group's index in its exp.
+ *   m_bits, round_mode : as bfp_quantize; seed_r and seed_c are the seeds of the
+ *                two outputs, gid a group's index in its exp.
+ *   status_word : as bfp_quantize, for the rows of slots with an expert: what rows
+ *                of dropped slots hold never sets it.
  * Outputs sized by bfp_quantized_sizes(tokens * top, C, 16, m_bits) and (C,
  * places, 16, m_bits).  tokens * top * C / 16 and C * places / 16 below 2^31
  * (BFP_E_UNSUPPORTED otherwise).

@@ -650,7 +650,8 @@ def quantize_experts(x: torch.Tensor, plan: ExpertPlan, gather: bool = False, m:
     gemm_experts_grad.
     ``gather``: x is [tokens, C] and slot i reads row i // top; otherwise x is
     [slots, C], in the experts' order already (what gemm_experts returns, or its
-    gradient).  C a multiple of 16."""
+    gradient).  C a multiple of 16.  ``status`` is set for infinities and NaN in
+    rows of slots that have an expert; dropped slots' rows may hold any."""
     _need_cuda(x, "x", torch.float32)
     if rounding not in ROUNDING:
         raise ValueError("rounding must be one of %s" % sorted(ROUNDING))

@@ -103,17 +103,21 @@ struct Divisor {
   }
 };
 
-// Rows taken from other places of x (GATHER of k_quantize_rows): row r is row
-// order[r] / top of x, whose rows hold `groups` groups.
-struct Gather {
+// Which rows k_quantize_rows takes: x's own; those of an expert layer's slots, row r
+// being row order[r] / top of x; or x's own as those slots, in the experts' order
+// already.  A row holds row_groups groups.  Slots from *kept on were dropped: their
+// rows are converted too, but say nothing about the input (status).
+enum { kRowsAll = 0, kRowsGathered = 1, kRowsSlots = 2 };
+struct SlotRows {
   const int32_t* order;
+  const int32_t* kept;
   Divisor top, groups;
   uint32_t row_groups;
   int rows;  // of x
 };
-struct NoGather {};
-template <bool GATHER> struct GatherArg { typedef NoGather type; };
-template <> struct GatherArg<true> { typedef Gather type; };
+struct AllRows {};
+template <int FROM> struct RowsArg { typedef SlotRows type; };
+template <> struct RowsArg<kRowsAll> { typedef AllRows type; };
 
 // Groups along the contiguous last axis: group gid covers x[gid*G, gid*G+G).
 // A lane owns GPL consecutive groups (two of 16 -- one 32-value packing unit
@@ -126,12 +130,12 @@ template <> struct GatherArg<true> { typedef Gather type; };
 // all 64 banks on the read-back.  (Reading 64 contiguous bytes per lane
 // straight from global memory instead leaves each load instruction touching
 // 64 scattered 16-byte pieces, which costs about a third of HBM bandwidth.)
-template <int G, int MODE, int NCH, bool ADAPT, int P0, int P1, bool GATHER = false>
+template <int G, int MODE, int NCH, bool ADAPT, int P0, int P1, int FROM = kRowsAll>
 __global__ __launch_bounds__(256) void k_quantize_rows(const float* __restrict__ x, int64_t ngroups, uint32_t m,
                                                        uint32_t key0, uint32_t key1, uint8_t* __restrict__ mant0,
                                                        uint8_t* __restrict__ mant1, uint8_t* __restrict__ exps,
                                                        uint32_t* status, double* part,
-                                                       typename GatherArg<GATHER>::type from) {
+                                                       typename RowsArg<FROM>::type from) {
   constexpr int GPL = G <= 16 ? 32 / G : 1;  // groups per lane: 32 values for g <= 16
   constexpr int CPG = G / 4;                         // 16-byte chunks per group
   constexpr int CPL = GPL * CPG;                     // 16-byte chunks per lane
@@ -151,7 +155,7 @@ __global__ __launch_bounds__(256) void k_quantize_rows(const float* __restrict__
     const int l = slot / CPL;
     const int c = (slot % CPL) ^ ((l / LANES_PER_SWZ) % CPL);
     // chunks of groups past the end reread the wave's last valid chunk (unused)
-    if constexpr (GATHER) {
+    if constexpr (FROM == kRowsGathered) {
       const int q = min(l * CPL + c, qmax_chunk);
       const uint32_t group = (uint32_t)g0 + (uint32_t)(q / CPG), row = from.groups.div(group);
       const int src = min(max((int)from.top.div((uint32_t)from.order[row]), 0), from.rows - 1);
@@ -184,6 +188,14 @@ __global__ __launch_bounds__(256) void k_quantize_rows(const float* __restrict__
   bool nonfinite;
   quantize_groups<G, GPL, MODE, NCH, ADAPT, P0, P1, true>(b, m, (uint64_t)gid, key0, key1, w, E, nonfinite, s_lo,
                                                           s_hi);
+  if constexpr (FROM != kRowsAll) {
+    if (status && nonfinite) {
+      const int64_t groups = (int64_t)*from.kept * from.row_groups;
+      nonfinite = false;
+#pragma unroll
+      for (int gi = 0; gi < GPL; ++gi) nonfinite |= E[gi] == 255u && gid + gi < groups;
+    }
+  }
   if (GPL > 1 && nmine == GPL) {
     // every group: one packing unit of 32 values (its bytes are the groups'
     // bytes side by side) and GPL exponent bytes
@@ -401,7 +413,7 @@ static hipError_t launch_rows_t(const float* x, int64_t ngroups, int m, uint64_t
   constexpr int GPL = G <= 16 ? 32 / G : 1;  // groups per lane (as in the kernel)
   const int64_t blocks = (ngroups + 256 * GPL - 1) / (256 * GPL);
   hipLaunchKernelGGL((k_quantize_rows<G, MODE, NCH, ADAPT, P0, P1>), dim3((unsigned)blocks), dim3(256), 0, s, x, ngroups,
-                     (uint32_t)m, (uint32_t)seed, (uint32_t)(seed >> 32), mant0, mant1, exps, status, part, NoGather{});
+                     (uint32_t)m, (uint32_t)seed, (uint32_t)(seed >> 32), mant0, mant1, exps, status, part, AllRows{});
   return hipGetLastError();
 }
 
@@ -843,12 +855,17 @@ static hipError_t launch_experts_t(const float* x, const ExpertSlots& sl, int64_
                                    uint64_t seed_r, uint64_t seed_c, uint8_t* mr, uint8_t* er, uint8_t* mc,
                                    uint8_t* ec, uint32_t* status, hipStream_t s) {
   const int64_t b0 = plane_group_bytes(16, m, 0), rgroups = (int64_t)sl.slots * (C / 16), cgroups = C * (klen / 16);
-  if (!mc) {  // the row grouping alone, gathered
-    const Gather from{sl.order, sl.top, Divisor((uint32_t)(C / 16)), (uint32_t)(C / 16), sl.rows};
-    const int64_t blocks = (rgroups + 511) / 512;  // (two groups per lane)
-    hipLaunchKernelGGL((k_quantize_rows<16, MODE, NCH, false, P0, P1, true>), dim3((unsigned)blocks), dim3(256), 0, s, x,
-                       rgroups, (uint32_t)m, (uint32_t)seed_r, (uint32_t)(seed_r >> 32), mr, mr + rgroups * b0, er,
-                       status, nullptr, from);
+  if (!mc) {  // the row grouping alone
+    const SlotRows from{sl.order, sl.offsets + sl.n, sl.top, Divisor((uint32_t)(C / 16)), (uint32_t)(C / 16), sl.rows};
+    const dim3 grid((unsigned)((rgroups + 511) / 512));  // (two groups per lane)
+    if (sl.gather)
+      hipLaunchKernelGGL((k_quantize_rows<16, MODE, NCH, false, P0, P1, kRowsGathered>), grid, dim3(256), 0, s, x,
+                         rgroups, (uint32_t)m, (uint32_t)seed_r, (uint32_t)(seed_r >> 32), mr, mr + rgroups * b0, er,
+                         status, nullptr, from);
+    else
+      hipLaunchKernelGGL((k_quantize_rows<16, MODE, NCH, false, P0, P1, kRowsSlots>), grid, dim3(256), 0, s, x,
+                         rgroups, (uint32_t)m, (uint32_t)seed_r, (uint32_t)(seed_r >> 32), mr, mr + rgroups * b0, er,
+                         status, nullptr, from);
     return hipGetLastError();
   }
   const int tiles_c = (int)((C + 63) / 64);
@@ -865,7 +882,8 @@ hipError_t launch_quantize_experts(const float* x, int64_t rows, int64_t C, int 
                                    int64_t klen, int m, int mode, uint64_t seed_r, uint64_t seed_c, uint8_t* mr,
                                    uint8_t* er, uint8_t* mc, uint8_t* ec, uint32_t* status, hipStream_t s) {
   if (slots == 0 || C == 0) return hipSuccess;
-  if (!mc && top == 0) return launch_quantize_rows(x, slots, C, 16, m, mode, seed_r, mr, er, status, s);
+  // (rows in order whose dropped ones nobody asks about are any rows)
+  if (!mc && top == 0 && !status) return launch_quantize_rows(x, slots, C, 16, m, mode, seed_r, mr, er, nullptr, s);
   const ExpertSlots sl{order, offsets, k_offsets, experts, (int)slots, (int)rows, Divisor((uint32_t)(top > 0 ? top : 1)),
                        top > 0};
 #define FASTBFP_EXPERTS(MODE)                                                                                          do {                                                                                                                   if (m <= 2) return launch_experts_t<MODE, 1, kPlaneFP4, kPlaneFP6>(x, sl, C, klen, m, seed_r, seed_c, mr, er, mc,                                                                        ec, status, s);                                   if (m <= 4) return launch_experts_t<MODE, 1, kPlaneFP6, kPlaneFP6>(x, sl, C, klen, m, seed_r, seed_c, mr, er, mc,                                                                        ec, status, s);                                   if (m <= 6) return launch_experts_t<MODE, 2, kPlaneFP6, kPlaneLo2>(x, sl, C, klen, m, seed_r, seed_c, mr, er, mc,                                                                        ec, status, s);                                   return launch_experts_t<MODE, 2, kPlaneFP6, kPlaneFP6>(x, sl, C, klen, m, seed_r, seed_c, mr, er, mc, ec, status,                                                            s);                                                         } while (0)

@@ -38,3 +38,52 @@ def test_plan_of_many_slots(slots, experts, dtype):
     place = np.empty_like(order)
     place[order] = np.arange(slots)
     assert np.array_equal(p.place.cpu().numpy(), place)
+
+
+# An odd number of groups in a row (a lane's two straddle rows), and rows that end with
+# a lane, a wave and a workgroup.
+@pytest.mark.parametrize("C", [16, 48, 1024, 8192])
+@pytest.mark.parametrize("m", [2, 4, 6, 8])
+def test_status_of_dropped_slots(C, m):
+    """What a dropped slot's row holds sets no status, whichever outputs are asked for;
+    what the row before it holds does."""
+    announce("status of dropped slots, C = %d, m = %d" % (C, m))
+    ids = torch.tensor([[1, -1], [0, 5], [-1, -1], [0, 1], [-1, 0]], device="cuda")  # 5 of 10 kept; token 2 has none
+    p = fb.expert_plan(ids, 2)
+    kept = 5
+    assert int(p.offsets[-1]) == kept
+    asked = [dict(), dict(cols=False), dict(rows=False)]
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def status(x, **kw):
+        st.zero_()
+        fb.quantize_experts(x, p, m=m, status=st, **kw)
+        return int(st.item())
+
+    x = torch.ones((10, C), device="cuda")
+    for at in (0, C - 1):
+        for value in (float("nan"), float("inf")):
+            poison = x.clone()
+            poison[kept:, at] = value
+            assert [status(poison, **kw) for kw in asked] == [0, 0, 0], (at, value)
+            poison[kept - 1, at] = value
+            assert [status(poison, **kw) for kw in asked] == [1, 1, 1], (at, value)
+            tokens = x[:5].clone()
+            tokens[2, at] = value
+            assert [status(tokens, gather=True, **kw) for kw in asked] == [0, 0, 0], (at, value)
+            tokens[4, at] = value
+            assert [status(tokens, gather=True, **kw) for kw in asked] == [1, 1, 1], (at, value)
+
+
+@pytest.mark.parametrize("gather", [True, False])
+def test_status_leaves_the_bytes(gather):
+    """Asking for the status changes no byte of what is written."""
+    announce("conversions with and without a status")
+    ids = torch.tensor([[1, -1], [0, 5], [-1, -1], [0, 1], [-1, 0]], device="cuda")
+    p = fb.expert_plan(ids, 2)
+    x = torch.randn((5 if gather else 10, 272), device="cuda")
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for m in (2, 4, 6, 8):
+        a, _ = fb.quantize_experts(x, p, gather=gather, m=m, cols=False)
+        b, _ = fb.quantize_experts(x, p, gather=gather, m=m, cols=False, status=st)
+        assert torch.equal(a.mant, b.mant) and torch.equal(a.exp, b.exp)
