@@ -734,7 +734,8 @@ def _combine_args(y, plan, gates):
         raise ValueError("y must be [%d, N]" % plan.slots)
     if gates is not None:
         _need_cuda(gates, "gates", torch.float32)
-        if gates.numel() != plan.slots:
+        # (a token's gates lie side by side: [top, tokens] holds as many in another order)
+        if gates.numel() != plan.slots or (gates.dim() > 1 and gates.shape[-1] != plan.top):
             raise ValueError("gates must be [%d, %d]" % (plan.tokens, plan.top))
     return y.shape[1]
 

@@ -87,3 +87,21 @@ def test_status_leaves_the_bytes(gather):
         a, _ = fb.quantize_experts(x, p, gather=gather, m=m, cols=False)
         b, _ = fb.quantize_experts(x, p, gather=gather, m=m, cols=False, status=st)
         assert torch.equal(a.mant, b.mant) and torch.equal(a.exp, b.exp)
+
+
+def test_gates_in_another_order():
+    """[top, tokens] holds as many gates as [tokens, top], in another order."""
+    announce("gates of a wrong shape are refused")
+    p = fb.expert_plan(torch.tensor([[0, 1], [1, 2], [2, 0]], device="cuda"), 3)
+    y, dout = torch.randn((6, 16), device="cuda"), torch.randn((3, 16), device="cuda")
+    gates = torch.rand((3, 2), device="cuda")
+    want = fb.combine_experts(y, p, gates)
+    assert torch.equal(fb.combine_experts(y, p, gates.reshape(-1)), want)  # the slots in order
+    for bad in (gates.t().contiguous(), gates.reshape(6, 1), gates.reshape(1, 6), gates[:2].contiguous()):
+        with pytest.raises(ValueError):
+            fb.combine_experts(y, p, bad)
+        with pytest.raises(ValueError):
+            fb.combine_experts_grad(dout, y, p, bad)
+    one = fb.expert_plan(torch.tensor([0, 2, 1, 1, 0, 2], device="cuda"), 3)  # one choice each
+    g = gates.reshape(6)
+    assert torch.equal(fb.combine_experts(y, one, g), fb.combine_experts(y, one, g[:, None].contiguous()))
