@@ -266,9 +266,12 @@ __global__ __launch_bounds__(256) void k_combine(const float* __restrict__ y, co
 // y[place[slot]]; zeros for dropped slots.  WPS waves take a slot: one where
 // there are enough slots to fill the card, so that the slots of a token, which
 // follow one another, read its row of dout from the same L1; four otherwise.
-// The products are added lane by lane in the order of the columns, then over the
-// lanes and waves in a fixed tree.  Bound by HBM: y read and dy written once, 211 us
-// or 5.5 TB/s for 8192 tokens of 4 slots and 4096 columns.
+// Four products at a time are added in FP32 and those sums in 64 bits (lane by lane in
+// the order of the columns, then over the lanes and waves in a fixed tree), rounded
+// once.  (A chain of N / 64 FP32 sums a lane, which this replaces, was as fast and the
+// largest part of the error; 64 bits from the products on took 4% longer.)  Bound by
+// HBM: y read and dy written once, 211 us or 5.5 TB/s for 8192 tokens of 4 slots and
+// 4096 columns.
 template <int V, int WPS>
 __global__ __launch_bounds__(256) void k_combine_grad(const float* __restrict__ dout, const float* __restrict__ y,
                                                       const float* __restrict__ gates,
@@ -277,11 +280,11 @@ __global__ __launch_bounds__(256) void k_combine_grad(const float* __restrict__ 
                                                       int64_t N, int64_t slots, float* __restrict__ dy,
                                                       float* __restrict__ dgates) {
   typedef typename vec<V>::type v_t;
-  __shared__ float part[4];
+  __shared__ double part[4];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t slot = (int64_t)blockIdx.x * (4 / WPS) + wave / WPS;
   const bool live = slot < slots;
-  float dot = 0.0f;
+  double dot = 0.0;
   if (live) {
     const int p = place[slot], kept = min(max(offsets[experts], 0), (int)slots);
     const bool in = p >= 0 && p < kept;
@@ -296,8 +299,10 @@ __global__ __launch_bounds__(256) void k_combine_grad(const float* __restrict__ 
           const v_t a = *reinterpret_cast<const v_t*>(d + c);
           const v_t b = __builtin_nontemporal_load(reinterpret_cast<const v_t*>(src + c));
           r = g * a;
+          float sum = a[0] * b[0];
 #pragma unroll
-          for (int k = 0; k < V; ++k) dot = __builtin_fmaf(a[k], b[k], dot);
+          for (int k = 1; k < V; ++k) sum = __builtin_fmaf(a[k], b[k], sum);
+          dot += (double)sum;
         }
         __builtin_nontemporal_store(r, reinterpret_cast<v_t*>(dst + c));
       }
@@ -310,7 +315,7 @@ __global__ __launch_bounds__(256) void k_combine_grad(const float* __restrict__ 
     __syncthreads();
     dot = (part[0] + part[1]) + (part[2] + part[3]);
   }
-  if (live && dgates && lane == 0 && wave % WPS == 0) dgates[slot] = dot;
+  if (live && dgates && lane == 0 && wave % WPS == 0) dgates[slot] = (float)dot;
 }
 
 bool rows_aligned(int64_t N, const void* a, const void* b, const void* c) {

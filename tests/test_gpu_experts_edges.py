@@ -105,3 +105,35 @@ def test_gates_in_another_order():
     one = fb.expert_plan(torch.tensor([0, 2, 1, 1, 0, 2], device="cuda"), 3)  # one choice each
     g = gates.reshape(6)
     assert torch.equal(fb.combine_experts(y, one, g), fb.combine_experts(y, one, g[:, None].contiguous()))
+
+
+def losing_terms(n):
+    """n values near 1 of which every sum in order loses nearly half a unit in its last
+    place, so that n FP32 sums in a row are off by about 0.35 n 2^-24 of the result."""
+    out, s = np.empty(n, np.float32), np.float32(0)
+    for i in range(n):
+        out[i] = np.float32(1.0 + 0.49 * np.spacing(s)) if s >= 2 else np.float32(1)
+        s = np.float32(s + out[i])
+    return out
+
+
+# Slots that take four waves each, and one: the columns from one of a lane's to its next.
+@pytest.mark.parametrize("tokens,top,N,stride", [(1, 1, 262144, 1024), (3, 2, 262144, 1024), (4099, 1, 4096, 256),
+                                                 (2100, 2, 4095, 64)])
+def test_gate_gradients_of_long_rows(tokens, top, N, stride):
+    """dgates at most 5 2^-24 of the terms' absolute sum off, whatever N is: four
+    products and their sums in FP32, 2^-24 each; the rounding of the result; and sums
+    in 64 bits, N 2^-53.  The terms lose all they can in one FP32 sum a lane."""
+    announce("gate gradients, %d x %d, N = %d" % (tokens, top, N))
+    c = np.arange(N)
+    v = 4 if N % 4 == 0 else 1
+    row = losing_terms(N // stride * v + v)[c // stride * v + c % v]
+    rng = np.random.Generator(np.random.PCG64(N))
+    ids = np.argsort(rng.random((tokens, 5)), axis=1)[:, :top]
+    p = fb.expert_plan(torch.from_numpy(ids).cuda(), 5)
+    scale = np.ldexp(1.0, rng.integers(-3, 4, tokens * top)).astype(np.float32)  # (exact; tells the slots apart)
+    y = torch.from_numpy(row).cuda()[None] * torch.from_numpy(scale).cuda()[:, None]
+    _, dg = fb.combine_experts_grad(torch.ones((tokens, N), device="cuda"), y, p)
+    want = row.astype(np.float64).sum() * scale[p.place.cpu().numpy()].reshape(tokens, top)
+    err = np.abs(dg.cpu().numpy() - want) / want
+    assert np.all(err <= 5 * 2.0 ** -24 + N * 2.0 ** -53), err.max() * 2 ** 24
