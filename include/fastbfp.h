@@ -702,6 +702,7 @@ int bfp_combine_experts_grad(const float* dout, const float* y, const float* gat
  *   momentum_out : may be momentum (in place).
  *   steps        : 1 .. 16;  eps >= 0.
  *   workspace    : bfp_orthogonalize_ws_size bytes, 256-byte aligned; overwritten.
+ *                  Must not overlap the arrays.
  * Norms are summed in 64 bits.  The products are computed to about FP32's accuracy
  * (operands in two FP16 planes, 22 bits; FP32 sums) in an order that depends on
  * the sizes alone.  rows and cols below 2^20 and rows * cols up to 2^29

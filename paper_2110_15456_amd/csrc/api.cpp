@@ -837,6 +837,9 @@ int bfp_orthogonalize(const float* grad, const float* momentum, float* momentum_
   if (momentum && (!apart(out, momentum_out) || !apart(grad, momentum_out) ||
                    (momentum != momentum_out && !apart(momentum, momentum_out))))
     return BFP_E_ARG;
+  for (const void* a : {static_cast<const void*>(grad), static_cast<const void*>(momentum),
+                        static_cast<const void*>(momentum ? momentum_out : nullptr), static_cast<const void*>(out)})
+    if (overlap(workspace, need, a, bytes)) return BFP_E_ARG;
   return status_of(fastbfp::launch_orthogonalize(grad, momentum, momentum ? momentum_out : nullptr, beta,
                                                  nesterov != 0, batch, rows, cols, steps, eps, out,
                                                  static_cast<uint8_t*>(workspace), static_cast<hipStream_t>(stream)));

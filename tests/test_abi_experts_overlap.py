@@ -52,3 +52,18 @@ def test_gradients(lib, written, read):
         p[written] = ctypes.c_void_p(at)
         assert lib.bfp_combine_experts_grad(p["dout"], p["y"], p["gates"], p["place"], p["offsets"], TOKENS, TOP,
                                             EXPERTS, N, p["dy"], p["dgates"], None) == E_ARG, hex(at)
+
+
+@pytest.mark.parametrize("over", ["grad", "momentum", "momentum_out", "out"])
+def test_workspace_of_the_update(lib, over):
+    """The update's workspace is overwritten: not over what it reads or writes."""
+    batch, rows, cols = 2, 64, 128
+    need = ctypes.c_size_t(0)
+    assert lib.bfp_orthogonalize_ws_size(batch, rows, cols, ctypes.byref(need)) == 0
+    size = batch * rows * cols * 4  # (a multiple of 256, as the workspace's places are)
+    at = dict(grad=0x10000000, momentum=0x20000000, momentum_out=0x30000000, out=0x40000000)
+    p = {k: ctypes.c_void_p(v) for k, v in at.items()}
+    assert need.value % 256 == 0
+    for ws in (at[over], at[over] + size - 256, at[over] - need.value + 256):
+        assert lib.bfp_orthogonalize(p["grad"], p["momentum"], p["momentum_out"], 0.9, 1, batch, rows, cols, 5, 1e-7,
+                                     p["out"], ctypes.c_void_p(ws), need, None) == E_ARG, hex(ws)
