@@ -76,7 +76,7 @@
 extern "C" {
 #endif
 
-#define FASTBFP_ABI_VERSION 8
+#define FASTBFP_ABI_VERSION 9
 
 typedef enum {
   BFP_ROUND_NEAREST = 0,    /* add half an LSB, then truncate (ties away from zero) */
@@ -660,6 +660,20 @@ int bfp_gemm_experts(const uint8_t* a_mant, const uint8_t* a_exp, int a_m_bits, 
 int bfp_gemm_experts_grad(const uint8_t* a_mant, const uint8_t* a_exp, int a_m_bits, const uint8_t* b_mant,
                           const uint8_t* b_exp, int b_m_bits, const int32_t* k_offsets, int experts, int64_t M,
                           int64_t N, int64_t places, int m_a, int m_b, float* C, void* stream);
+
+/*
+ * bfp_gemm_experts_route, bfp_gemm_experts_grad_route -- which kernel the product
+ * runs on.  Host only, nothing is launched.
+ *   rows  : 16 or 32: the few-token kernel, on tiles of so many slots; 128: the
+ *           tiled kernel on tiles of 128 x 128; 0: on the operand formats' large
+ *           tile.
+ *   waves : waves that split K for a tile of the few-token kernel, else 0.
+ * BFP_E_ARG also where there is nothing to write.  For tests and tuning.
+ */
+int bfp_gemm_experts_route(int a_m_bits, int b_m_bits, int experts, int64_t slots, int64_t N, int64_t K, int m_a,
+                           int m_b, int* rows, int* waves);
+int bfp_gemm_experts_grad_route(int a_m_bits, int b_m_bits, int experts, int64_t M, int64_t N, int64_t places, int m_a,
+                                int m_b, int* rows);
 
 /*
  * bfp_combine_experts -- out[t][n] = sum over j of gates[t][j] y[place[t top + j]][n]

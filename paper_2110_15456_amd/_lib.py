@@ -59,6 +59,8 @@ SIGNATURES = {
     "bfp_quantize_experts": (_I, [_P, _I64, _I, _P, _P, _P, _I64, _I, _I, _I, _I, _U64, _U64, _P, _P, _P, _P, _P, _P]),
     "bfp_gemm_experts": (_I, [_P, _P, _I, _P, _P, _I, _P, _I, _I64, _I64, _I64, _I, _I, _P, _I64, _P]),
     "bfp_gemm_experts_grad": (_I, [_P, _P, _I, _P, _P, _I, _P, _I, _I64, _I64, _I64, _I, _I, _P, _P]),
+    "bfp_gemm_experts_route": (_I, [_I, _I, _I, _I64, _I64, _I64, _I, _I] + [ctypes.POINTER(ctypes.c_int)] * 2),
+    "bfp_gemm_experts_grad_route": (_I, [_I, _I, _I, _I64, _I64, _I64, _I, _I, ctypes.POINTER(ctypes.c_int)]),
     "bfp_combine_experts": (_I, [_P, _P, _P, _P, _I64, _I, _I, _I64, _P, _P]),
     "bfp_combine_experts_grad": (_I, [_P, _P, _P, _P, _P, _I64, _I, _I, _I64, _P, _P, _P]),
     "bfp_orthogonalize_ws_size": (_I, [_I64, _I64, _I64, ctypes.POINTER(ctypes.c_size_t)]),
@@ -66,7 +68,7 @@ SIGNATURES = {
                                ctypes.c_size_t, _P]),
     "bfp_adaptive_mantissa": (_I, [ctypes.c_double, ctypes.c_double, ctypes.c_double]),
 }
-ABI_VERSION = 8
+ABI_VERSION = 9
 
 _lock = threading.Lock()
 _lib = None

@@ -95,6 +95,29 @@ int check_routing(int64_t tokens, int64_t top, int experts) {
   return BFP_OK;
 }
 
+// The products of experts: shapes, formats and grids.
+int check_experts_shape(int a_m, int b_m, int experts, int64_t slots, int64_t N, int64_t K, int m_a, int m_b) {
+  int st = check_routing(slots, 1, experts);
+  if (st != BFP_OK) return st;
+  st = check_gemm_shape(a_m, b_m, slots, N, K, 16, m_a, m_b);
+  if (st != BFP_OK) return st;
+  if (!fast_path(a_m, b_m, 16, m_a, m_b)) return BFP_E_UNSUPPORTED;
+  // (one tile more for each expert than rows fill)
+  if ((slots / 128 + experts + 1) * ((N + 63) / 64) > 0x7fffffff) return BFP_E_UNSUPPORTED;
+  return BFP_OK;
+}
+
+int check_experts_grad_shape(int a_m, int b_m, int experts, int64_t M, int64_t N, int64_t places, int m_a, int m_b) {
+  int st = check_routing(0, 1, experts);
+  if (st != BFP_OK) return st;
+  st = check_gemm_shape(a_m, b_m, M, N, places, 16, m_a, m_b);
+  if (st != BFP_OK) return st;
+  if (places % 128 != 0) return BFP_E_SHAPE;
+  if (!fast_path(a_m, b_m, 16, m_a, m_b)) return BFP_E_UNSUPPORTED;
+  if (((M + 127) / 128) * ((N + 63) / 64) > 0x7fffffff / experts) return BFP_E_UNSUPPORTED;
+  return BFP_OK;
+}
+
 // Whether the `an` bytes at a and the `bn` bytes at b share any (null: nothing there).
 bool overlap(const void* a, uint64_t an, const void* b, uint64_t bn) {
   const uint64_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
@@ -742,6 +765,28 @@ int bfp_quantize_experts(const float* x, int64_t C, int gather, const int32_t* o
                                                     static_cast<hipStream_t>(stream)));
 }
 
+int bfp_gemm_experts_route(int a_m_bits, int b_m_bits, int experts, int64_t slots, int64_t N, int64_t K, int m_a,
+                           int m_b, int* rows, int* waves) {
+  const int st = check_experts_shape(a_m_bits, b_m_bits, experts, slots, N, K, m_a, m_b);
+  if (st != BFP_OK) return st;
+  if (!rows || !waves || slots == 0 || N == 0) return BFP_E_ARG;
+  const fastbfp::ExpertsRoute r = fastbfp::experts_route(a_m_bits, planes_used(a_m_bits, m_a), b_m_bits,
+                                                         planes_used(b_m_bits, m_b), experts, slots, N, K);
+  *rows = r.rows;
+  *waves = r.waves;
+  return BFP_OK;
+}
+
+int bfp_gemm_experts_grad_route(int a_m_bits, int b_m_bits, int experts, int64_t M, int64_t N, int64_t places, int m_a,
+                                int m_b, int* rows) {
+  const int st = check_experts_grad_shape(a_m_bits, b_m_bits, experts, M, N, places, m_a, m_b);
+  if (st != BFP_OK) return st;
+  if (!rows || M == 0 || N == 0) return BFP_E_ARG;
+  *rows = fastbfp::experts_grad_route(a_m_bits, planes_used(a_m_bits, m_a), b_m_bits, planes_used(b_m_bits, m_b),
+                                      experts, M, N, places).rows;
+  return BFP_OK;
+}
+
 int bfp_gemm_experts(const uint8_t* a_mant, const uint8_t* a_exp, int a_m_bits, const uint8_t* b_mant,
                      const uint8_t* b_exp, int b_m_bits, const int32_t* offsets, int experts, int64_t slots, int64_t N,
                      int64_t K, int m_a, int m_b, float* C, int64_t ldc, void* stream) {
@@ -749,9 +794,8 @@ int bfp_gemm_experts(const uint8_t* a_mant, const uint8_t* a_exp, int a_m_bits, 
   if (st != BFP_OK) return st;
   st = check_gemm(a_mant, a_m_bits, b_mant, b_m_bits, slots, N, K, 16, m_a, m_b);
   if (st != BFP_OK) return st;
-  if (!fast_path(a_m_bits, b_m_bits, 16, m_a, m_b)) return BFP_E_UNSUPPORTED;
-  // (one tile more for each expert than rows fill)
-  if ((slots / 128 + experts + 1) * ((N + 63) / 64) > 0x7fffffff) return BFP_E_UNSUPPORTED;
+  st = check_experts_shape(a_m_bits, b_m_bits, experts, slots, N, K, m_a, m_b);
+  if (st != BFP_OK) return st;
   if (ldc < N) return BFP_E_SHAPE;
   if (slots == 0 || N == 0) return BFP_OK;
   if (!C || !aligned(C, 4) || !offsets || !aligned(offsets, 4) || (K > 0 && (!a_exp || !b_exp))) return BFP_E_ARG;
@@ -767,9 +811,8 @@ int bfp_gemm_experts_grad(const uint8_t* a_mant, const uint8_t* a_exp, int a_m_b
   if (st != BFP_OK) return st;
   st = check_gemm(a_mant, a_m_bits, b_mant, b_m_bits, M, N, places, 16, m_a, m_b);
   if (st != BFP_OK) return st;
-  if (places % 128 != 0) return BFP_E_SHAPE;
-  if (!fast_path(a_m_bits, b_m_bits, 16, m_a, m_b)) return BFP_E_UNSUPPORTED;
-  if (((M + 127) / 128) * ((N + 63) / 64) > 0x7fffffff / experts) return BFP_E_UNSUPPORTED;
+  st = check_experts_grad_shape(a_m_bits, b_m_bits, experts, M, N, places, m_a, m_b);
+  if (st != BFP_OK) return st;
   if (M == 0 || N == 0) return BFP_OK;
   if (!C || !aligned(C, 4) || !k_offsets || !aligned(k_offsets, 4)) return BFP_E_ARG;
   if (places > 0 && (!a_exp || !b_exp)) return BFP_E_ARG;

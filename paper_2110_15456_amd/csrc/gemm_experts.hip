@@ -125,46 +125,70 @@ Price price(const Operands& p, int experts, int64_t slots, int64_t K) {
   return out;
 }
 
+Operands operands(const uint8_t* a_mant, const uint8_t* a_exp, int a_m, int na, const uint8_t* b_mant,
+                  const uint8_t* b_exp, int b_m, int nb, int64_t a_rows, int64_t b_rows, int64_t M, int64_t N, int64_t K,
+                  int scale_log2) {
+  return Operands{a_mant, a_exp, a_rows * (K / 16) * plane_group_bytes(16, a_m, 0), b_mant, b_exp,
+                  b_rows * (K / 16) * plane_group_bytes(16, b_m, 0), (int)M, (int)N, (int)(K / 16), na, nb,
+                  fmt_flag(a_m, na), fmt_flag(b_m, nb), ldexpf(1.0f, scale_log2)};
+}
+
+ExpertsRoute route_rows(const Operands& p, int experts, int64_t slots, int64_t K) {
+  const Segments seg{nullptr, experts, (int)slots};
+  const Price us = price(p, experts, slots, K);
+  const double tiled = us.small < us.big ? us.small : us.big;
+  for (int rm = 1; rm <= 2; ++rm) {
+    const int64_t rows = most_segment_tiles(seg, 16 * rm);
+    if (us.few[rm - 1] > tiled || us.few[rm - 1] > us.few[2 - rm] || rows > direct::kMaxRowTiles) continue;
+    const int64_t cols = ceil_div(p.N, direct_experts_cols(p.na, p.nb, rm)), pairs = ceil_div(K / 16, 32);
+    // waves for a tile: until every CU has eight
+    int kw = 1;
+    while (kw < direct::kExpertWaves && rows * cols * kw < 2048 && 2 * kw <= pairs) kw *= 2;
+    const int64_t each = rows * cols * kw / (512 * direct::kExpertWaves);
+    return ExpertsRoute{16 * rm, kw, each < 1 ? 1 : each > 4 ? 4 : (int)each};
+  }
+  return ExpertsRoute{us.small <= us.big ? 128 : 0, 0, 0};
+}
+
+ExpertsRoute route_grad(const Operands& p, int experts, int64_t M, int64_t klen) {
+  // (the tiles of every expert, at the mean length of K)
+  Price us{};
+  price_tiles(p, (double)(experts * ceil_div(M, 128)), (double)(experts * ceil_div(M, 256)),
+              (double)klen / 128.0 / experts, us);
+  return ExpertsRoute{us.small <= us.big ? 128 : 0, 0, 0};
+}
+
 }  // namespace
+
+ExpertsRoute experts_route(int a_m, int na, int b_m, int nb, int experts, int64_t slots, int64_t N, int64_t K) {
+  return route_rows(operands(nullptr, nullptr, a_m, na, nullptr, nullptr, b_m, nb, slots, experts * N, slots, N, K, 0),
+                    experts, slots, K);
+}
+
+ExpertsRoute experts_grad_route(int a_m, int na, int b_m, int nb, int experts, int64_t M, int64_t N, int64_t klen) {
+  return route_grad(operands(nullptr, nullptr, a_m, na, nullptr, nullptr, b_m, nb, M, N, M, N, klen, 0), experts, M,
+                    klen);
+}
 
 hipError_t launch_gemm_experts(const uint8_t* a_mant, const uint8_t* a_exp, int a_m, int na, const uint8_t* b_mant,
                                const uint8_t* b_exp, int b_m, int nb, const int32_t* offsets, int experts,
                                int64_t slots, int64_t N, int64_t K, int scale_log2, float* C, int64_t ldc,
                                hipStream_t s) {
   if (slots == 0 || N == 0) return hipSuccess;
-  const Operands p{a_mant, a_exp, slots * (K / 16) * plane_group_bytes(16, a_m, 0), b_mant, b_exp,
-                   experts * N * (K / 16) * plane_group_bytes(16, b_m, 0), (int)slots, (int)N, (int)(K / 16), na, nb,
-                   fmt_flag(a_m, na), fmt_flag(b_m, nb), ldexpf(1.0f, scale_log2)};
+  const Operands p = operands(a_mant, a_exp, a_m, na, b_mant, b_exp, b_m, nb, slots, experts * N, slots, N, K, scale_log2);
   const Segments seg{offsets, experts, (int)slots};
-  const Price us = price(p, experts, slots, K);
-  const double tiled = us.small < us.big ? us.small : us.big;
-  for (int rm = 1; rm <= 2; ++rm) {
-    const int64_t rows = most_segment_tiles(seg, 16 * rm);
-    if (us.few[rm - 1] > tiled || us.few[rm - 1] > us.few[2 - rm] || rows > direct::kMaxRowTiles) continue;
-    const int wide = direct_experts_cols(na, nb, rm);
-    const int64_t cols = ceil_div(N, wide), pairs = ceil_div(K / 16, 32);
-    // waves for a tile: until every CU has eight
-    int kw = 1;
-    while (kw < direct::kExpertWaves && rows * cols * kw < 2048 && 2 * kw <= pairs) kw *= 2;
-    const int64_t each = rows * cols * kw / (512 * direct::kExpertWaves);
-    return run_direct(p, rm, kw, each < 1 ? 1 : each > 4 ? 4 : (int)each, C, ldc, seg, s);
-  }
-  return run_tiled(p, us.small <= us.big, false, C, ldc, seg, s);
+  const ExpertsRoute r = route_rows(p, experts, slots, K);
+  if (r.waves > 0) return run_direct(p, r.rows / 16, r.waves, r.each, C, ldc, seg, s);
+  return run_tiled(p, r.rows == 128, false, C, ldc, seg, s);
 }
 
 hipError_t launch_gemm_experts_grad(const uint8_t* a_mant, const uint8_t* a_exp, int a_m, int na, const uint8_t* b_mant,
                                     const uint8_t* b_exp, int b_m, int nb, const int32_t* k_offsets, int experts,
                                     int64_t M, int64_t N, int64_t klen, int scale_log2, float* C, hipStream_t s) {
   if (M == 0 || N == 0) return hipSuccess;
-  const Operands p{a_mant, a_exp, M * (klen / 16) * plane_group_bytes(16, a_m, 0), b_mant, b_exp,
-                   N * (klen / 16) * plane_group_bytes(16, b_m, 0), (int)M, (int)N, (int)(klen / 16), na, nb,
-                   fmt_flag(a_m, na), fmt_flag(b_m, nb), ldexpf(1.0f, scale_log2)};
+  const Operands p = operands(a_mant, a_exp, a_m, na, b_mant, b_exp, b_m, nb, M, N, M, N, klen, scale_log2);
   const Segments seg{k_offsets, experts, (int)klen};
-  // (the tiles of every expert, at the mean length of K)
-  Price us{};
-  price_tiles(p, (double)(experts * ceil_div(M, 128)), (double)(experts * ceil_div(M, 256)),
-              (double)klen / 128.0 / experts, us);
-  return run_tiled(p, us.small <= us.big, true, C, N, seg, s);
+  return run_tiled(p, route_grad(p, experts, M, klen).rows == 128, true, C, N, seg, s);
 }
 
 }  // namespace fastbfp

@@ -178,6 +178,14 @@ hipError_t launch_quantize_experts(const float* x, int64_t rows, int64_t C, int 
                                    const int32_t* offsets, const int32_t* k_offsets, int experts, int64_t slots,
                                    int64_t klen, int m, int mode, uint64_t seed_r, uint64_t seed_c, uint8_t* mr,
                                    uint8_t* er, uint8_t* mc, uint8_t* ec, uint32_t* status, hipStream_t s);
+// How a product of experts runs: rows 16 or 32, the few-token kernel on tiles of so many
+// slots, `waves` waves to a tile and `each` groups of tiles to a workgroup; else the
+// tiled kernel (waves 0), rows 128 on tiles of 128 x 128, 0 on the formats' large ones.
+struct ExpertsRoute {
+  int rows, waves, each;
+};
+ExpertsRoute experts_route(int a_m, int na, int b_m, int nb, int experts, int64_t slots, int64_t N, int64_t K);
+ExpertsRoute experts_grad_route(int a_m, int na, int b_m, int nb, int experts, int64_t M, int64_t N, int64_t klen);
 // C[p] = A[p] . B_e^T for the slots p of expert e (B: N rows of K for each).
 hipError_t launch_gemm_experts(const uint8_t* a_mant, const uint8_t* a_exp, int a_m, int na, const uint8_t* b_mant,
                                const uint8_t* b_exp, int b_m, int nb, const int32_t* offsets, int experts,

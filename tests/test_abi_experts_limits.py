@@ -28,3 +28,24 @@ def test_plan_workgroups_are_bounded(experts):
     # below, one workgroup for each 4096 slots
     for slots in (4097, 8192, 8193, 100000):
         assert plan_ws(slots, experts) == -(-slots // 4096) * (experts + 1) * 4
+
+
+def test_route_arguments():
+    lib = _lib.load()
+    rows, waves = ctypes.c_int(-9), ctypes.c_int(-9)
+
+    def route(am=4, bm=4, experts=8, slots=64, N=256, K=256, ma=4, mb=4, r=ctypes.byref(rows), w=ctypes.byref(waves)):
+        return lib.bfp_gemm_experts_route(am, bm, experts, slots, N, K, ma, mb, r, w)
+
+    def grad(am=4, bm=4, experts=8, M=64, N=256, places=1024, ma=4, mb=4, r=ctypes.byref(rows)):
+        return lib.bfp_gemm_experts_grad_route(am, bm, experts, M, N, places, ma, mb, r)
+
+    assert route() == 0 and rows.value in (0, 16, 32, 128) and (waves.value > 0) == (rows.value in (16, 32))
+    assert grad() == 0 and rows.value in (0, 128)
+    for bad in (dict(r=None), dict(w=None), dict(slots=0), dict(N=0), dict(slots=-1), dict(experts=0)):
+        assert route(**bad) == 1, bad
+    for bad in (dict(r=None), dict(M=0), dict(N=0), dict(experts=0)):
+        assert grad(**bad) == 1, bad
+    assert route(K=40) == 2 and grad(places=192) == 2
+    assert route(ma=3) == 3 and route(experts=513) == 3 and grad(ma=3) == 3
+    assert route(am=9) == 4 and grad(mb=5) == 4
