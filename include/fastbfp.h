@@ -727,6 +727,18 @@ int bfp_orthogonalize(const float* grad, const float* momentum, float* momentum_
                       int64_t batch, int64_t rows, int64_t cols, int steps, float eps, float* out, void* workspace,
                       size_t workspace_bytes, void* stream);
 
+/*
+ * bfp_orthogonalize_route -- the products' workgroup tiles.  Host only, nothing is
+ * launched; for tests and tuning.
+ *   tiles : int[3]: their edge for X X^T, for the products of symmetric matrices
+ *           and for the one that writes X.  stages : int[3]: their stages in LDS.
+ *   parts : int[2], whole : int64[2]: of the first two, the parts of K in which the
+ *           tiles after the first `whole` are summed (1: all run whole).
+ * Matrices of up to 128 rows or columns take the symmetric products in one kernel.
+ */
+int bfp_orthogonalize_route(int64_t batch, int64_t rows, int64_t cols, int* tiles, int* stages, int* parts,
+                            int64_t* whole);
+
 #ifdef __cplusplus
 }
 #endif

@@ -64,6 +64,8 @@ SIGNATURES = {
     "bfp_combine_experts": (_I, [_P, _P, _P, _P, _I64, _I, _I, _I64, _P, _P]),
     "bfp_combine_experts_grad": (_I, [_P, _P, _P, _P, _P, _I64, _I, _I, _I64, _P, _P, _P]),
     "bfp_orthogonalize_ws_size": (_I, [_I64, _I64, _I64, ctypes.POINTER(ctypes.c_size_t)]),
+    "bfp_orthogonalize_route": (_I, [_I64, _I64, _I64] + [ctypes.POINTER(ctypes.c_int)] * 3 +
+                                [ctypes.POINTER(ctypes.c_int64)]),
     "bfp_orthogonalize": (_I, [_P, _P, _P, ctypes.c_float, _I, _I64, _I64, _I64, _I, ctypes.c_float, _P, _P,
                                ctypes.c_size_t, _P]),
     "bfp_adaptive_mantissa": (_I, [ctypes.c_double, ctypes.c_double, ctypes.c_double]),

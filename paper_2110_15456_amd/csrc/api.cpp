@@ -860,6 +860,17 @@ int bfp_orthogonalize_ws_size(int64_t batch, int64_t rows, int64_t cols, size_t*
   return BFP_OK;
 }
 
+int bfp_orthogonalize_route(int64_t batch, int64_t rows, int64_t cols, int* tiles, int* stages, int* parts,
+                            int64_t* whole) {
+  const int st = check_matrices(batch, rows, cols);
+  if (st != BFP_OK) return st;
+  if (!tiles || !stages || !parts || !whole || batch == 0 || rows == 0 || cols == 0) return BFP_E_ARG;
+  const fastbfp::OrthoRoute r = fastbfp::orthogonalize_route(batch, rows, cols);
+  for (int i = 0; i < 3; ++i) tiles[i] = r.tile[i], stages[i] = r.stages[i];
+  for (int i = 0; i < 2; ++i) parts[i] = r.parts[i], whole[i] = r.whole[i];
+  return BFP_OK;
+}
+
 int bfp_orthogonalize(const float* grad, const float* momentum, float* momentum_out, float beta, int nesterov,
                       int64_t batch, int64_t rows, int64_t cols, int steps, float eps, float* out, void* workspace,
                       size_t workspace_bytes, void* stream) {

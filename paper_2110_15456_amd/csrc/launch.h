@@ -203,6 +203,14 @@ hipError_t launch_combine_experts_grad(const float* dout, const float* y, const 
 
 // The orthogonalised update (orthogonalize.hip).  momentum null: of grad itself.
 int64_t orthogonalize_ws(int64_t batch, int64_t rows, int64_t cols);
+// Tiles of X X^T, of the products of symmetric matrices and of Q X, and their stages in
+// LDS; for the first two the parts of K that the last tiles are summed in, and how many
+// tiles run whole.
+struct OrthoRoute {
+  int tile[3], stages[3], parts[2];
+  int64_t whole[2];
+};
+OrthoRoute orthogonalize_route(int64_t batch, int64_t rows, int64_t cols);
 hipError_t launch_orthogonalize(const float* grad, const float* momentum, float* momentum_out, float beta,
                                 bool nesterov, int64_t batch, int64_t rows, int64_t cols, int steps, float eps,
                                 float* out, uint8_t* ws, hipStream_t s);

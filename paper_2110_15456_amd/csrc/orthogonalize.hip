@@ -749,22 +749,54 @@ NsPlan ns_plan(int64_t batch, int64_t rows, int64_t cols) {
   return p;
 }
 
+// Stages of a product's slabs in LDS (k_ns_gemm).
+int stages_of(int tile, int64_t wgs, int64_t slabs) { return tile == 64 && wgs <= 512 && slabs <= 12 ? 4 : 2; }
+
 template <bool TR, int OUT>
 hipError_t run_gemm(const Gemm& g, int tile, int64_t wgs, hipStream_t s) {
   if (tile == 256)
     hipLaunchKernelGGL((k_ns_gemm<256, 256, 2, 4, TR, OUT, 2>), dim3((unsigned)wgs), dim3(512), 0, s, g);
   else if (tile == 128)
     hipLaunchKernelGGL((k_ns_gemm<128, 128, 2, 2, TR, OUT, 2>), dim3((unsigned)wgs), dim3(256), 0, s, g);
-  else if (wgs <= 512 && (g.parts > 1 ? g.part_slabs : blocks_of(g.K)) <= 12)
+  else if (stages_of(tile, wgs, g.parts > 1 ? g.part_slabs : blocks_of(g.K)) == 4)
     hipLaunchKernelGGL((k_ns_gemm<64, 64, 2, 2, TR, OUT, 4>), dim3((unsigned)wgs), dim3(256), 0, s, g);
   else
     hipLaunchKernelGGL((k_ns_gemm<64, 64, 2, 2, TR, OUT, 2>), dim3((unsigned)wgs), dim3(256), 0, s, g);
   return hipGetLastError();
 }
 
+// A symmetric product's launch: slabs in a part of K, parts, workgroups.
+struct SymLaunch {
+  int part_slabs, parts;
+  int64_t tiles, wgs;
+};
+SymLaunch sym_launch(const Tiling& how, int64_t batch, int64_t n, int64_t K) {
+  const int64_t t = (n + how.tile - 1) / how.tile, tri = batch * t * (t + 1) / 2;
+  const int slabs = (int)blocks_of(K), ps = (slabs + how.parts - 1) / how.parts, parts = (slabs + ps - 1) / ps;
+  return SymLaunch{ps, parts, tri, how.whole + (tri - how.whole) * parts};
+}
+
 }  // namespace
 
 int64_t orthogonalize_ws(int64_t batch, int64_t rows, int64_t cols) { return ns_plan(batch, rows, cols).bytes; }
+
+OrthoRoute orthogonalize_route(int64_t batch, int64_t rows, int64_t cols) {
+  const NsPlan p = ns_plan(batch, rows, cols);
+  OrthoRoute r{};
+  auto sym = [&](int i, const Tiling& how, int64_t K) {
+    const SymLaunch l = sym_launch(how, batch, p.n, K);
+    r.tile[i] = how.tile;
+    r.stages[i] = stages_of(how.tile, l.wgs, l.parts > 1 ? l.part_slabs : blocks_of(K));
+    r.parts[i] = l.parts;
+    r.whole[i] = how.whole;
+  };
+  sym(0, p.gram, p.k);
+  sym(1, p.square, p.n);
+  const int64_t t = p.apply.tile;
+  r.tile[2] = p.apply.tile;
+  r.stages[2] = stages_of(p.apply.tile, batch * ((p.n + t - 1) / t) * ((p.k + t - 1) / t), blocks_of(p.n));
+  return r;
+}
 
 hipError_t launch_orthogonalize(const float* grad, const float* momentum, float* momentum_out, float beta,
                                 bool nesterov, int64_t batch, int64_t rows, int64_t cols, int steps, float eps,
@@ -800,13 +832,13 @@ hipError_t launch_orthogonalize(const float* grad, const float* momentum, float*
   // out = alpha a b^T + beta m + gamma I of symmetric n x n matrices
   auto product = [&](const uint8_t* a, const uint8_t* b, int64_t batch_bytes, int K, const Tiling& how, uint8_t* o,
                      float alpha, const uint8_t* m, float beta_m, float gamma) {
-    const int64_t t = (n + how.tile - 1) / how.tile, tri = batch * t * (t + 1) / 2;
-    const int slabs = (int)blocks_of(K), ps = (slabs + how.parts - 1) / how.parts, parts = (slabs + ps - 1) / ps;
-    const Gemm g{a, batch_bytes, b, batch_bytes, n, n, K, (int)t, (int)t, alpha, o, p.s_bytes, (int)p.ld, m, beta_m,
-                 gamma, (int)how.whole, parts, ps, sum};
-    const hipError_t err = run_gemm<false, kSym>(g, how.tile, how.whole + (tri - how.whole) * parts, s);
-    if (err != hipSuccess || how.whole == tri) return err;
-    const int64_t pieces = (tri - how.whole) * (how.tile / 32) * (how.tile / 32);
+    const SymLaunch l = sym_launch(how, batch, n, K);
+    const int t = (n + how.tile - 1) / how.tile;
+    const Gemm g{a, batch_bytes, b, batch_bytes, n, n, K, t, t, alpha, o, p.s_bytes, (int)p.ld, m, beta_m, gamma,
+                 (int)how.whole, l.parts, l.part_slabs, sum};
+    const hipError_t err = run_gemm<false, kSym>(g, how.tile, l.wgs, s);
+    if (err != hipSuccess || how.whole == l.tiles) return err;
+    const int64_t pieces = (l.tiles - how.whole) * (how.tile / 32) * (how.tile / 32);
     if (how.tile == 256) hipLaunchKernelGGL(k_ns_finish<256>, dim3((unsigned)pieces), dim3(256), 0, s, g);
     else if (how.tile == 64) hipLaunchKernelGGL(k_ns_finish<64>, dim3((unsigned)pieces), dim3(256), 0, s, g);
     else hipLaunchKernelGGL(k_ns_finish<128>, dim3((unsigned)pieces), dim3(256), 0, s, g);
@@ -820,13 +852,13 @@ hipError_t launch_orthogonalize(const float* grad, const float* momentum, float*
     const uint8_t* Q = nullptr;
     int q_scale = 0;
     if (n <= kChainMost) {
-      const int slabs = (int)blocks_of(k), ps = (slabs + p.gram.parts - 1) / p.gram.parts, parts = (slabs + ps - 1) / ps;
-      const int64_t t = (n + 63) / 64, tri = batch * t * (t + 1) / 2;
-      e = run_gemm<false, kSym>(Gemm{X[at], p.x_bytes, X[at], p.x_bytes, n, n, k, (int)t, (int)t, 1.0f, nullptr, 0,
-                                     (int)p.ld, nullptr, 0.0f, 0.0f, 0, parts, ps, sum},
-                                64, tri * parts, s);
+      const SymLaunch l = sym_launch(p.gram, batch, n, k);
+      const int t = (n + 63) / 64;
+      e = run_gemm<false, kSym>(Gemm{X[at], p.x_bytes, X[at], p.x_bytes, n, n, k, t, t, 1.0f, nullptr, 0, (int)p.ld,
+                                     nullptr, 0.0f, 0.0f, 0, l.parts, l.part_slabs, sum},
+                                64, l.wgs, s);
       if (e != hipSuccess) return e;
-      const Chain c{sum, parts, n, group == 2, poly[0], p.s_bytes};
+      const Chain c{sum, l.parts, n, group == 2, poly[0], p.s_bytes};
       if (n <= 32) hipLaunchKernelGGL(k_ns_chain<1>, dim3((unsigned)batch), dim3(64), 0, s, c);
       else if (n <= 64) hipLaunchKernelGGL(k_ns_chain<2>, dim3((unsigned)batch), dim3(256), 0, s, c);
       else if (n <= 96) hipLaunchKernelGGL(k_ns_chain<3>, dim3((unsigned)batch), dim3(576), 0, s, c);

@@ -49,3 +49,17 @@ def test_route_arguments():
     assert route(K=40) == 2 and grad(places=192) == 2
     assert route(ma=3) == 3 and route(experts=513) == 3 and grad(ma=3) == 3
     assert route(am=9) == 4 and grad(mb=5) == 4
+
+
+def test_update_route_arguments():
+    lib = _lib.load()
+    tiles, stages, parts, whole = (ctypes.c_int * 3)(), (ctypes.c_int * 3)(), (ctypes.c_int * 2)(), (ctypes.c_int64 * 2)()
+    out = [tiles, stages, parts, whole]
+    assert lib.bfp_orthogonalize_route(2, 300, 500, *out) == 0
+    assert all(t in (64, 128, 256) for t in tiles) and all(s in (2, 4) for s in stages) and min(parts) >= 1
+    turned = [type(o)() for o in out]
+    assert lib.bfp_orthogonalize_route(2, 500, 300, *turned) == 0 and list(map(list, out)) == list(map(list, turned))
+    for i in range(4):
+        assert lib.bfp_orthogonalize_route(2, 300, 500, *[None if j == i else o for j, o in enumerate(out)]) == 1
+    assert lib.bfp_orthogonalize_route(0, 300, 500, *out) == 1 and lib.bfp_orthogonalize_route(1, 0, 5, *out) == 1
+    assert lib.bfp_orthogonalize_route(1, 1 << 20, 16, *out) == 3
