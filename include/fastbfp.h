@@ -699,8 +699,11 @@ int bfp_combine_experts_grad(const float* dout, const float* y, const float* gat
 
 /*
  * bfp_orthogonalize -- a step of momentum whose result is orthogonalised, the
- * direction of a weight update (for bfp_weight_update, with alpha = -learning
- * rate, instead of the raw gradient).  For each of `batch` matrices [rows][cols]:
+ * direction of a weight update (of one matrix: bfp_weight_update takes it, with
+ * alpha = -learning rate, in place of the raw gradient; of the matrices of several
+ * experts: added to the weights, whose two groupings then are bfp_quantize_nd along
+ * either axis, as bfp_weight_update's column grouping would run on from one
+ * expert's rows to the next one's).  For each of `batch` matrices [rows][cols]:
  *   momentum_out = beta momentum + grad
  *   U = grad + beta momentum_out (nesterov = 1) or momentum_out (0)
  *   X = U / (Frobenius norm of U + eps)

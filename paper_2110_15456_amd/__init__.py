@@ -835,8 +835,12 @@ def orthogonal_update(grad: torch.Tensor, momentum: torch.Tensor, beta: float = 
     """A step of momentum and its orthogonalised direction: ``(update,
     momentum_out)`` with momentum_out = beta * momentum + grad (momentum itself
     may be passed for it: in place) and update the orthogonalize of grad + beta *
-    momentum_out (nesterov) or of momentum_out.  weight_update(w, update, -lr)
-    takes it to the weights and their two BFP groupings."""
+    momentum_out (nesterov) or of momentum_out.  For one matrix
+    weight_update(w, update, -lr) takes it to the weights and their two BFP
+    groupings.  For a batch w [experts, N, K]: w.add_(update, alpha=-lr), then
+    quantize(w) and quantize(w, group_axis=1), the operands of gemm_experts and of
+    its gradient (weight_update is 2-D: its column grouping of the flattened
+    weights would run on from one expert's rows to the next one's)."""
     _need_cuda(grad, "grad", torch.float32)
     _need_cuda(momentum, "momentum", torch.float32)
     if momentum.shape != grad.shape:

@@ -137,3 +137,28 @@ def test_gate_gradients_of_long_rows(tokens, top, N, stride):
     want = row.astype(np.float64).sum() * scale[p.place.cpu().numpy()].reshape(tokens, top)
     err = np.abs(dg.cpu().numpy() - want) / want
     assert np.all(err <= 5 * 2.0 ** -24 + N * 2.0 ** -53), err.max() * 2 ** 24
+
+
+@pytest.mark.parametrize("N", [48, 40])
+def test_update_of_every_experts_weights(N):
+    """The update of a batch of matrices, taken to the weights and their two groupings
+    as the binding describes, is each expert's own (N a multiple of 16 or not: the
+    grouping along N needs one)."""
+    announce("weights of experts updated, N = %d" % N)
+    E, K = 3, 64
+    w, grad = torch.randn((E, N, K), device="cuda"), torch.randn((E, N, K), device="cuda")
+    step, momentum = fb.orthogonal_update(grad, torch.zeros_like(grad))
+    new = w.clone().add_(step, alpha=-0.5)
+    along_k = fb.quantize(new)
+    along_n = fb.quantize(new, group_axis=1) if N % 16 == 0 else None
+    for e in range(E):
+        one, m_one = fb.orthogonal_update(grad[e].contiguous(), torch.zeros_like(grad[e]))
+        assert torch.equal(m_one, momentum[e])
+        assert float((one - step[e]).norm()) <= 1e-4 * float(one.norm())  # (another batch: other parts of the sums)
+        if along_n is None:
+            continue
+        _, rows, cols = fb.weight_update(w[e].contiguous(), step[e].contiguous(), -0.5)
+        r, c = slice(e * N, (e + 1) * N), slice(e * K, (e + 1) * K)
+        assert torch.equal(rows.exp, along_k.exp[r]) and torch.equal(cols.exp, along_n.exp[c])
+        assert torch.equal(fb.dequantize(rows), fb.dequantize(along_k)[r])
+        assert torch.equal(fb.dequantize(cols), fb.dequantize(along_n)[c])
