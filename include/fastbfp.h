@@ -720,8 +720,14 @@ int bfp_combine_experts_grad(const float* dout, const float* y, const float* gat
  *   steps        : 1 .. 16;  eps >= 0.
  *   workspace    : bfp_orthogonalize_ws_size bytes, 256-byte aligned; overwritten.
  *                  Must not overlap the arrays.
- * Norms are summed in 64 bits.  The products are computed to about FP32's accuracy
- * (operands in two FP16 planes, 22 bits; FP32 sums) in an order that depends on
+ * Norms are summed in 64 bits.  The products' operands are two FP16 planes, which
+ * hold an entry of X to 2^-23 of itself or 2^-40, whichever is more (X's norm is 1 at
+ * first), with FP32 sums: in each matrix' norm about the error of the formula in FP32.
+ * Rows or columns of U far weaker than the rest are held more coarsely than FP32
+ * would, a row of r times U's norm to about 2^-40 sqrt(cols) / r (rows 10^-4 and
+ * 10^-6 of the others in 1024 x 4096: 8e-6 and 8e-4); beyond 8 steps or so, which
+ * grow such rows to the size of the others, that is the error of the matrix.  Sums
+ * are added in an order that depends on
  * the sizes alone.  rows and cols below 2^20 and rows * cols up to 2^29
  * (BFP_E_UNSUPPORTED beyond).
  */
