@@ -710,6 +710,8 @@ int bfp_combine_experts_grad(const float* dout, const float* y, const float* gat
  *   `steps` times:  S = X X^T,  X = (a I + b S + c S^2) X   (X X^T on the shorter
  *   side: X^T X where rows > cols), (a, b, c) = (3.4445, -4.7750, 2.0315)
  *   out = X
+ * (form and coefficients of the Muon optimiser: K. Jordan and others, "Muon: An
+ * optimizer for hidden layers in neural networks", 2024)
  * so that U's singular vectors stay and its singular values go to about 1 (five
  * steps: 0.7 to 1.2 for those above 0.3% of the norm).  A zero U gives zeros where
  * eps > 0.
@@ -726,10 +728,9 @@ int bfp_combine_experts_grad(const float* dout, const float* y, const float* gat
  * Rows or columns of U far weaker than the rest are held more coarsely than FP32
  * would, a row of r times U's norm to about 2^-40 sqrt(cols) / r (rows 10^-4 and
  * 10^-6 of the others in 1024 x 4096: 8e-6 and 8e-4); beyond 8 steps or so, which
- * grow such rows to the size of the others, that is the error of the matrix.  Sums
- * are added in an order that depends on
- * the sizes alone.  rows and cols below 2^20 and rows * cols up to 2^29
- * (BFP_E_UNSUPPORTED beyond).
+ * grow such rows to the size of the others, that is the error of the matrix.  The
+ * order of the sums depends on the sizes alone.  rows and cols below 2^20 and
+ * rows * cols up to 2^29 (BFP_E_UNSUPPORTED beyond).
  */
 int bfp_orthogonalize_ws_size(int64_t batch, int64_t rows, int64_t cols, size_t* workspace_bytes);
 int bfp_orthogonalize(const float* grad, const float* momentum, float* momentum_out, float beta, int nesterov,

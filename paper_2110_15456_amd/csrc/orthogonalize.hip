@@ -3,7 +3,9 @@
 //   M' = beta M + G,  U = G + beta M' (Nesterov) or M',  X = U / (|U|_F + eps),
 //   repeated:  S = X X^T,  X <- (a I + b S + c S^2) X
 // with (a, b, c) = (3.4445, -4.7750, 2.0315), which takes every singular value
-// of X in (0, 1] towards 1 (into about 0.7 .. 1.2) and leaves the vectors.
+// of X in (0, 1] towards 1 (into about 0.7 .. 1.2) and leaves the vectors.  (Form and
+// coefficients of the Muon optimiser: K. Jordan and others, "Muon: An optimizer for
+// hidden layers in neural networks", 2024.)
 //
 // X is kept with no more rows than columns (n <= k; the transpose of U where it
 // has more), so the products are n x n x k, n x n x n and n x k x n.
