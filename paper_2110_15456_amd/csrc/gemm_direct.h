@@ -357,7 +357,7 @@ hipError_t launch_direct_t(int rm, int rn, const uint8_t* a_mant, const uint8_t*
   if (rm == RM && rn == RN) {                                                                                         \
     if (out)                                                                                                          \
       hipLaunchKernelGGL((k_gemm_direct<NA, NB, FA, FB, G, RM, RN, true>), grid, dim3(64 * nw), 0, s, a_mant, a_exp,  \
-                         a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, *out);                                                 \
+                         a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, *out);                                   \
     else                                                                                                              \
       hipLaunchKernelGGL((k_gemm_direct<NA, NB, FA, FB, G, RM, RN, false>), grid, dim3(64 * nw), 0, s, a_mant, a_exp, \
                          a_ps, b_mant, b_exp, b_ps, M, N, ng, scale, C, ldc, direct::Out{});                          \

@@ -11,6 +11,7 @@
 // group per lane makes one Philox call serve 16 values, which keeps stochastic
 // rounding within the HBM-bound budget.
 #include <mutex>
+#include <type_traits>
 
 #include "bfp_quant.h"
 #include "segments.h"
@@ -870,7 +871,10 @@ static hipError_t launch_experts_t(const float* x, const ExpertSlots& sl, int64_
   }
   const int tiles_c = (int)((C + 63) / 64);
   const dim3 grid((unsigned)(klen / 64 * tiles_c));
-#define FASTBFP_EXPERTS(ROWS)                                                                                            hipLaunchKernelGGL((k_quantize_experts<MODE, NCH, P0, P1, ROWS>), grid, dim3(256), 0, s, x, sl, C, klen, tiles_c,                         (uint32_t)m, (uint32_t)seed_r, (uint32_t)(seed_r >> 32), (uint32_t)seed_c,                                             (uint32_t)(seed_c >> 32), mr, mr + rgroups * b0, er, mc, mc + cgroups * b0, ec, status)
+#define FASTBFP_EXPERTS(ROWS)                                                                                         \
+  hipLaunchKernelGGL((k_quantize_experts<MODE, NCH, P0, P1, ROWS>), grid, dim3(256), 0, s, x, sl, C, klen, tiles_c,   \
+                     (uint32_t)m, (uint32_t)seed_r, (uint32_t)(seed_r >> 32), (uint32_t)seed_c,                       \
+                     (uint32_t)(seed_c >> 32), mr, mr + rgroups * b0, er, mc, mc + cgroups * b0, ec, status)
   if (mr) FASTBFP_EXPERTS(true);
   else FASTBFP_EXPERTS(false);
 #undef FASTBFP_EXPERTS
@@ -886,11 +890,17 @@ hipError_t launch_quantize_experts(const float* x, int64_t rows, int64_t C, int 
   if (!mc && top == 0 && !status) return launch_quantize_rows(x, slots, C, 16, m, mode, seed_r, mr, er, nullptr, s);
   const ExpertSlots sl{order, offsets, k_offsets, experts, (int)slots, (int)rows, Divisor((uint32_t)(top > 0 ? top : 1)),
                        top > 0};
-#define FASTBFP_EXPERTS(MODE)                                                                                          do {                                                                                                                   if (m <= 2) return launch_experts_t<MODE, 1, kPlaneFP4, kPlaneFP6>(x, sl, C, klen, m, seed_r, seed_c, mr, er, mc,                                                                        ec, status, s);                                   if (m <= 4) return launch_experts_t<MODE, 1, kPlaneFP6, kPlaneFP6>(x, sl, C, klen, m, seed_r, seed_c, mr, er, mc,                                                                        ec, status, s);                                   if (m <= 6) return launch_experts_t<MODE, 2, kPlaneFP6, kPlaneLo2>(x, sl, C, klen, m, seed_r, seed_c, mr, er, mc,                                                                        ec, status, s);                                   return launch_experts_t<MODE, 2, kPlaneFP6, kPlaneFP6>(x, sl, C, klen, m, seed_r, seed_c, mr, er, mc, ec, status,                                                            s);                                                         } while (0)
-  if (mode == kNearest) FASTBFP_EXPERTS(kNearest);
-  if (mode == kStochastic) FASTBFP_EXPERTS(kStochastic);
-  FASTBFP_EXPERTS(kTruncate);
-#undef FASTBFP_EXPERTS
+  auto run = [&](auto mode) {
+    constexpr int MODE = decltype(mode)::value;
+    auto go = m <= 2   ? launch_experts_t<MODE, 1, kPlaneFP4, kPlaneFP6>
+              : m <= 4 ? launch_experts_t<MODE, 1, kPlaneFP6, kPlaneFP6>
+              : m <= 6 ? launch_experts_t<MODE, 2, kPlaneFP6, kPlaneLo2>
+                       : launch_experts_t<MODE, 2, kPlaneFP6, kPlaneFP6>;
+    return go(x, sl, C, klen, m, seed_r, seed_c, mr, er, mc, ec, status, s);
+  };
+  if (mode == kNearest) return run(std::integral_constant<int, kNearest>{});
+  if (mode == kStochastic) return run(std::integral_constant<int, kStochastic>{});
+  return run(std::integral_constant<int, kTruncate>{});
 }
 
 template <int NCH, int P0, int P1 = kPlaneFP6>
