@@ -68,9 +68,9 @@ hipError_t run_direct(const Operands& p, int rm, int kw, int each, float* C, int
 // so the tiles of rows are those that slots spread over all experts would have, each
 // expert's last one half full.  Fitted to graph replays of ten calls at 1 to 1024
 // slots an expert, 4 to 128 experts of 256 x 256 to 4096 x 4096: over 288 products of up
-// to 160 slots an expert the kernel taken is 3% slower than the fastest in the mean
-// and 43% at worst.  What decided, us (few tokens on 16 and 32 rows, tiles of 128 x 128,
-// large tiles):
+// to 160 slots an expert the kernel taken is 4% slower than the fastest in the mean and
+// 50% at worst, over 92 of more slots 1% and 32%.  What decided, us (few tokens on 16 and
+// 32 rows, tiles of 128 x 128, large tiles):
 //   8 x 2048 x 2048 (4,4)    4 slots   7.2   9.0   18   32     (6,6)  12     -   31  37
 //                           24        11.4   9.6   19   31            18     -   31  37
 //                           64        22    22     19   32            40     -   34  38

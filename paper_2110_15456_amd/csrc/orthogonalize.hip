@@ -198,11 +198,18 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 64 && ST == 2 ? 4 : 2) void k
   const uint8_t* B = p.b + batch * p.b_batch + (TR ? (int64_t)col0 * 4 : (int64_t)col0 * b_row);
   const rsrc_t rb = make_rsrc(B, TR ? (uint32_t)p.K * b_row - (uint32_t)col0 * 4 : (uint32_t)min(BN, p.N - col0) * b_row);
 
-  v16 acc[TM][TN];
+  // The sums of hi hi and, on the 64 tile, those of hi lo + lo hi beside them, which then
+  // are rounded at their own size, 2^-11 of the other (all of it in one: 30% more error on
+  // 256 x 512 to 2048 x 2048, and no faster; larger tiles have no registers left).
+  constexpr bool APART = BM == 64;
+  v16 acc[TM][TN], cross[APART ? TM : 1][APART ? TN : 1];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = v16{};
+    for (int j = 0; j < TN; ++j) {
+      acc[i][j] = v16{};
+      if constexpr (APART) cross[i][j] = v16{};
+    }
 
   const uint32_t chunk = (uint32_t)((lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7));
   const uint32_t ab_lane = chunk * 16;  // (rows of A, and of B without TR)
@@ -266,9 +273,15 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 64 && ST == 2 ? 4 : 2) void k
       for (int i = 0; i < TM; ++i) {
         const h8 hi = frag(cur, wr * WM + 32 * i, h, 0), lo = frag(cur, wr * WM + 32 * i, h, 1);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) mma(acc[i][j], lo, b[j][0]);
+        for (int j = 0; j < TN; ++j) {
+          if constexpr (APART) mma(cross[i][j], lo, b[j][0]);
+          else mma(acc[i][j], lo, b[j][0]);
+        }
 #pragma unroll
-        for (int j = 0; j < TN; ++j) mma(acc[i][j], hi, b[j][1]);
+        for (int j = 0; j < TN; ++j) {
+          if constexpr (APART) mma(cross[i][j], hi, b[j][1]);
+          else mma(acc[i][j], hi, b[j][1]);
+        }
 #pragma unroll
         for (int j = 0; j < TN; ++j) mma(acc[i][j], hi, b[j][0]);
       }
@@ -302,6 +315,12 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 64 && ST == 2 ? 4 : 2) void k
   // sits at g ^ swz(r): 16 rows of one granule, and 8 rows 8 apart, on all banks.
   // (On the 64 tile the four waves' 32 x 32 are one such piece, of which each
   // writes a quarter.)
+  if constexpr (APART) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] += cross[i][j];
+  }
   __syncthreads();
   constexpr bool JOIN = BM == 64;
   static_assert(JOIN ? BN == 64 && NW == 4 && STAGE == 16384
@@ -455,6 +474,14 @@ __global__ __launch_bounds__(256) void k_ns_finish(Gemm p) {
 // Everything stays in LDS, in two matrices (128 KB at n = 128), as each product takes
 // the place of an operand that it is the last to read: a launch for each product
 // takes 6.9 us at n = 64 where its 12 MFMAs a wave take 0.3.
+//
+// A's diagonal takes its own way: it is zero in A's fragments, and a_rr b_rc, with a_rr
+// (and b_rr) in FP32, is added to what the MFMAs give.  The matrix cores add eight
+// products after aligning them to the largest and dropping what lies below its last
+// place; these matrices are near-diagonal, and next to a product of two diagonal values
+// the others lost their last bits (update of 64 x 576 of noise: 2.7e-6 off, FP32 1.7e-6;
+// now 0.6e-6, for 1.2 us more in a launch of 7.0; the diagonal's products in MFMAs of
+// their own, at 22 bits: 1.0e-6, 0.7 us).
 struct Chain {
   const float* sums;  // [matrix][tile of the lower triangle][part][64][64]
   int parts, n, pair;
@@ -465,11 +492,13 @@ template <int NB>
 __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
   constexpr int R = KS * NB, ROW = BLOCK * NB, NT = 64 * NB * NB, T = 64;
   __shared__ __attribute__((aligned(128))) uint8_t mem[2][R * ROW];
+  __shared__ __attribute__((aligned(16))) float diag[2][R];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int wr = wave / NB, wc = wave % NB, fr = lane & 31, fk = lane >> 5;
   // chunk c (16 bytes) of row r, spread over the banks within its block
   auto at = [](int r, int c) { return r * ROW + (c & ~7) * 16 + ((c & 7) ^ (NB % 2 ? (r >> 1) & 7 : r & 7)) * 16; };
-  auto put4 = [&](uint8_t* m, int r, int c, const v4& v) {
+  // four values of a row of matrix m
+  auto put4 = [&](int m, int r, int c, const v4& v) {
     h4 hi, lo;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -477,49 +506,80 @@ __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
       lo[t] = (_Float16)(v[t] - (float)hi[t]);
     }
     const int chunk = c / KS * 8 + (c % KS) / 8;
-    *reinterpret_cast<h4*>(m + at(r, chunk) + (c & 4) * 2) = hi;
-    *reinterpret_cast<h4*>(m + at(r, chunk + 4) + (c & 4) * 2) = lo;
+    *reinterpret_cast<h4*>(mem[m] + at(r, chunk) + (c & 4) * 2) = hi;
+    *reinterpret_cast<h4*>(mem[m] + at(r, chunk + 4) + (c & 4) * 2) = lo;
   };
-  // dst = alpha a b^T + beta m + gamma I; dst may be any of the others
-  auto product = [&](uint8_t* dst, const uint8_t* a, const uint8_t* b, float alpha, const uint8_t* m, float beta,
-                     float gamma) {
-    v16 acc = {};
+  // this lane's four values, of row r of the wave's tile, with d on the diagonal
+  auto get4 = [&](int m, int r, int c, float d) -> v4 {
+    const int chunk = c / KS * 8 + (c % KS) / 8;
+    const h4 hi = *reinterpret_cast<const h4*>(mem[m] + at(r, chunk) + (c & 4) * 2);
+    const h4 lo = *reinterpret_cast<const h4*>(mem[m] + at(r, chunk + 4) + (c & 4) * 2);
+    v4 v;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = r == c + t ? d : (float)hi[t] + (float)lo[t];
+    return v;
+  };
+  // zero where the diagonal lies in this lane's eight columns of either half of a block
+  u4 off[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int i = fr - 16 * k - 8 * fk - 2 * t;
+      off[k][t] = i == 0 ? 0xFFFF0000u : i == 1 ? 0x0000FFFFu : 0xFFFFFFFFu;
+    }
+  // dst = alpha a b^T + beta m + gamma I for symmetric b; dst may be any of the others,
+  // m -1: none
+  auto product = [&](int dst, int ia, int ib, float alpha, int im, float beta, float gamma) {
+    const uint8_t *a = mem[ia], *b = mem[ib];
+    const int r = 32 * wr + fr;
+    const float da = diag[ia][r], db = diag[ib][r], dm = im >= 0 ? diag[im][r] : 0.0f;
+    v16 acc = {}, cross = {};
 #pragma unroll
     for (int h = 0; h < 2 * NB; ++h) {
       h8 f[2][2];
 #pragma unroll
       for (int pl = 0; pl < 2; ++pl) {
         const int chunk = h / 2 * 8 + pl * 4 + 2 * (h & 1) + fk;
-        f[0][pl] = *reinterpret_cast<const h8*>(a + at(32 * wr + fr, chunk));
+        f[0][pl] = *reinterpret_cast<const h8*>(a + at(r, chunk));
         f[1][pl] = *reinterpret_cast<const h8*>(b + at(32 * wc + fr, chunk));
       }
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[1][0], f[0][1], acc, 0, 0, 0);
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[1][1], f[0][0], acc, 0, 0, 0);
+      if (h / 2 == wr) {  // (the whole wave: A's diagonal lies in these columns)
+#pragma unroll
+        for (int pl = 0; pl < 2; ++pl) f[0][pl] = __builtin_bit_cast(h8, __builtin_bit_cast(u4, f[0][pl]) & off[h & 1]);
+      }
+      cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[1][0], f[0][1], cross, 0, 0, 0);
+      cross = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[1][1], f[0][0], cross, 0, 0, 0);
       acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[1][0], f[0][0], acc, 0, 0, 0);
     }
+    acc += cross;
     v4 out[4];
+    float d = 0.0f;  // the lane's value on the diagonal, if it has one
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const int r = 32 * wr + fr, c = 32 * wc + 8 * q + 4 * fk, chunk = c / KS * 8 + (c % KS) / 8;
+      const int c = 32 * wc + 8 * q + 4 * fk;
+      const v4 vb = get4(ib, r, c, db);
       v4& v = out[q];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) v[t] = acc[4 * q + t] * alpha;
-      if (m) {
-        const h4 hi = *reinterpret_cast<const h4*>(m + at(r, chunk) + (c & 4) * 2);
-        const h4 lo = *reinterpret_cast<const h4*>(m + at(r, chunk + 4) + (c & 4) * 2);
+      for (int t = 0; t < 4; ++t) v[t] = __builtin_fmaf(da, vb[t], acc[4 * q + t]) * alpha;
+      if (im >= 0) {
+        const v4 vm = im == ib ? vb : get4(im, r, c, dm);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) v[t] += beta * ((float)hi[t] + (float)lo[t]);
+        for (int t = 0; t < 4; ++t) v[t] += beta * vm[t];
       }
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-        if (r == c + t && r < p.n) v[t] += gamma;
+      for (int t = 0; t < 4; ++t) {
+        v[t] += r == c + t && r < p.n ? gamma : 0.0f;
+        d = r == c + t ? v[t] : d;
+      }
     }
     __syncthreads();  // every wave has read
 #pragma unroll
-    for (int q = 0; q < 4; ++q) put4(dst, 32 * wr + fr, 32 * wc + 8 * q + 4 * fk, out[q]);
+    for (int q = 0; q < 4; ++q) put4(dst, r, 32 * wc + 8 * q + 4 * fk, out[q]);
+    if (wr == wc && ((fr >> 2) & 1) == fk) diag[dst][r] = d;
     __syncthreads();
   };
-  uint8_t *S = mem[0], *P = mem[1];
+  constexpr int S = 0, P = 1;
   // the triangle's tiles, four values of a row at a time; those below the diagonal mirrored
   constexpr int QUADS = (NB <= 2 ? 1 : 3) * T * T / 4, EACH = (QUADS + NT - 1) / NT;
   const float* sums = p.sums + (int64_t)blockIdx.x * (QUADS * 4) * p.parts;
@@ -538,11 +598,12 @@ __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
     if (q >= QUADS || r >= R || c >= R) continue;
     const v4 v = sum[u] * ldexpf(1.0f, kSScale - 2 * kXScale);
     put4(S, r, c, v);
+    if (r / 4 == c / 4) diag[S][r] = v[r % 4];
     if (t != 1) continue;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const _Float16 hi = (_Float16)v[j];
-      uint8_t* o = S + (r & 7) * 2;
+      uint8_t* o = mem[S] + (r & 7) * 2;
       *reinterpret_cast<_Float16*>(o + at(c + j, r / KS * 8 + (r % KS) / 8)) = hi;
       *reinterpret_cast<_Float16*>(o + at(c + j, r / KS * 8 + (r % KS) / 8 + 4)) = (_Float16)(v[j] - (float)hi);
     }
@@ -551,18 +612,18 @@ __global__ __launch_bounds__(64 * NB * NB) void k_ns_chain(Chain p) {
   const float one = ldexpf(1.0f, -kPScale), sq = ldexpf(kC, kPScale - 2 * kSScale), li = ldexpf(kB, kPScale - kSScale);
   const float id = ldexpf(kA, kPScale);
   product(P, S, S, sq, S, li, id);
-  const uint8_t* Q = P;
+  int Q = P;
   if (p.pair) {
-    product(S, S, P, one, nullptr, 0.0f, 0.0f);  // S P
-    product(S, S, P, one, nullptr, 0.0f, 0.0f);  // P S P
-    product(S, S, S, sq, S, li, id);             // P'
-    product(S, S, P, ldexpf(1.0f, kQScale - 2 * kPScale), nullptr, 0.0f, 0.0f);
+    product(S, S, P, one, -1, 0.0f, 0.0f);  // S P
+    product(S, S, P, one, -1, 0.0f, 0.0f);  // P S P
+    product(S, S, S, sq, S, li, id);        // P'
+    product(S, S, P, ldexpf(1.0f, kQScale - 2 * kPScale), -1, 0.0f, 0.0f);
     Q = S;
   }
   uint8_t* out = p.out + blockIdx.x * p.out_batch;
   for (int q = tid; q < p.n * NB * 8; q += NT) {
     const int r = q / (NB * 8), c = q % (NB * 8);
-    *reinterpret_cast<h8*>(out + (int64_t)r * ROW + c * 16) = *reinterpret_cast<const h8*>(Q + at(r, c));
+    *reinterpret_cast<h8*>(out + (int64_t)r * ROW + c * 16) = *reinterpret_cast<const h8*>(mem[Q] + at(r, c));
   }
 }
 

@@ -52,3 +52,24 @@ def test_weak_columns(n, k):
     u = torch.randn((n, k), generator=torch.Generator(device="cuda").manual_seed(n), device="cuda")
     u[1::2] *= 1e-4
     assert torch.equal(fb.orthogonalize(u.t().contiguous()).t(), fb.orthogonalize(u))
+
+
+# Fixed before the first run: no less accurate than the formula in FP32 on the same
+# input, in the mean over eight draws; a quarter more for the draws themselves.
+@pytest.mark.parametrize("n,k", [(16, 16), (48, 48), (64, 576), (32, 1000), (96, 300), (128, 128), (128, 1152), (160, 160),
+                                 (256, 512), (512, 512)])
+@pytest.mark.parametrize("strong", [0, 8], ids=["noise", "strong"])
+def test_no_less_accurate_than_fp32(n, k, strong):
+    announce("orthogonalize %d x %d against FP32, %d strong directions" % (n, k, strong))
+    ours = low = 0.0
+    for seed in range(8):
+        g = torch.Generator(device="cuda").manual_seed(100 + seed)
+        u = 1e-4 * torch.randn((n, k), generator=g, device="cuda")
+        if strong:
+            u += 1e-2 / k ** 0.5 * (torch.randn((n, strong), generator=g, device="cuda") @
+                                    torch.randn((strong, k), generator=g, device="cuda"))
+        want = plain(u.double(), 5)
+        size = float(want.norm())
+        ours += float((fb.orthogonalize(u).double() - want).norm()) / size / 8
+        low += float((plain(u, 5).double() - want).norm()) / size / 8
+    assert ours <= 1.25 * low, (ours, low)
