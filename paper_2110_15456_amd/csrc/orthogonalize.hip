@@ -34,7 +34,7 @@
 // FP16 ends at 2^-24, though, so an entry is held to 2^-23 of itself or (of X) 2^-40 at
 // least: rows or columns 2^-20 and more below the rest lose what FP32 would keep of
 // them (rows at 10^-6 of the others, 1024 x 4096: 8e-4 of themselves after five steps,
-// FP32 5e-7; of the matrix 1.3e-6, FP32 4.2e-6).  That is this layout's price: planes
+// FP32 5e-7; of the matrix 1.1e-6, FP32 4.2e-6).  That is this layout's price: planes
 // with an exponent range of their own would be three of BF16 and six MFMAs.
 //
 // Layout ("planes"): rows of blocks of 32 columns, a block 128 bytes, 32 hi then

@@ -194,3 +194,25 @@ def test_gradients(m_a, m_b, tile):
                 for t, m in ((dy, m_a), (xs, m_b)))
         assert within(out[1 + e], a, b), e
     assert np.any(np.diff(koff) == 0)
+
+
+@pytest.mark.parametrize("m_a,m_b", [(1, 3), (3, 1), (3, 5), (5, 7), (7, 5), (7, 7), (1, 7), (5, 1)])
+@pytest.mark.parametrize("rows", [16, 128, 0])
+def test_odd_widths(m_a, m_b, rows):
+    found = sizes_for(m_a, m_a, m_b, (rows, None), (256, 400))
+    if found is None:
+        assert rows == 0 and m_a > 4 and m_b > 4  # (one tile for two planes of each)
+        return
+    announce("products (%d, %d) on %d rows: %d experts, %d slots, %d x %d" % (m_a, m_b, rows, *found))
+    check_rows(m_a, m_a, m_b, *found)
+
+
+def test_nothing_to_add():
+    """K = 0: products of nothing are zeros."""
+    announce("products over no values")
+    ids = torch.tensor([0, 1, 1, 2, -1], device="cuda")
+    p = fb.expert_plan(ids, 3)
+    A, _ = fb.quantize_experts(torch.zeros((5, 0), device="cuda"), p, gather=True, cols=False)
+    W = fb.quantize(torch.zeros((3 * 8, 0), device="cuda"))
+    out = torch.full((5, 8), 7.0, device="cuda")
+    assert not bool(fb.gemm_experts(A, W, p, out=out).any())
