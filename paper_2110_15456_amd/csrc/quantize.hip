@@ -759,9 +759,9 @@ hipError_t launch_weight_update(const float* w, const float* dw, float alpha, fl
 // behind an expert's last slot are zeros and rows can lie anywhere in x.
 // 16384 slots of 4096 values, one plane: 100 us for both groupings and 81 for the token
 // grouping alone, 3.5 and 3.9 TB/s; the row grouping alone (gathered by
-// k_quantize_rows) 61 us, 5.2 TB/s of slots' rows read and written.  HBM sees a token's
-// row once for its two slots (134 and 55 MB by the counters, 3.1 TB/s), but the kernel
-// takes as long as the dense conversion of as many rows.
+// k_quantize_rows) 61 us, 5.2 TB/s: a token's row is fetched for each of its two slots (267
+// MB by the counters, calibrated on a copy, and 55 MB written), as these lie far apart in
+// the experts' order.
 struct ExpertSlots {
   const int32_t* order;
   const int32_t* offsets;    // first slot of each expert, in order
