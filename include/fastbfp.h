@@ -4,7 +4,9 @@
  * Block Floating Point with Stochastic Rounding", HPCA 2022).
  *
  * Two operations sit behind this boundary, and what training and serving put
- * around them (the expert layer's products, the orthogonalised update):
+ * around them (8-bit floating-point blocks and their products, the norm in front of a
+ * product, the expert layer's products, the gradients' clipping, the orthogonalised
+ * update):
  *   bfp_quantize  FP32 -> BFP conversion (section III-A; converter of
  *                 section V-C): one shared exponent per group of g values,
  *                 sign-magnitude mantissas of m bits, nearest, stochastic or
@@ -76,7 +78,7 @@
 extern "C" {
 #endif
 
-#define FASTBFP_ABI_VERSION 9
+#define FASTBFP_ABI_VERSION 10
 
 typedef enum {
   BFP_ROUND_NEAREST = 0,    /* add half an LSB, then truncate (ties away from zero) */
@@ -748,6 +750,152 @@ int bfp_orthogonalize(const float* grad, const float* momentum, float* momentum_
  */
 int bfp_orthogonalize_route(int64_t batch, int64_t rows, int64_t cols, int* tiles, int* stages, int* parts,
                             int64_t* whole);
+
+/*
+ * 8-bit floating-point blocks: e4m3 or e5m2 codes (OCP 8-bit floating point: e4m3 has no
+ * infinities, 448 is its largest value; e5m2's is 57344) with one power-of-two scale for
+ * each 128 consecutive values of a row (the last block of a row may be shorter).
+ *
+ * A tensor of rows x len:
+ *   codes : uint8 [rows][128 * blocks], blocks = len / 128 rounded up; zeros behind a
+ *           row's last value.  16-byte aligned.
+ *   exp   : uint8 [rows][blocks rounded up to a multiple of 4], zeros behind a row's last
+ *           block: a block's values are its codes' times 2^(exp - 127).  4-byte aligned.
+ *
+ * A block's scale is the least power of two (not below 2^-127) by which its largest
+ * value is at most the format's; codes are the nearest ones to value / scale, ties to
+ * even.  FP32 subnormals read as zero.  Infinities and NaN are stored as NaN, do not
+ * count for the scale, and set bit 0 of the status word.
+ * len is at most 2^23 (BFP_E_UNSUPPORTED beyond).
+ */
+typedef enum {
+  BFP_FP8_E4M3 = 0,
+  BFP_FP8_E5M2 = 1
+} bfp_fp8_t;
+
+/* Types of what passes between a norm, the products and the update. */
+typedef enum {
+  BFP_F32 = 0,
+  BFP_BF16 = 1
+} bfp_type_t;
+
+/* Host-side sizes of the two arrays of a rows x len tensor. */
+int bfp_fp8_sizes(int64_t rows, int64_t len, size_t* code_bytes, size_t* exp_bytes);
+
+/*
+ * bfp_quantize_fp8 -- FP32 or BF16 -> 8-bit blocks.
+ *   x           : x_type [R][C], row-major, contiguous, aligned to a value (16 bytes for
+ *                 full speed).
+ *   group_axis  : 1 -> blocks along the rows (rows = R, len = C); 0 -> down the columns,
+ *                 written transposed (rows = C, len = R), as bfp_quantize.
+ *   status_word : optional device uint32.
+ * Outputs must not overlap x or each other (BFP_E_ARG).
+ */
+int bfp_quantize_fp8(const void* x, int x_type, int64_t R, int64_t C, int group_axis, int format, uint8_t* codes,
+                     uint8_t* exp, uint32_t* status_word, void* stream);
+
+/* bfp_quantize_fp8_dual -- both, from one read: codes_r and exp_r as group_axis 1 writes
+ * them, codes_c and exp_c as group_axis 0. */
+int bfp_quantize_fp8_dual(const void* x, int x_type, int64_t R, int64_t C, int format, uint8_t* codes_r,
+                          uint8_t* exp_r, uint8_t* codes_c, uint8_t* exp_c, uint32_t* status_word, void* stream);
+
+/* bfp_dequantize_fp8 -- the values, FP32 [rows][len] (exact, but for those below FP32's
+ * range, which are rounded). */
+int bfp_dequantize_fp8(const uint8_t* codes, const uint8_t* exp, int64_t rows, int64_t len, int format, float* y,
+                       void* stream);
+
+/*
+ * bfp_gemm_fp8 -- C = A . B^T, c_type [M][N], of 8-bit tensors A [M][K] and B [N][K] in
+ * either format each:
+ *   C[i][j] = sum over blocks of 2^(ea + eb - 254) sum over the block of a b
+ * Products are exact.  Of eight consecutive ones what lies below 2^-13 of the largest may
+ * be dropped (the matrix instruction's alignment: at most 2^-10 of the largest in all,
+ * about 2^-14 of the products' size at random, whatever K); sums from there on are FP32,
+ * rounded once for BF16.  Their order depends on the sizes and on whether the workspace
+ * has room.
+ *   ldc       : row stride of C, at least N (BFP_E_SHAPE otherwise); C aligned to a value.
+ *   workspace : bfp_gemm_fp8_ws_size bytes (0 for most products), 16-byte aligned, with
+ *               which K is summed in parts where the output alone has too little work for
+ *               the card; overwritten.  With less, or NULL, the product runs whole.
+ * C and the workspace must not overlap what is read, or each other (BFP_E_ARG).
+ */
+int bfp_gemm_fp8_ws_size(int64_t M, int64_t N, int64_t K, size_t* workspace_bytes);
+int bfp_gemm_fp8(const uint8_t* a_codes, const uint8_t* a_exp, int a_format, const uint8_t* b_codes,
+                 const uint8_t* b_exp, int b_format, int64_t M, int64_t N, int64_t K, void* C, int c_type,
+                 int64_t ldc, void* workspace, size_t workspace_bytes, void* stream);
+
+/* bfp_gemm_fp8_route -- the kernel of a product with that workspace: its tile and the
+ * parts of K.  Host only, nothing is launched.  For tests and tuning. */
+int bfp_gemm_fp8_route(int64_t M, int64_t N, int64_t K, size_t workspace_bytes, int* tile, int* parts);
+
+/*
+ * bfp_rms_norm -- the root-mean-square norm of each row, with a residual's addition in
+ * front:
+ *   h = x + residual (x itself where residual is NULL), in FP32
+ *   r = (mean(h^2) + eps)^(-1/2),  y = h r weight
+ * r and y are computed in 64 bits and rounded once to FP32.
+ *   x           : x_type [rows][d], contiguous; d at most 16384 (BFP_E_UNSUPPORTED beyond).
+ *   residual    : FP32 [rows][d], or NULL.
+ *   weight      : FP32 [d].   eps : finite, not negative.
+ *   h           : optional FP32 [rows][d]; may be an FP32 x or residual (in place).
+ *   rstd        : optional FP32 [rows], r for the gradient.
+ *   y           : FP32 [rows][d]; may be an FP32 x or residual (where h is not).
+ * All aligned to a value (16 bytes for full speed).  Other overlaps are BFP_E_ARG.
+ *
+ * bfp_rms_norm_fp8 and bfp_rms_norm_bfp -- the same with y converted on the way, as
+ * bfp_quantize_fp8 and bfp_quantize (groups of 16; d a multiple of 16, BFP_E_SHAPE
+ * otherwise) convert it along its rows, byte for byte.
+ */
+int bfp_rms_norm(const void* x, int x_type, const float* residual, const float* weight, int64_t rows, int64_t d, double eps,
+                 float* h, float* rstd, float* y, void* stream);
+int bfp_rms_norm_fp8(const void* x, int x_type, const float* residual, const float* weight, int64_t rows, int64_t d, double eps,
+                     float* h, float* rstd, int format, uint8_t* codes, uint8_t* exp, uint32_t* status_word,
+                     void* stream);
+int bfp_rms_norm_bfp(const void* x, int x_type, const float* residual, const float* weight, int64_t rows, int64_t d, double eps,
+                     float* h, float* rstd, int m_bits, int round_mode, uint64_t seed, uint8_t* mant, uint8_t* exp,
+                     uint32_t* status_word, void* stream);
+
+/*
+ * bfp_rms_norm_grad -- its gradients, with u = weight dy:
+ *   dx = r u - h r^3 mean(u h) + dresidual,  dweight = sum over the rows of dy h r
+ *   dy        : dy_type [rows][d].   h, rstd : of the forward pass.   dresidual : optional, the gradient that reaches h
+ *               beside the norm; dx is the gradient of x and of the residual alike.
+ *   dx        : FP32 [rows][d]; may be an FP32 dy or dresidual (in place).
+ *   dweight   : FP32 [d]; zeros where rows is 0.
+ *   workspace : bfp_rms_norm_grad_ws_size bytes, 4-byte aligned; overwritten.
+ * Sums along rows and over rows are 64 bits; their order depends on the sizes alone.
+ * Other overlaps are BFP_E_ARG.
+ */
+int bfp_rms_norm_grad_ws_size(int64_t rows, int64_t d, size_t* workspace_bytes);
+int bfp_rms_norm_grad(const void* dy, int dy_type, const float* h, const float* rstd, const float* weight,
+                      const float* dresidual, int64_t rows, int64_t d, float* dx, float* dweight, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/*
+ * bfp_sum_squares -- the sum of squares over a list of FP32 or BF16 tensors, in 64 bits (squares
+ * are exact there and none is out of range) and an order that depends on the sizes alone.
+ *   tensors, sizes : HOST arrays of `count` device pointers (contiguous data of `type`,
+ *                    aligned to a value) and numbers of values; read before the call returns.
+ *   sumsq          : one double.   workspace : bfp_sum_squares_ws_size bytes, 8-byte
+ *                    aligned; overwritten.
+ * Sums of several cards or shards add up before bfp_clip_gradients.
+ */
+int bfp_sum_squares_ws_size(const int64_t* sizes, int64_t count, size_t* workspace_bytes);
+int bfp_sum_squares(const void* const* tensors, int type, const int64_t* sizes, int64_t count, double* sumsq,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * bfp_clip_gradients -- out[i] = tensors[i] * min(1, max_norm / norm), norm = sqrt(*sumsq):
+ * factor and products in 64 bits, rounded to FP32 (and from there to BF16).
+ *   out      : HOST array of device pointers; out[i] may be tensors[i] (in place: nothing
+ *              moves then unless norm is above max_norm).  Other overlaps of an output with
+ *              an input or another output are BFP_E_ARG.
+ *   max_norm : not negative, not NaN.   sumsq : as bfp_sum_squares writes it.
+ *   norm     : one double, written.
+ * A norm that is infinite or NaN scales nothing: the tensors keep the values that made it.
+ */
+int bfp_clip_gradients(const void* const* tensors, void* const* out, int type, const int64_t* sizes, int64_t count,
+                       double max_norm, const double* sumsq, double* norm, void* stream);
 
 #ifdef __cplusplus
 }

@@ -27,7 +27,9 @@ __all__ = ["BFPTensor", "BFPError", "quantize", "quantize_dual", "weight_update"
            "PackedBFPTensor", "packed_sizes", "quantize_packed", "dequantize_packed", "gemm_packed", "repack",
            "gemm_ws_size", "ExpertPlan", "expert_plan", "quantize_experts", "gemm_experts", "gemm_experts_grad",
            "combine_experts", "combine_experts_grad", "orthogonalize", "orthogonal_update",
-           "orthogonalize_ws_size"]
+           "orthogonalize_ws_size", "FP8Tensor", "quantize_fp8", "quantize_fp8_dual", "dequantize_fp8", "gemm_fp8",
+           "gemm_fp8_ws_size", "rms_norm", "rms_norm_grad", "TensorList", "tensor_list", "sum_squares",
+           "clip_gradients"]
 
 ROUNDING = {"nearest": 0, "stochastic": 1, "truncate": 2}
 
@@ -853,3 +855,7 @@ def orthogonal_update(grad: torch.Tensor, momentum: torch.Tensor, beta: float = 
             raise ValueError("momentum_out has the wrong shape")
     o = _orthogonalize(grad, momentum, momentum_out, beta, nesterov, steps, eps, out, workspace)
     return o, momentum_out
+
+
+from .layer import (FP8Tensor, TensorList, clip_gradients, dequantize_fp8, gemm_fp8, gemm_fp8_ws_size,  # noqa: E402
+                    quantize_fp8, quantize_fp8_dual, rms_norm, rms_norm_grad, sum_squares, tensor_list)

@@ -68,9 +68,24 @@ SIGNATURES = {
                                 [ctypes.POINTER(ctypes.c_int64)]),
     "bfp_orthogonalize": (_I, [_P, _P, _P, ctypes.c_float, _I, _I64, _I64, _I64, _I, ctypes.c_float, _P, _P,
                                ctypes.c_size_t, _P]),
+    "bfp_fp8_sizes": (_I, [_I64, _I64, ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(ctypes.c_size_t)]),
+    "bfp_quantize_fp8": (_I, [_P, _I, _I64, _I64, _I, _I, _P, _P, _P, _P]),
+    "bfp_quantize_fp8_dual": (_I, [_P, _I, _I64, _I64, _I, _P, _P, _P, _P, _P, _P]),
+    "bfp_dequantize_fp8": (_I, [_P, _P, _I64, _I64, _I, _P, _P]),
+    "bfp_gemm_fp8_ws_size": (_I, [_I64, _I64, _I64, ctypes.POINTER(ctypes.c_size_t)]),
+    "bfp_gemm_fp8_route": (_I, [_I64, _I64, _I64, ctypes.c_size_t] + [ctypes.POINTER(ctypes.c_int)] * 2),
+    "bfp_gemm_fp8": (_I, [_P, _P, _I, _P, _P, _I, _I64, _I64, _I64, _P, _I, _I64, _P, ctypes.c_size_t, _P]),
+    "bfp_rms_norm": (_I, [_P, _I, _P, _P, _I64, _I64, ctypes.c_double, _P, _P, _P, _P]),
+    "bfp_rms_norm_fp8": (_I, [_P, _I, _P, _P, _I64, _I64, ctypes.c_double, _P, _P, _I, _P, _P, _P, _P]),
+    "bfp_rms_norm_bfp": (_I, [_P, _I, _P, _P, _I64, _I64, ctypes.c_double, _P, _P, _I, _I, _U64, _P, _P, _P, _P]),
+    "bfp_rms_norm_grad_ws_size": (_I, [_I64, _I64, ctypes.POINTER(ctypes.c_size_t)]),
+    "bfp_rms_norm_grad": (_I, [_P, _I, _P, _P, _P, _P, _I64, _I64, _P, _P, _P, ctypes.c_size_t, _P]),
+    "bfp_sum_squares_ws_size": (_I, [_P, _I64, ctypes.POINTER(ctypes.c_size_t)]),
+    "bfp_sum_squares": (_I, [_P, _I, _P, _I64, _P, _P, ctypes.c_size_t, _P]),
+    "bfp_clip_gradients": (_I, [_P, _P, _I, _P, _I64, ctypes.c_double, _P, _P, _P]),
     "bfp_adaptive_mantissa": (_I, [ctypes.c_double, ctypes.c_double, ctypes.c_double]),
 }
-ABI_VERSION = 9
+ABI_VERSION = 10
 
 _lock = threading.Lock()
 _lib = None

@@ -21,7 +21,8 @@ ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 ARCH = "gfx950"
 SOURCES = ["quantize.hip", "packed.hip", "repack.hip", "gemm_mx.hip", "gemm_direct.hip", "gemm_direct_g32.hip",
            "gemm_parts.hip", "gemm_general.hip", "gemm_experts.hip", "gemm_direct_experts.hip", "experts.hip",
-           "orthogonalize.hip", "api.cpp"] + [
+           "orthogonalize.hip", "quantize_fp8.hip", "gemm_fp8.hip", "rms_norm.hip", "gradients.hip", "api.cpp",
+           "api_layer.cpp"] + [
     "gemm_mx_%s%s.hip" % (p, g) for g in ("", "_g32") for p in ("11", "12", "21", "22")] + [
     "gemm_mx_11n_%d%d.hip" % (fa, fb) for fa in (0, 1) for fb in (0, 1)] + [
     "gemm_mx_experts_%s.hip" % p for p in ("11", "12", "21", "22")]

@@ -4,7 +4,12 @@
 #include <hip/hip_runtime.h>
 
 #include "../../include/fastbfp.h"
+#include "checks.h"
 #include "launch.h"
+
+using fastbfp::aligned;
+using fastbfp::overlap;
+using fastbfp::status_of;
 
 namespace {
 
@@ -26,8 +31,6 @@ int check_tensor(int64_t rows, int64_t len, int g, int m) {
   return BFP_OK;
 }
 
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
 // Planes the GEMM reads for an operand stored at m_stored and used at m_use:
 // every stored plane, or only the high plane when the low chunk (2 bits for
 // m = 5, 6; 4 for m = 7, 8) is dropped.
@@ -36,8 +39,6 @@ int planes_used(int m_stored, int m_use) {
   if (m_stored > 4 && m_use == m_stored - fastbfp::low_chunk_bits(m_stored)) return 1;
   return 0;
 }
-
-int status_of(hipError_t e) { return e == hipSuccess ? BFP_OK : BFP_E_HIP; }
 
 // True when the block-scaled kernel (gemm_mx.h) takes the product: groups of
 // 16 or 32 and each operand at its stored width or with its low chunk plane
@@ -116,12 +117,6 @@ int check_experts_grad_shape(int a_m, int b_m, int experts, int64_t M, int64_t N
   if (!fast_path(a_m, b_m, 16, m_a, m_b)) return BFP_E_UNSUPPORTED;
   if (((M + 127) / 128) * ((N + 63) / 64) > 0x7fffffff / experts) return BFP_E_UNSUPPORTED;
   return BFP_OK;
-}
-
-// Whether the `an` bytes at a and the `bn` bytes at b share any (null: nothing there).
-bool overlap(const void* a, uint64_t an, const void* b, uint64_t bn) {
-  const uint64_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
-  return a && b && (p < q ? q - p < an && bn > 0 : p - q < bn && an > 0);
 }
 
 // Whether a weighted sum's output shares bytes with what its kernel reads.

@@ -1,0 +1,139 @@
+// fp8.h -- 8-bit floating-point blocks: e4m3 or e5m2 codes (OCP 8-bit floating point)
+// with one power-of-two scale for each 128 consecutive values of a row, the E8M0 block
+// scale of gfx950's MFMA of K = 128 (shared by its four blocks of 32).
+//
+// The scale of a block is the least power of two by which its largest value is at most
+// the format's, 448 = 1.75 * 2^8 (57344 = 1.75 * 2^15): with the FP32 exponent field E of
+// the largest magnitude, 2^(E - 127 - 8), or twice that where its fraction is above 0.75.
+// So no value is beyond the format, and codes are the hardware converter's nearest-even
+// ones of x / scale, an exact power-of-two scaling.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace fastbfp {
+
+namespace fp8 {
+
+enum { kE4M3 = 0, kE5M2 = 1 };  // (the MFMA's format codes; bfp_fp8_t)
+
+constexpr int kBlock = 128;
+
+__host__ __device__ constexpr int64_t blocks_of(int64_t len) { return (len + kBlock - 1) / kBlock; }
+// Bytes from one row's codes, or scales, to the next one's.
+__host__ __device__ constexpr int64_t code_pitch(int64_t len) { return blocks_of(len) * kBlock; }
+__host__ __device__ constexpr int64_t exp_pitch(int64_t len) { return (blocks_of(len) + 3) / 4 * 4; }
+
+typedef float v4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+// Magnitude bits of a value as the block's maximum takes them: subnormals, infinities
+// and NaN do not count.
+__device__ __forceinline__ uint32_t counted(uint32_t bits) {
+  const uint32_t a = bits & 0x7FFFFFFFu;
+  return a - 0x00800000u < 0x7F000000u ? a : 0u;
+}
+__device__ __forceinline__ bool finite(uint32_t bits) { return (bits & 0x7FFFFFFFu) < 0x7F800000u; }
+
+// The scale's byte (2^(byte - 127)) for the largest magnitude's bits.
+__device__ __forceinline__ uint32_t scale_of(uint32_t amax, int fmt) {
+  const int e = (int)(amax >> 23) + ((amax & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return (uint32_t)max(e - (fmt == kE4M3 ? 8 : 15), 0);
+}
+// 1 / scale, a power of two in FP32's range (the byte is at most 247).
+__device__ __forceinline__ float inverse(uint32_t scale) { return __uint_as_float((254u - scale) << 23); }
+
+// What the converter takes for x: subnormals as zero, infinities as NaN.
+__device__ __forceinline__ float ready(uint32_t bits, float inv) {
+  const uint32_t a = bits & 0x7FFFFFFFu;
+  if (a < 0x00800000u) bits &= 0x80000000u;
+  if (a >= 0x7F800000u) bits |= 0x7FC00000u;
+  return __uint_as_float(bits) * inv;
+}
+
+// Codes of four values.
+__device__ __forceinline__ uint32_t convert4(const u4& b, float inv, int fmt) {
+  const float x0 = ready(b[0], inv), x1 = ready(b[1], inv), x2 = ready(b[2], inv), x3 = ready(b[3], inv);
+  if (fmt == kE4M3) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x0, x1, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, lo, true);
+  }
+  const int lo = __builtin_amdgcn_cvt_pk_bf8_f32(x0, x1, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(x2, x3, lo, true);
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false));
+}
+// The maximum over the 32 lanes of a half wave, in all of them.
+__device__ __forceinline__ uint32_t max_half_wave(uint32_t v) {
+  v = max_dpp<0xB1>(v);   // quad_perm 1 0 3 2
+  v = max_dpp<0x4E>(v);   // quad_perm 2 3 0 1
+  v = max_dpp<0x141>(v);  // mirrored within eight lanes
+  v = max_dpp<0x140>(v);  // mirrored within sixteen
+  return max(v, (uint32_t)__shfl_xor((int)v, 16));
+}
+__device__ __forceinline__ uint32_t max4(const u4& b) {
+  return max(max(counted(b[0]), counted(b[1])), max(counted(b[2]), counted(b[3])));
+}
+
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+typedef uint16_t bf16_t;  // a BF16 value's bits, the upper half of an FP32's
+
+// Bits (FP32) of four values from `left` (of a row) on: those past the row's end are
+// zeros.  Rows of any length begin at any multiple of a value's bytes.
+__device__ __forceinline__ u4 load4(const float* p, int64_t left) {
+  typedef u4 __attribute__((aligned(4))) u4_any;
+  if (left >= 4) return *reinterpret_cast<const u4_any*>(p);
+  u4 v = u4{0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int t = 0; t < 3; ++t)
+    if (t < left) v[t] = __float_as_uint(p[t]);
+  return v;
+}
+__device__ __forceinline__ u4 load4(const bf16_t* p, int64_t left) {
+  typedef u2 __attribute__((aligned(2))) u2_any;
+  if (left >= 4) {
+    const u2 v = *reinterpret_cast<const u2_any*>(p);
+    return u4{v[0] << 16, v[0] & 0xFFFF0000u, v[1] << 16, v[1] & 0xFFFF0000u};
+  }
+  u4 v = u4{0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int t = 0; t < 3; ++t)
+    if (t < left) v[t] = (uint32_t)p[t] << 16;
+  return v;
+}
+// Stores them, rounded to the nearest (ties to even) for BF16.
+__device__ __forceinline__ void store4(float* p, const u4& v, int64_t left) {
+  typedef u4 __attribute__((aligned(4))) u4_any;
+  if (left >= 4) {
+    *reinterpret_cast<u4_any*>(p) = v;
+    return;
+  }
+#pragma unroll
+  for (int t = 0; t < 3; ++t)
+    if (t < left) p[t] = __uint_as_float(v[t]);
+}
+__device__ __forceinline__ u2 to_bf16(const u4& v) {
+  b4 b;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) b[t] = (__bf16)__uint_as_float(v[t]);
+  return __builtin_bit_cast(u2, b);
+}
+__device__ __forceinline__ void store4(bf16_t* p, const u4& v, int64_t left) {
+  typedef u2 __attribute__((aligned(2))) u2_any;
+  const u2 b = to_bf16(v);
+  if (left >= 4) {
+    *reinterpret_cast<u2_any*>(p) = b;
+    return;
+  }
+#pragma unroll
+  for (int t = 0; t < 3; ++t)
+    if (t < left) p[t] = (bf16_t)(b[t / 2] >> (16 * (t & 1)));
+}
+
+}  // namespace fp8
+
+}  // namespace fastbfp

@@ -215,4 +215,45 @@ hipError_t launch_orthogonalize(const float* grad, const float* momentum, float*
                                 bool nesterov, int64_t batch, int64_t rows, int64_t cols, int steps, float eps,
                                 float* out, uint8_t* ws, hipStream_t s);
 
+// 8-bit floating-point blocks (fp8.h, quantize_fp8.hip, gemm_fp8.hip).  group_axis as for
+// quantize; codes_r and exps_r may both be null.
+hipError_t launch_quantize_fp8(const void* x, bool bf16, int64_t R, int64_t C, int group_axis, int fmt, uint8_t* codes,
+                               uint8_t* exps, uint32_t* status, hipStream_t s);
+hipError_t launch_quantize_fp8_dual(const void* x, bool bf16, int64_t R, int64_t C, int fmt, uint8_t* codes_r, uint8_t* exps_r,
+                                    uint8_t* codes_c, uint8_t* exps_c, uint32_t* status, hipStream_t s);
+hipError_t launch_dequantize_fp8(const uint8_t* codes, const uint8_t* exps, int64_t rows, int64_t len, int fmt,
+                                 float* y, hipStream_t s);
+// How a product runs: the workgroup tile's edge, and K in `parts` parts of `part_slabs`
+// blocks (parts > 1, where there is room: into the workspace, added up afterwards).
+struct Fp8Plan {
+  int tile, part_slabs, parts;
+};
+Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool room);
+int64_t fp8_plan_ws(const Fp8Plan& plan, int64_t M, int64_t N);  // bytes
+hipError_t launch_gemm_fp8(const Fp8Plan& plan, const uint8_t* a, const uint8_t* ea, int fa, const uint8_t* b,
+                           const uint8_t* eb, int fb, int64_t M, int64_t N, int64_t K, void* C, bool bf16, int64_t ldc,
+                           float* ws, hipStream_t s);
+
+// The norm (rms_norm.hip).  residual, h and rstd may be null.
+constexpr int64_t kMaxNorm = 16384;  // values of a row
+hipError_t launch_rms_norm(const void* x, bool bf16, const float* residual, const float* w, int64_t rows, int64_t d, double eps,
+                           float* h, float* rstd, float* y, hipStream_t s);
+hipError_t launch_rms_norm_fp8(const void* x, bool bf16, const float* residual, const float* w, int64_t rows, int64_t d,
+                               double eps, float* h, float* rstd, int fmt, uint8_t* codes, uint8_t* exps,
+                               uint32_t* status, hipStream_t s);
+hipError_t launch_rms_norm_bfp(const void* x, bool bf16, const float* residual, const float* w, int64_t rows, int64_t d,
+                               double eps, float* h, float* rstd, int m, int mode, uint64_t seed, uint8_t* mant,
+                               uint8_t* exps, uint32_t* status, hipStream_t s);
+int64_t rms_norm_grad_parts(int64_t rows, int64_t d);  // rows of d values in the workspace
+hipError_t launch_rms_norm_grad(const void* dy, bool bf16, const float* h, const float* rstd, const float* w,
+                                const float* dresidual, int64_t rows, int64_t d, float* dx, float* dw, float* ws,
+                                hipStream_t s);
+
+// The norm over a list of tensors and their scaling (gradients.hip).
+int64_t gradient_pieces(const int64_t* sizes, int64_t count);  // doubles of the workspace
+hipError_t launch_sum_squares(const void* const* in, bool bf16, const int64_t* sizes, int64_t count, double* sumsq, double* ws,
+                              hipStream_t s);
+hipError_t launch_scale_gradients(const void* const* in, void* const* out, bool bf16, const int64_t* sizes, int64_t count,
+                                  double max_norm, const double* sumsq, double* norm, hipStream_t s);
+
 }  // namespace fastbfp

@@ -1,0 +1,207 @@
+// quantize_fp8.hip -- FP32 -> 8-bit floating-point blocks (fp8.h) along either axis, or
+// both from one read, and the inverse.  HBM-bound: 4 bytes read and 1 + 1/128 written a
+// value (2 + 1/64 with both).
+#include "fp8.h"
+#include "launch.h"
+
+namespace fastbfp {
+
+namespace fp8 {
+
+// Blocks along the rows.  Half a wave takes four blocks of a row, a lane four values of
+// each: every load reads 512 contiguous bytes, every store writes a block's 128, and
+// the four scales leave as one dword.
+template <int FMT, class T>
+__global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int64_t len, uint32_t quads_row,
+                                                  int64_t quads, uint8_t* __restrict__ codes,
+                                                  uint8_t* __restrict__ exps, uint32_t* status) {
+  const int64_t q = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (q >= quads) return;
+  const int lane = threadIdx.x & 31;
+  const int64_t row = q / quads_row;
+  const int64_t c0 = (q - row * quads_row) * (4 * kBlock) + 4 * lane;
+  const T* src = x + row * len;
+  u4 v[4];
+#pragma unroll
+  for (int b = 0; b < 4; ++b) v[b] = load4(src + c0 + b * kBlock, len - (c0 + b * kBlock));
+  uint32_t scales = 0, bad = 0;
+  uint8_t* out = codes + row * code_pitch(len);
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    const uint32_t s = scale_of(max_half_wave(max4(v[b])), FMT);
+    scales |= s << (8 * b);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) bad |= finite(v[b][t]) ? 0u : 1u;
+    const uint32_t w = convert4(v[b], inverse(s), FMT);
+    if (c0 - 4 * lane + b * kBlock < len) *reinterpret_cast<uint32_t*>(out + c0 + b * kBlock) = w;
+  }
+  if (lane == 0) *reinterpret_cast<uint32_t*>(exps + row * exp_pitch(len) + (c0 / kBlock)) = scales;
+  if (status && bad) atomicOr(status, 1u);
+}
+
+// Blocks down the columns (transposed: output row c is column c), and with ROWS also
+// along the rows, by tiles of 128 x 128 in LDS: a tile holds a block of each of its rows
+// and of each of its columns.
+constexpr int kStride = kBlock + 4;     // of a tile's row in LDS, floats
+constexpr int kCodeStride = kBlock + 16;  // of a column's codes, bytes
+
+template <int FMT, bool ROWS, class T>
+__global__ __launch_bounds__(256) void k_fp8_tiles(const T* __restrict__ x, int64_t R, int64_t C, uint32_t tiles_c,
+                                                   uint8_t* __restrict__ codes_r, uint8_t* __restrict__ exps_r,
+                                                   uint8_t* __restrict__ codes_c, uint8_t* __restrict__ exps_c,
+                                                   uint32_t* status) {
+  __shared__ __attribute__((aligned(16))) float tile[kBlock * kStride];
+  __shared__ uint32_t top[2][kBlock];
+  const int tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
+  const int64_t r0 = (int64_t)tr * kBlock, c0 = (int64_t)tc * kBlock;
+  const int half = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint32_t bad = 0;
+#pragma unroll 4
+  for (int i = 0; i < kBlock / 8; ++i) {
+    const int r = i * 8 + half;
+    u4 v = u4{0u, 0u, 0u, 0u};
+    if (r0 + r < R) v = load4(x + (r0 + r) * C + c0 + 4 * lane, C - (c0 + 4 * lane));
+#pragma unroll
+    for (int t = 0; t < 4; ++t) bad |= finite(v[t]) ? 0u : 1u;
+    *reinterpret_cast<u4*>(&tile[r * kStride + 4 * lane]) = v;
+    if constexpr (ROWS) {
+      const uint32_t s = scale_of(max_half_wave(max4(v)), FMT);
+      const uint32_t w = convert4(v, inverse(s), FMT);
+      if (r0 + r < R) {
+        *reinterpret_cast<uint32_t*>(codes_r + (r0 + r) * code_pitch(C) + c0 + 4 * lane) = w;
+        uint8_t* e = exps_r + (r0 + r) * exp_pitch(C) + tc;
+        if (lane == 0) *e = (uint8_t)s;
+        // (the scales behind a row's last block are zeros)
+        if (tc + 1 == (int)tiles_c && lane > 0 && lane < (int)(exp_pitch(C) - tc)) e[lane] = 0;
+      }
+    }
+  }
+  __syncthreads();
+  const int c = threadIdx.x & 127, h = threadIdx.x >> 7;
+  u4 v[16];
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[i][t] = __float_as_uint(tile[(64 * h + 4 * i + t) * kStride + c]);
+    m = max(m, max4(v[i]));
+  }
+  top[h][c] = m;
+  __syncthreads();  // (also: the tile is read)
+  const uint32_t s = scale_of(max(top[0][c], top[1][c]), FMT);
+  const float inv = inverse(s);
+  uint8_t* out = reinterpret_cast<uint8_t*>(tile);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    u4 w;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) w[t] = convert4(v[4 * i + t], inv, FMT);
+    *reinterpret_cast<u4*>(out + c * kCodeStride + 64 * h + 16 * i) = w;
+  }
+  if (c0 + c < C) {
+    uint8_t* e = exps_c + (c0 + c) * exp_pitch(R) + tr;
+    if (h == 0) *e = (uint8_t)s;
+    else if (r0 + kBlock >= R)
+      for (int k = 1; k < (int)(exp_pitch(R) - tr); ++k) e[k] = 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int cc = i * 32 + (threadIdx.x >> 3), at = (threadIdx.x & 7) * 16;
+    if (c0 + cc < C)
+      *reinterpret_cast<u4*>(codes_c + (c0 + cc) * code_pitch(R) + r0 + at) =
+          *reinterpret_cast<const u4*>(out + cc * kCodeStride + at);
+  }
+  if (status && bad) atomicOr(status, 1u);
+}
+
+// The values: codes times their block's scale (exact unless below FP32's range).
+template <int FMT>
+__global__ __launch_bounds__(256) void k_fp8_values(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ exps,
+                                                    int64_t len, int64_t words_row, int64_t words,
+                                                    float* __restrict__ y) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= words) return;
+  const int64_t row = i / words_row, k = (i - row * words_row) * 4;
+  const int w = *reinterpret_cast<const int*>(codes + row * code_pitch(len) + k);
+  const int e = (int)exps[row * exp_pitch(len) + k / kBlock] - 127;
+  float f[4];
+  if constexpr (FMT == kE4M3) {
+    f[0] = __builtin_amdgcn_cvt_f32_fp8(w, 0), f[1] = __builtin_amdgcn_cvt_f32_fp8(w, 1);
+    f[2] = __builtin_amdgcn_cvt_f32_fp8(w, 2), f[3] = __builtin_amdgcn_cvt_f32_fp8(w, 3);
+  } else {
+    f[0] = __builtin_amdgcn_cvt_f32_bf8(w, 0), f[1] = __builtin_amdgcn_cvt_f32_bf8(w, 1);
+    f[2] = __builtin_amdgcn_cvt_f32_bf8(w, 2), f[3] = __builtin_amdgcn_cvt_f32_bf8(w, 3);
+  }
+  u4 v;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) v[t] = __float_as_uint(__builtin_ldexpf(f[t], e));
+  store4(y + row * len + k, v, len - k);
+}
+
+}  // namespace fp8
+
+namespace fp8 {
+
+template <int FMT, class T>
+hipError_t launch_rows(const T* x, int64_t R, int64_t C, uint8_t* codes, uint8_t* exps, uint32_t* status,
+                       hipStream_t s) {
+  const int64_t quads_row = (blocks_of(C) + 3) / 4, quads = R * quads_row;
+  hipLaunchKernelGGL((k_fp8_rows<FMT, T>), dim3((unsigned)((quads + 7) / 8)), dim3(256), 0, s, x, C,
+                     (uint32_t)quads_row, quads, codes, exps, status);
+  return hipGetLastError();
+}
+
+template <int FMT, class T>
+hipError_t launch_tiles(const T* x, int64_t R, int64_t C, uint8_t* codes_r, uint8_t* exps_r, uint8_t* codes_c,
+                        uint8_t* exps_c, uint32_t* status, hipStream_t s) {
+  const uint32_t tiles_c = (uint32_t)blocks_of(C);
+  const dim3 grid((unsigned)(blocks_of(R) * tiles_c));
+  if (codes_r)
+    hipLaunchKernelGGL((k_fp8_tiles<FMT, true, T>), grid, dim3(256), 0, s, x, R, C, tiles_c, codes_r, exps_r, codes_c,
+                       exps_c, status);
+  else
+    hipLaunchKernelGGL((k_fp8_tiles<FMT, false, T>), grid, dim3(256), 0, s, x, R, C, tiles_c, codes_r, exps_r, codes_c,
+                       exps_c, status);
+  return hipGetLastError();
+}
+
+}  // namespace fp8
+
+hipError_t launch_quantize_fp8(const void* x, bool bf16, int64_t R, int64_t C, int group_axis, int fmt, uint8_t* codes,
+                               uint8_t* exps, uint32_t* status, hipStream_t s) {
+  using namespace fp8;
+  if (group_axis == 0) return launch_quantize_fp8_dual(x, bf16, R, C, fmt, nullptr, nullptr, codes, exps, status, s);
+  const float* f = static_cast<const float*>(x);
+  const bf16_t* b = static_cast<const bf16_t*>(x);
+  if (fmt == kE4M3)
+    return bf16 ? launch_rows<kE4M3>(b, R, C, codes, exps, status, s) : launch_rows<kE4M3>(f, R, C, codes, exps, status, s);
+  return bf16 ? launch_rows<kE5M2>(b, R, C, codes, exps, status, s) : launch_rows<kE5M2>(f, R, C, codes, exps, status, s);
+}
+
+hipError_t launch_quantize_fp8_dual(const void* x, bool bf16, int64_t R, int64_t C, int fmt, uint8_t* codes_r,
+                                    uint8_t* exps_r, uint8_t* codes_c, uint8_t* exps_c, uint32_t* status,
+                                    hipStream_t s) {
+  using namespace fp8;
+  const float* f = static_cast<const float*>(x);
+  const bf16_t* b = static_cast<const bf16_t*>(x);
+  if (fmt == kE4M3)
+    return bf16 ? launch_tiles<kE4M3>(b, R, C, codes_r, exps_r, codes_c, exps_c, status, s)
+                : launch_tiles<kE4M3>(f, R, C, codes_r, exps_r, codes_c, exps_c, status, s);
+  return bf16 ? launch_tiles<kE5M2>(b, R, C, codes_r, exps_r, codes_c, exps_c, status, s)
+              : launch_tiles<kE5M2>(f, R, C, codes_r, exps_r, codes_c, exps_c, status, s);
+}
+
+hipError_t launch_dequantize_fp8(const uint8_t* codes, const uint8_t* exps, int64_t rows, int64_t len, int fmt,
+                                 float* y, hipStream_t s) {
+  using namespace fp8;
+  const int64_t words_row = (len + 3) / 4, words = rows * words_row;
+  const dim3 grid((unsigned)((words + 255) / 256));
+  if (fmt == kE4M3)
+    hipLaunchKernelGGL(k_fp8_values<kE4M3>, grid, dim3(256), 0, s, codes, exps, len, words_row, words, y);
+  else
+    hipLaunchKernelGGL(k_fp8_values<kE5M2>, grid, dim3(256), 0, s, codes, exps, len, words_row, words, y);
+  return hipGetLastError();
+}
+
+}  // namespace fastbfp

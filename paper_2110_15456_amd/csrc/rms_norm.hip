@@ -1,0 +1,349 @@
+// rms_norm.hip -- a residual's addition and the root-mean-square norm of the sum, with
+// the output left in FP32 or converted on the way (8-bit blocks or BFP groups of 16), and
+// the norm's gradients.
+//
+//   h = x + residual (FP32),  r = (mean(h^2) + eps)^(-1/2),  y = h r w
+// The mean, r and the product are 64 bits and y is rounded once to FP32: y is the formula's
+// value whatever the launch, and the converted output the conversion of that y.  (64-bit
+// multiplies and adds run at FP32's rate here, and the kernel waits for HBM.)
+// HBM-bound: x and the residual read once, h and the output written once.
+#include "fp8.h"
+#include "gemm_direct.h"
+#include "launch.h"
+
+namespace fastbfp {
+
+namespace norm {
+
+using fp8::load4;
+using fp8::store4;
+using fp8::u4;
+
+// Sum over the workgroup of NT threads, in all of them; the order depends on NT alone.
+template <int NT>
+__device__ __forceinline__ double block_sum(double v, double* red) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) v += red[i];
+  }
+  return v;
+}
+
+enum { kToF32 = 0, kToFp8 = 1, kToBfp = 2 };
+
+struct Args {
+  const void* x;  // FP32 or BF16
+  const float *residual, *w;
+  int64_t rows, d;
+  double eps;
+  float *h, *rstd, *y;  // (h and rstd may be null)
+  uint8_t *codes, *exps;
+  int fmt;
+  uint32_t* status;
+  direct::Out bfp;
+};
+
+// A workgroup of NT threads takes a row, thread t its values 4 (t + NT k) .. + 3.
+template <int NT, int NV, bool RES, int TO, class T>
+__global__ __launch_bounds__(NT) void k_rms_norm(Args p) {
+  __shared__ double red[NT > 64 ? NT / 64 : 1];
+  __shared__ __attribute__((aligned(16))) float stage[TO == kToBfp ? 4 * NT : 4];
+  const int64_t row = blockIdx.x, d = p.d;
+  const int t = threadIdx.x;
+  const T* x = static_cast<const T*>(p.x) + row * d;
+  u4 v[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) v[k] = load4(x + 4 * (t + NT * k), d - 4 * (t + NT * k));
+  if constexpr (RES) {
+    u4 z[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) z[k] = load4(p.residual + row * d + 4 * (t + NT * k), d - 4 * (t + NT * k));
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[k][i] = __float_as_uint(__uint_as_float(v[k][i]) + __uint_as_float(z[k][i]));
+    }
+  }
+  double sum = 0.0;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    if (p.h) store4(p.h + row * d + 4 * (t + NT * k), v[k], d - 4 * (t + NT * k));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const double a = (double)__uint_as_float(v[k][i]);
+      sum = __builtin_fma(a, a, sum);
+    }
+  }
+  sum = block_sum<NT>(sum, red);
+  const double r = 1.0 / sqrt(sum / (double)d + p.eps);
+  if (p.rstd && t == 0) p.rstd[row] = (float)r;
+  uint32_t bad = 0;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int64_t c = 4 * (t + NT * k);
+    const u4 w = load4(p.w + c, d - c);
+    u4 y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      y[i] = __float_as_uint((float)((double)__uint_as_float(v[k][i]) * r * (double)__uint_as_float(w[i])));
+    if constexpr (TO == kToF32) {
+      store4(p.y + row * d + c, y, d - c);
+    } else if constexpr (TO == kToFp8) {
+      if (c >= d)  // (past the end, where 0 r w may be NaN)
+        y = u4{0u, 0u, 0u, 0u};
+      else if (d - c < 4)
+#pragma unroll
+        for (int i = 1; i < 4; ++i) y[i] = c + i < d ? y[i] : 0u;
+      const uint32_t s = fp8::scale_of(fp8::max_half_wave(fp8::max4(y)), p.fmt);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bad |= fp8::finite(y[i]) ? 0u : 1u;
+      const int64_t block = c / fp8::kBlock;
+      if (block * fp8::kBlock < d)
+        *reinterpret_cast<uint32_t*>(p.codes + row * fp8::code_pitch(d) + c) = fp8::convert4(y, fp8::inverse(s), p.fmt);
+      if ((t & 31) == 0 && block < fp8::exp_pitch(d)) p.exps[row * fp8::exp_pitch(d) + block] = (uint8_t)s;
+    } else {
+      // each wave gathers its 256 consecutive values, 16 groups, and converts a group a lane
+      float* mine = stage + 256 * (t >> 6);
+      *reinterpret_cast<u4*>(mine + 4 * (t & 63)) = y;
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+      __builtin_amdgcn_wave_barrier();
+      const int64_t g0 = 16 * (int64_t)((t >> 6) + NT / 64 * k);  // the wave's first group
+      if ((t & 63) < 16 && 16 * (g0 + (t & 63)) < d) {
+        uint32_t b[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const u4 q = *reinterpret_cast<const u4*>(mine + 16 * (t & 63) + 4 * i);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) b[4 * i + e] = q[e];
+        }
+        bad |= direct::convert(b, row * (d / 16) + g0 + (t & 63), p.bfp) ? 1u : 0u;
+      }
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_s_waitcnt(0xC07F);
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+  if constexpr (TO != kToF32) {
+    if (TO == kToFp8 && t == 0 && NT * NV * 4 / fp8::kBlock < fp8::exp_pitch(d)) {
+      // (scales behind the last block that no thread's values reach)
+      for (int64_t b = NT * NV * 4 / fp8::kBlock; b < fp8::exp_pitch(d); ++b) p.exps[row * fp8::exp_pitch(d) + b] = 0;
+    }
+    if (p.status && bad) atomicOr(p.status, 1u);
+  }
+}
+
+// The gradients, for u = w dy and h, r of the forward pass:
+//   dx = r u - h r^3 mean(u h) (+ dresidual),  dw = sum over rows of dy h r
+// A workgroup takes rows b, b + gridDim, ...; its share of dw stays in registers, in 64
+// bits, and goes to part[b] in FP32.
+struct GradArgs {
+  const void* dy;  // FP32 or BF16
+  const float *h, *rstd, *w, *dresidual;
+  int64_t rows, d;
+  float *dx, *part;
+};
+template <int NT, int NV, bool RES, class T>
+__global__ __launch_bounds__(NT) void k_rms_norm_grad(GradArgs p) {
+  __shared__ double red[2][NT > 64 ? NT / 64 : 1];
+  const int64_t d = p.d;
+  const int t = threadIdx.x;
+  u4 w[NV];
+  double dw[NV][4];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    w[k] = load4(p.w + 4 * (t + NT * k), d - 4 * (t + NT * k));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dw[k][i] = 0.0;
+  }
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+    const float r = p.rstd[row];
+    u4 g[NV], h[NV], z[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int64_t c = 4 * (t + NT * k);
+      g[k] = load4(static_cast<const T*>(p.dy) + row * d + c, d - c);
+      h[k] = load4(p.h + row * d + c, d - c);
+      if constexpr (RES) z[k] = load4(p.dresidual + row * d + c, d - c);
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      float s4 = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float dy = __uint_as_float(g[k][i]), hv = __uint_as_float(h[k][i]);
+        s4 = __builtin_fmaf(dy * __uint_as_float(w[k][i]), hv, s4);
+        dw[k][i] += (double)(dy * (hv * r));
+      }
+      sum += (double)s4;
+    }
+    // (two places for the waves' sums: a wave may be a row ahead of one that still reads)
+    sum = block_sum<NT>(sum, red[turn]);
+    const float a = (float)((double)r * (double)r * (double)r * (sum / (double)d));
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int64_t c = 4 * (t + NT * k);
+      u4 o;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float u = __uint_as_float(g[k][i]) * __uint_as_float(w[k][i]);
+        float v = __builtin_fmaf(-__uint_as_float(h[k][i]), a, u * r);
+        if constexpr (RES) v += __uint_as_float(z[k][i]);
+        o[i] = __float_as_uint(v);
+      }
+      store4(p.dx + row * d + c, o, d - c);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int64_t c = 4 * (t + NT * k);
+    u4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __float_as_uint((float)dw[k][i]);
+    store4(p.part + (int64_t)blockIdx.x * d + c, o, d - c);
+  }
+}
+
+// dw[c] = the sum of part[b][c] over b, in 64 bits and a fixed order: 16 columns a
+// workgroup, 16 runs of rows each.
+__global__ __launch_bounds__(256) void k_rms_norm_join(const float* __restrict__ part, int parts, int64_t d,
+                                                       float* __restrict__ dw) {
+  __shared__ double red[16][17];
+  const int c = threadIdx.x & 15, run = threadIdx.x >> 4;
+  const int64_t col = (int64_t)blockIdx.x * 16 + c;
+  double v = 0.0;
+  if (col < d)
+    for (int b = run; b < parts; b += 16) v += (double)part[(int64_t)b * d + col];
+  red[run][c] = v;
+  __syncthreads();
+  if (run == 0 && col < d) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) v += red[i][c];
+    dw[col] = (float)v;
+  }
+}
+
+// Threads to a row and vectors to a thread.
+struct Shape {
+  int nt, nv;
+};
+Shape shape_of(int64_t d) {
+  const int nt = d <= 1024 ? 64 : d <= 4096 ? 256 : 1024;
+  const int64_t v = (d + 4 * nt - 1) / (4 * nt);
+  return {nt, v <= 1 ? 1 : v <= 2 ? 2 : 4};
+}
+
+template <int NT, int NV, class T>
+hipError_t launch_norm(const Args& a, int to, hipStream_t s) {
+  const dim3 grid((unsigned)a.rows);
+#define FASTBFP_NORM(RES, TO) hipLaunchKernelGGL((k_rms_norm<NT, NV, RES, TO, T>), grid, dim3(NT), 0, s, a)
+  if (a.residual) {
+    if (to == kToF32) FASTBFP_NORM(true, kToF32);
+    else if (to == kToFp8) FASTBFP_NORM(true, kToFp8);
+    else FASTBFP_NORM(true, kToBfp);
+  } else {
+    if (to == kToF32) FASTBFP_NORM(false, kToF32);
+    else if (to == kToFp8) FASTBFP_NORM(false, kToFp8);
+    else FASTBFP_NORM(false, kToBfp);
+  }
+#undef FASTBFP_NORM
+  return hipGetLastError();
+}
+template <int NT, class T>
+hipError_t launch_norm_nv(const Args& a, int nv, int to, hipStream_t s) {
+  return nv == 1   ? launch_norm<NT, 1, T>(a, to, s)
+         : nv == 2 ? launch_norm<NT, 2, T>(a, to, s)
+                   : launch_norm<NT, 4, T>(a, to, s);
+}
+template <class T>
+hipError_t launch_t(const Args& a, int to, hipStream_t s) {
+  const Shape f = shape_of(a.d);
+  return f.nt == 64    ? launch_norm_nv<64, T>(a, f.nv, to, s)
+         : f.nt == 256 ? launch_norm_nv<256, T>(a, f.nv, to, s)
+                       : launch_norm_nv<1024, T>(a, f.nv, to, s);
+}
+hipError_t launch(const Args& a, bool bf16, int to, hipStream_t s) {
+  return bf16 ? launch_t<fp8::bf16_t>(a, to, s) : launch_t<float>(a, to, s);
+}
+
+template <int NT, class T>
+void launch_grad(const GradArgs& a, int nv, int parts, hipStream_t s) {
+  const dim3 grid((unsigned)parts), block(NT);
+#define FASTBFP_GRAD(NV)                                                                    \
+  if (a.dresidual) hipLaunchKernelGGL((k_rms_norm_grad<NT, NV, true, T>), grid, block, 0, s, a); \
+  else hipLaunchKernelGGL((k_rms_norm_grad<NT, NV, false, T>), grid, block, 0, s, a)
+  if (nv == 1) {
+    FASTBFP_GRAD(1);
+  } else if (nv == 2) {
+    FASTBFP_GRAD(2);
+  } else {
+    FASTBFP_GRAD(4);
+  }
+#undef FASTBFP_GRAD
+}
+
+template <class T>
+void launch_grad_t(const GradArgs& a, int parts, hipStream_t s) {
+  const Shape f = shape_of(a.d);
+  if (f.nt == 64) launch_grad<64, T>(a, f.nv, parts, s);
+  else if (f.nt == 256) launch_grad<256, T>(a, f.nv, parts, s);
+  else launch_grad<1024, T>(a, f.nv, parts, s);
+}
+
+}  // namespace norm
+
+hipError_t launch_rms_norm(const void* x, bool bf16, const float* residual, const float* w, int64_t rows, int64_t d, double eps,
+                           float* h, float* rstd, float* y, hipStream_t s) {
+  norm::Args a{};
+  a.x = x, a.residual = residual, a.w = w, a.rows = rows, a.d = d, a.eps = eps, a.h = h, a.rstd = rstd, a.y = y;
+  return norm::launch(a, bf16, norm::kToF32, s);
+}
+
+hipError_t launch_rms_norm_fp8(const void* x, bool bf16, const float* residual, const float* w, int64_t rows, int64_t d,
+                               double eps, float* h, float* rstd, int fmt, uint8_t* codes, uint8_t* exps,
+                               uint32_t* status, hipStream_t s) {
+  norm::Args a{};
+  a.x = x, a.residual = residual, a.w = w, a.rows = rows, a.d = d, a.eps = eps, a.h = h, a.rstd = rstd;
+  a.fmt = fmt, a.codes = codes, a.exps = exps, a.status = status;
+  return norm::launch(a, bf16, norm::kToFp8, s);
+}
+
+hipError_t launch_rms_norm_bfp(const void* x, bool bf16, const float* residual, const float* w, int64_t rows, int64_t d,
+                               double eps, float* h, float* rstd, int m, int mode, uint64_t seed, uint8_t* mant,
+                               uint8_t* exps, uint32_t* status, hipStream_t s) {
+  norm::Args a{};
+  a.x = x, a.residual = residual, a.w = w, a.rows = rows, a.d = d, a.eps = eps, a.h = h, a.rstd = rstd;
+  a.status = status;
+  a.bfp = {mant, mant + rows * (d / 16) * plane_group_bytes(16, m, 0), exps, status, m, mode, (uint32_t)seed,
+           (uint32_t)(seed >> 32)};
+  return norm::launch(a, bf16, norm::kToBfp, s);
+}
+
+int64_t rms_norm_grad_parts(int64_t rows, int64_t d) {
+  (void)d;
+  return rows < 512 ? rows : 512;
+}
+
+hipError_t launch_rms_norm_grad(const void* dy, bool bf16, const float* h, const float* rstd, const float* w,
+                                const float* dresidual, int64_t rows, int64_t d, float* dx, float* dw, float* ws,
+                                hipStream_t s) {
+  const int parts = (int)rms_norm_grad_parts(rows, d);
+  if (rows > 0) {
+    const norm::GradArgs a{dy, h, rstd, w, dresidual, rows, d, dx, ws};
+    if (bf16) norm::launch_grad_t<fp8::bf16_t>(a, parts, s);
+    else norm::launch_grad_t<float>(a, parts, s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(norm::k_rms_norm_join, dim3((unsigned)((d + 15) / 16)), dim3(256), 0, s, ws, parts, d, dw);
+  return hipGetLastError();
+}
+
+}  // namespace fastbfp

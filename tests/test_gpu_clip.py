@@ -1,0 +1,100 @@
+"""The norm over a list of tensors and their clipping on the GPU, against 64 bits."""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2110_15456_amd as fb
+from paper_2110_15456_amd import synth
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def lists(sizes, seed=0, scale=1.0):
+    return [np.float32(synth.draw("grads", (n,), seed + i) * scale) for i, n in enumerate(sizes)]
+
+
+def total(xs):
+    return math.sqrt(math.fsum(math.fsum((x.astype(np.float64) ** 2).tolist()) for x in xs))
+
+
+SIZES = [[1], [0, 5], [3, 16384, 16385, 1], [70000], [1000] * 130, list(range(1, 300)), [200001, 7, 40000]]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("ratio", [0.5, 3.0])
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: "%dx%d" % (len(s), max(s)))
+def test_clip(sizes, ratio, dtype):
+    print(len(sizes), sum(sizes), ratio, dtype, flush=True)
+    # a rounding to the type: half a step, finfo.eps / 2 (a significand in [1, 2) of p bits has
+    # steps of 2^(1-p): 2^-24 for FP32's 24 bits, 2^-8 for BF16's 8), with FP32's in front of BF16's
+    half = 2.0 ** -24 * (1 + 1e-6) if dtype == torch.float32 else 2.0 ** -8 * (1 + 2.0 ** -15)
+    xs = lists(sizes)
+    if dtype == torch.bfloat16:
+        xs = [torch.from_numpy(x).to(dtype).float().numpy() for x in xs]
+    n = total(xs)
+    most = n / ratio
+    f = min(1.0, most / n)
+    gs = [torch.from_numpy(x).to(DEV).to(dtype) for x in xs]
+    sq = fb.sum_squares(gs)
+    # squares are exact; a sum of k of them is off by at most k half units of 64 bits
+    assert abs(float(sq) - n * n) <= (sum(sizes) + 1) * 2.0 ** -53 * n * n
+    # to other tensors, one bucket at odd places
+    bucket = torch.full((sum(sizes) + 2,), 9.0, device=DEV, dtype=dtype)
+    out = list(torch.split(bucket[1:-1], sizes))
+    held = fb.tensor_list(gs, out=out)
+    norm = fb.clip_gradients(held, most)
+    assert abs(float(norm) - n) <= (sum(sizes) + 3) * 2.0 ** -53 * n
+    for g, o, x in zip(gs, out, xs):
+        want = x.astype(np.float64) * f
+        assert np.array_equal(g.float().cpu().numpy(), x)
+        assert np.all(np.abs(o.float().cpu().numpy() - want) <= half * np.abs(want) + 2.0 ** -134)
+        if ratio < 1:
+            assert torch.equal(o, g)
+    assert float(bucket[0]) == 9.0 and float(bucket[-1]) == 9.0
+    # in place, the sum given
+    norm2 = fb.clip_gradients(gs, most, sumsq=sq)
+    assert torch.equal(norm2, norm)
+    for g, o in zip(gs, out):
+        assert torch.equal(g, o)
+
+
+def test_far_scales():
+    for scale in (1e-30, 1e30):
+        xs = lists([5000, 3], scale=scale)
+        gs = [torch.from_numpy(x).to(DEV) for x in xs]
+        n = total(xs)
+        assert abs(float(fb.clip_gradients(gs, 1e-3 * n)) - n) <= 1e-12 * n
+        assert abs(float(fb.sum_squares(gs)) ** 0.5 - 1e-3 * n) <= 1e-7 * 1e-3 * n
+
+
+def test_zero_and_largest_norms():
+    g = torch.zeros(100, device=DEV)
+    assert float(fb.clip_gradients([g], 1.0)) == 0.0 and not bool(g.any())
+    g = torch.ones(100, device=DEV)
+    assert float(fb.clip_gradients([g], math.inf)) == 10.0 and bool((g == 1).all())
+    assert float(fb.clip_gradients([g], 0.0)) == 10.0 and not bool(g.any())
+    e = torch.empty(0, device=DEV)
+    assert float(fb.sum_squares([e])) == 0.0 and float(fb.clip_gradients([e], 1.0)) == 0.0
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_a_norm_that_is_not_finite_scales_nothing(bad):
+    xs = lists([100, 50])
+    xs[1][7] = bad
+    gs = [torch.from_numpy(x).to(DEV) for x in xs]
+    norm = float(fb.clip_gradients(gs, 1e-6))
+    assert not math.isfinite(norm)
+    for g, x in zip(gs, xs):
+        assert np.array_equal(g.cpu().numpy(), x, equal_nan=True)
+
+
+def test_shapes_and_strides_of_a_model():
+    gs = [torch.randn(s, device=DEV) for s in ((3, 5), (7,), (2, 3, 4), ())]
+    n = math.sqrt(sum(float((g.double() ** 2).sum()) for g in gs))
+    assert abs(float(fb.clip_gradients(gs, 1.0)) - n) <= 1e-12 * n
+    assert abs(math.sqrt(sum(float((g.double() ** 2).sum()) for g in gs)) - 1.0) < 1e-6
