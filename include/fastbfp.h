@@ -824,9 +824,11 @@ int bfp_gemm_fp8(const uint8_t* a_codes, const uint8_t* a_exp, int a_format, con
                  const uint8_t* b_exp, int b_format, int64_t M, int64_t N, int64_t K, void* C, int c_type,
                  int64_t ldc, void* workspace, size_t workspace_bytes, void* stream);
 
-/* bfp_gemm_fp8_route -- the kernel of a product with that workspace: its tile and the
- * parts of K.  Host only, nothing is launched.  For tests and tuning. */
-int bfp_gemm_fp8_route(int64_t M, int64_t N, int64_t K, size_t workspace_bytes, int* tile, int* parts);
+/* bfp_gemm_fp8_route -- the kernel of a product with that workspace: the workgroup's tile,
+ * the waves that split its K (0: the tiled kernel) and the parts of K.  Host only, nothing
+ * is launched.  For tests and tuning. */
+int bfp_gemm_fp8_route(int64_t M, int64_t N, int64_t K, size_t workspace_bytes, int* rows, int* cols, int* waves,
+                       int* parts);
 
 /*
  * bfp_rms_norm -- the root-mean-square norm of each row, with a residual's addition in

@@ -73,7 +73,7 @@ SIGNATURES = {
     "bfp_quantize_fp8_dual": (_I, [_P, _I, _I64, _I64, _I, _P, _P, _P, _P, _P, _P]),
     "bfp_dequantize_fp8": (_I, [_P, _P, _I64, _I64, _I, _P, _P]),
     "bfp_gemm_fp8_ws_size": (_I, [_I64, _I64, _I64, ctypes.POINTER(ctypes.c_size_t)]),
-    "bfp_gemm_fp8_route": (_I, [_I64, _I64, _I64, ctypes.c_size_t] + [ctypes.POINTER(ctypes.c_int)] * 2),
+    "bfp_gemm_fp8_route": (_I, [_I64, _I64, _I64, ctypes.c_size_t] + [ctypes.POINTER(ctypes.c_int)] * 4),
     "bfp_gemm_fp8": (_I, [_P, _P, _I, _P, _P, _I, _I64, _I64, _I64, _P, _I, _I64, _P, ctypes.c_size_t, _P]),
     "bfp_rms_norm": (_I, [_P, _I, _P, _P, _I64, _I64, ctypes.c_double, _P, _P, _P, _P]),
     "bfp_rms_norm_fp8": (_I, [_P, _I, _P, _P, _I64, _I64, ctypes.c_double, _P, _P, _I, _P, _P, _P, _P]),

@@ -207,13 +207,15 @@ int bfp_gemm_fp8_ws_size(int64_t M, int64_t N, int64_t K, size_t* workspace_byte
   return BFP_OK;
 }
 
-int bfp_gemm_fp8_route(int64_t M, int64_t N, int64_t K, size_t workspace_bytes, int* tile, int* parts) {
+int bfp_gemm_fp8_route(int64_t M, int64_t N, int64_t K, size_t workspace_bytes, int* rows, int* cols, int* waves,
+                       int* parts) {
   const int st = check_product(M, N, K);
   if (st != BFP_OK) return st;
-  if (!tile || !parts || M == 0 || N == 0 || K == 0) return BFP_E_ARG;
+  if (!rows || !cols || !waves || !parts || M == 0 || N == 0 || K == 0) return BFP_E_ARG;
   fastbfp::Fp8Plan plan = fastbfp::fp8_plan(M, N, K, true);
   if ((int64_t)workspace_bytes < fastbfp::fp8_plan_ws(plan, M, N)) plan = fastbfp::fp8_plan(M, N, K, false);
-  *tile = plan.tile;
+  *rows = plan.rows, *cols = plan.cols;
+  *waves = plan.waves;
   *parts = plan.parts;
   return BFP_OK;
 }

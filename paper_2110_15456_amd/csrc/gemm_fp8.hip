@@ -8,6 +8,10 @@
 // beside another eight or the running sum); the eights' sums and C are FP32.  So C is off
 // by about 2^-14 of the products' size at random, whatever K: a fraction of BF16's
 // rounding, and 1/500 of what e4m3's rounding of a value does.
+#include <math.h>
+
+#include <type_traits>
+
 #include "fp8.h"
 #include "launch.h"
 
@@ -41,21 +45,56 @@ __device__ __forceinline__ int xcd_order(int bid, int n) {
   return xcd * (n / 8) + min(xcd, n % 8) + bid / 8;
 }
 
-// BM x BN tiles, WGM x WGN waves; a slab is one block of K, 128 bytes of every row,
-// brought by direct buffer -> LDS loads of 1 KB into one of two stages while the other
-// is computed on.  16-byte chunk c of row r sits at chunk c ^ ((r >> 1) & 7): 16 lanes
-// that read one chunk of 16 rows hit all 64 banks.  Rows past the end read zeros (the
-// buffer resources end at the last row).  A lane's scales are those of its rows, four
-// slabs in a dword.
-template <int BM, int BN, int WGM, int WGN, int FA, int FB, class T>
-__global__ __launch_bounds__(64 * WGM * WGN, 2) void k_gemm_fp8(Gemm p) {
-  constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 32, TN = WN / 32;
+// s_waitcnt's operand: vmcnt(n), and lgkmcnt(0) with `lds`.
+constexpr int wait_loads(int n, bool lds = false) { return (n & 15) | (n >> 4) << 14 | 7 << 4 | (lds ? 0 : 15) << 8; }
+
+// Asks for a step's LDS reads and LOADS loads evenly among its MFMAs: a wave's loads in one
+// run hold it up for as long as the L1 takes them, 64 cycles a KB.
+template <int TM, int TN, int LOADS>
+__device__ __forceinline__ void spread() {
+  if constexpr (TM * TN >= 4) {
+    constexpr int READS = (2 * (TM + TN) + TM * TN - 1) / (TM * TN), EACH = (LOADS + TM * TN - 1) / (TM * TN);
+#pragma unroll
+    for (int u = 0; u < TM * TN; ++u) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, LOADS ? 1 : 0);  // MFMA
+      if constexpr (LOADS > 0) __builtin_amdgcn_sched_group_barrier(0x010, EACH, 1);  // loads
+      __builtin_amdgcn_sched_group_barrier(0x100, READS, LOADS ? 1 : 0);  // LDS reads
+    }
+  }
+}
+
+// BM x BN tiles, 2 x 2 waves; a slab is one block of K, 128 bytes of every row, brought by
+// direct buffer -> LDS loads of 1 KB into one of two stages while the other is computed
+// on.  16-byte chunk c of row r sits at chunk c ^ ((r >> 1) & 7): 16 lanes that read one
+// chunk of 16 rows hit all 64 banks.  Rows past the end read zeros (the buffer resources
+// end at the last row).
+//
+// A slab is two steps of 64.  A step's fragments are read while the one before is
+// multiplied; between a slab's steps, when all of the slab is in registers, the waves
+// meet: the next slab has landed, and the loads of the one after it go to the stage that
+// was just read, a whole slab ahead of their use.
+//
+// Two stages, and on the 64 tile four: it serves products of so few tiles that a slab
+// takes as long as its loads do (1024 x 1024 x 8192 with two 34.8 us, with four 20.9; of 900
+// drawn products those on the 64 tile lose 1% with four alone).
+//
+// Measured: 4096 x 4096 x 16384 2.7 PFLOP/s, 8192 x 16384 x 4096 445 us, 2.47; a library's
+// FP8 product of 8192^3 reaches 2.64 on the same card.  The MFMAs alone, fed with nothing,
+// take 85% of that time (77% of the second's, which writes more): the clock falls under
+// them.  The 128 tile, two workgroups on a CU, is held to 1.95 by the LDS, which moves
+// 1.5 bytes for each of the 256 tile's.
+template <int BM, int BN, int FA, int FB, class T>
+__global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
+  constexpr int ST = BM == 64 ? 4 : 2;
+  constexpr int NW = 4, WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32;
   constexpr int OFF_B = BM * kBlock, STAGE = OFF_B + BN * kBlock;
-  static_assert((BM / 8) % NW == 0 && (BN / 8) % NW == 0 && NW % 2 == 0, "loads split evenly over the waves");
+  constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW;  // loads of a wave
   __shared__ __attribute__((aligned(128))) uint8_t stage0[STAGE];
   __shared__ __attribute__((aligned(128))) uint8_t stage1[STAGE];
+  __shared__ __attribute__((aligned(128))) uint8_t stage2[ST == 4 ? STAGE : 16];
+  __shared__ __attribute__((aligned(128))) uint8_t stage3[ST == 4 ? STAGE : 16];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const int wr = wave / WGN, wc = wave % WGN;
+  const int wr = wave >> 1, wc = wave & 1;
 
   const int tiles = p.tiles_m * p.tiles_n, id = xcd_order(blockIdx.x, gridDim.x), part = id / tiles, t = id % tiles;
   // bands of four tile rows, down each band's column first: the tiles that an XCD runs
@@ -65,103 +104,303 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void k_gemm_fp8(Gemm p) {
   const int slab0 = part * p.part_slabs, nslabs = min(p.part_slabs, p.slabs - slab0);
 
   const int arows = min(BM, p.M - row0), brows = min(BN, p.N - col0);
-  const rsrc_t ra = make_rsrc(p.a + (int64_t)row0 * p.pitch, (uint32_t)arows * p.pitch);
-  const rsrc_t rb = make_rsrc(p.b + (int64_t)col0 * p.pitch, (uint32_t)brows * p.pitch);
-  const rsrc_t rea = make_rsrc(p.ea + (int64_t)row0 * p.epitch, (uint32_t)arows * p.epitch);
-  const rsrc_t reb = make_rsrc(p.eb + (int64_t)col0 * p.epitch, (uint32_t)brows * p.epitch);
-
+  const uint8_t *pa = p.a + (int64_t)row0 * p.pitch, *pb = p.b + (int64_t)col0 * p.pitch;
+  const uint32_t size_a = (uint32_t)arows * p.pitch, size_b = (uint32_t)brows * p.pitch;
   v16 acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = v16{};
 
-  const uint32_t chunk = (uint32_t)((lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7)) * 16;
+  const uint32_t lane_off =
+      (uint32_t)(8 * wave + (lane >> 3)) * p.pitch + (uint32_t)((lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7)) * 16;
+  const uint32_t step_off = 8 * NW * p.pitch;  // from one of a wave's loads to the next
+  // (slabs behind the last one: the loads find an empty buffer and write zeros, so that the
+  // loop has no branch around them)
   auto issue = [&](uint8_t* stage, int s) __attribute__((always_inline)) {
-    const uint32_t k0 = (uint32_t)(slab0 + s) * kBlock + chunk;
+    const uint32_t k0 = (uint32_t)(slab0 + s) * kBlock;
+    const rsrc_t sa = make_rsrc(pa, s < nslabs ? size_a : 0u), sb = make_rsrc(pb, s < nslabs ? size_b : 0u);
 #pragma unroll
-    for (int u = 0; u < BM / 8 / NW; ++u) {
-      const int blk = wave + NW * u;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(stage + blk * 1024), 16,
-                                               (uint32_t)(8 * blk + (lane >> 3)) * p.pitch + k0, 0, 0, 0);
-    }
+    for (int u = 0; u < LA; ++u)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(sa, (lds_void*)(stage + (wave + NW * u) * 1024), 16, lane_off,
+                                               k0 + u * step_off, 0, 0);
 #pragma unroll
-    for (int u = 0; u < BN / 8 / NW; ++u) {
-      const int blk = wave + NW * u;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void*)(stage + OFF_B + blk * 1024), 16,
-                                               (uint32_t)(8 * blk + (lane >> 3)) * p.pitch + k0, 0, 0, 0);
-    }
+    for (int u = 0; u < LB; ++u)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(sb, (lds_void*)(stage + OFF_B + (wave + NW * u) * 1024), 16, lane_off,
+                                               k0 + u * step_off, 0, 0);
   };
   const int fr = lane & 31, fk = lane >> 5, fsw = (fr >> 1) & 7;
+  // (the chunks of a lane's 32 bytes of step h: 4 h + 2 fk and the one beside it)
+  const int at0 = fr * kBlock + (((2 * fk) ^ fsw) * 16), at1 = fr * kBlock + (((2 * fk + 1) ^ fsw) * 16);
   auto frag = [&](const uint8_t* tile, int r, int h) __attribute__((always_inline)) -> v8i {
-    const uint8_t* at = tile + (r + fr) * kBlock;
-    const u4 x = *reinterpret_cast<const u4*>(at + (((4 * h + 2 * fk) ^ fsw) * 16));
-    const u4 y = *reinterpret_cast<const u4*>(at + (((4 * h + 2 * fk + 1) ^ fsw) * 16));
+    const uint8_t* at = tile + r * kBlock;
+    const u4 x = *reinterpret_cast<const u4*>(at + (at0 ^ (64 * h)));
+    const u4 y = *reinterpret_cast<const u4*>(at + (at1 ^ (64 * h)));
     return v8i{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
   };
-  // the scales of slab s, one byte for each of the lane's rows
+  // the scales of four slabs from s on, for each of the lane's rows (their rows are whole
+  // dwords; behind the last slab: zeros)
   auto scales = [&](int s, int (&sa)[TM], int (&sb)[TN]) __attribute__((always_inline)) {
+    const rsrc_t ra = make_rsrc(p.ea + (int64_t)row0 * p.epitch, s < nslabs ? (uint32_t)arows * p.epitch : 0u);
+    const rsrc_t rb = make_rsrc(p.eb + (int64_t)col0 * p.epitch, s < nslabs ? (uint32_t)brows * p.epitch : 0u);
 #pragma unroll
     for (int i = 0; i < TM; ++i)
-      sa[i] = (int)__builtin_amdgcn_raw_buffer_load_b8(rea, (uint32_t)(wr * WM + 32 * i + fr) * p.epitch + slab0 + s, 0, 0);
+      sa[i] = (int)__builtin_amdgcn_raw_buffer_load_b32(ra, (uint32_t)(wr * WM + 32 * i + fr) * p.epitch, slab0 + s, 0);
 #pragma unroll
     for (int j = 0; j < TN; ++j)
-      sb[j] = (int)__builtin_amdgcn_raw_buffer_load_b8(reb, (uint32_t)(wc * WN + 32 * j + fr) * p.epitch + slab0 + s, 0, 0);
+      sb[j] = (int)__builtin_amdgcn_raw_buffer_load_b32(rb, (uint32_t)(wc * WN + 32 * j + fr) * p.epitch, slab0 + s, 0);
   };
+  v8i a[2][TM], b[2][TN];
   int sa[TM], sb[TN], na[TM], nb[TN];
-  auto step = [&](const uint8_t* cur, uint8_t* nxt, int s) __attribute__((always_inline)) {
-    // this wave's loads of slab s have landed and its reads of slab s - 1 are done
-    __builtin_amdgcn_s_waitcnt(0);
+  auto read = [&](const uint8_t* tile, int h, v8i (&fa)[TM], v8i (&fb)[TN]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j) fb[j] = frag(tile + OFF_B, wc * WN + 32 * j, h);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) fa[i] = frag(tile, wr * WM + 32 * i, h);
+  };
+  auto multiply = [&](const v8i (&fa)[TM], const v8i (&fb)[TN]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)  // (B first: a lane's quads are columns of a row)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j], fa[i], acc[i][j], FB, FA, 0, sb[j], 0, sa[i]);
+  };
+  // all but `younger` of this wave's loads have landed and its LDS reads are done, as are
+  // the other waves'
+  auto meet = [&](auto younger) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(wait_loads(decltype(younger)::value, true));
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+  };
+  constexpr std::integral_constant<int, 0> all{};
+  // slab s, the k-th of a run of ST: when its second step's fragments are read, slab s + 1
+  // has to have landed, while those of s + 2 .. s + ST - 1 (and the next run's scales,
+  // until they are older than slab s + 1) may be on the way
+  auto slab = [&](uint8_t* cur, uint8_t* nxt, auto kc, int s) __attribute__((always_inline)) {
+    constexpr int YOUNGER = (ST - 2) * (LA + LB) + (ST == 4 && decltype(kc)::value < 3 ? TM + TN : 0);
+    __builtin_amdgcn_sched_barrier(0);
+    read(cur, 1, a[1], b[1]);
+    multiply(a[0], b[0]);
+    spread<TM, TN, 0>();
+    __builtin_amdgcn_sched_barrier(0);
+    meet(std::integral_constant<int, YOUNGER>{});
+    issue(cur, s + ST);
+    read(nxt, 0, a[0], b[0]);  // (behind the last slab: what lies there, unused)
+    multiply(a[1], b[1]);
+    spread<TM, TN, LA + LB>();
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = (int)((uint32_t)sa[i] >> 8);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) sb[j] = (int)((uint32_t)sb[j] >> 8);
+  };
+  auto next_scales = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < TM; ++i) sa[i] = na[i];
 #pragma unroll
     for (int j = 0; j < TN; ++j) sb[j] = nb[j];
-    if (s + 1 < nslabs) {
-      scales(s + 1, na, nb);
-      issue(nxt, s + 1);
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      v8i b[TN];
-#pragma unroll
-      for (int j = 0; j < TN; ++j) b[j] = frag(cur + OFF_B, wc * WN + 32 * j, h);
-#pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const v8i a = frag(cur, wr * WM + 32 * i, h);
-#pragma unroll
-        for (int j = 0; j < TN; ++j)  // (B first: a lane's quads are columns of a row)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[j], a, acc[i][j], FB, FA, 0, sb[j], 0, sa[i]);
-      }
-    }
+    scales(s, na, nb);
   };
   scales(0, na, nb);
   issue(stage0, 0);
-  int s = 0;
-  for (; s + 2 <= nslabs; s += 2) {
-    step(stage0, stage1, s);
-    step(stage1, stage0, s + 1);
+  issue(stage1, 1);
+  if constexpr (ST == 4) {
+    issue(stage2, 2);
+    issue(stage3, 3);
   }
-  if (s < nslabs) step(stage0, stage1, s);
+  meet(std::integral_constant<int, (ST - 1) * (LA + LB)>{});
+  read(stage0, 0, a[0], b[0]);
+  if constexpr (ST == 2) {
+    for (int s = 0; s < nslabs; s += 2) {
+      if ((s & 2) == 0) next_scales(s + 4);
+      slab(stage0, stage1, std::integral_constant<int, 0>{}, s);
+      // (the 256 tile runs an odd slab's partner on zeros: around a branch here its
+      // fragments would not stay in registers)
+      if (BM == 256 || s + 1 < nslabs) slab(stage1, stage0, std::integral_constant<int, 1>{}, s + 1);
+    }
+  } else {
+    for (int s = 0; s < nslabs; s += 4) {
+      next_scales(s + 4);
+      slab(stage0, stage1, std::integral_constant<int, 0>{}, s);
+      if (s + 1 < nslabs) slab(stage1, stage2, std::integral_constant<int, 1>{}, s + 1);
+      if (s + 2 < nslabs) slab(stage2, stage3, std::integral_constant<int, 2>{}, s + 2);
+      if (s + 3 < nslabs) slab(stage3, stage0, std::integral_constant<int, 3>{}, s + 3);
+    }
+  }
 
-  // A lane holds columns 8 q + 4 fk .. + 3 of row fr of each 32 x 32 tile.
+  // A lane holds columns 8 q + 4 fk .. + 3 of row fr of each 32 x 32 tile.  32 rows of
+  // the wave's columns at a time go through its part of the first stage, so that rows
+  // leave as whole lines; 16-byte granule g of row r sits at g ^ swz(r), which spreads 16
+  // rows of one granule over all banks.
+  meet(all);
+  constexpr int G = WN / 4;  // granules of a row
+  float* tile = reinterpret_cast<float*>(stage0) + wave * (32 * WN);
+  auto swz = [](int r) __attribute__((always_inline)) -> int { return G == 8 ? (r >> 1) & 7 : r & 15; };
   T* C = static_cast<T*>(p.c) + part * p.part_stride;
+  // C past the caches where its rows are whole lines (8192 x 16384 x 4096: 475 -> 445 us),
+  // but for sums that are read again
+  const bool lines = p.part_stride == 0 && ((p.ldc * sizeof(T)) | reinterpret_cast<uintptr_t>(C)) % 128 == 0;
+  constexpr int V = 16 / sizeof(T), LR = WN / V, RI = 64 / LR;  // a lane's values, lanes of a row, rows at a time
+  const int c = col0 + wc * WN + lane % LR * V;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    const int r = row0 + wr * WM + 32 * i + fr;
-    if (r >= p.M) continue;
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int c = col0 + wc * WN + 32 * j + 8 * q + 4 * fk;
-        u4 v;
+        v4 v;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) v[t] = __float_as_uint(acc[i][j][4 * q + t]);
-        store4(C + r * p.ldc + c, v, p.N - c);
+        for (int t = 0; t < 4; ++t) v[t] = acc[i][j][4 * q + t];
+        *reinterpret_cast<v4*>(tile + fr * WN + ((8 * j + 2 * q + fk) ^ swz(fr)) * 4) = v;
       }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int it = 0; it < 32 / RI; ++it) {
+      const int r = it * RI + lane / LR, g = lane % LR * (V / 4), row = row0 + wr * WM + 32 * i + r;
+      const u4 x = *reinterpret_cast<const u4*>(tile + r * WN + (g ^ swz(r)) * 4);
+      u4 y = u4{0u, 0u, 0u, 0u};
+      if constexpr (V == 8) y = *reinterpret_cast<const u4*>(tile + r * WN + ((g + 1) ^ swz(r)) * 4);
+      if (row >= p.M) continue;
+      T* o = C + row * p.ldc + c;
+      if (lines && c + V <= p.N) {
+        if constexpr (V == 4) {
+          __builtin_nontemporal_store(x, reinterpret_cast<u4*>(o));
+        } else {
+          const u2 lo = to_bf16(x), hi = to_bf16(y);
+          __builtin_nontemporal_store(u4{lo[0], lo[1], hi[0], hi[1]}, reinterpret_cast<u4*>(o));
+        }
+      } else if constexpr (V == 4) {
+        store4(o, x, p.N - c);
+      } else {
+        store8(o, x, y, p.N - c);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Few rows of A: a workgroup takes 16 RM rows x 16 RN columns, and its waves split K: a wave
+// takes every waves-th run of four slabs.  Each keeps four slabs of its own on the way to
+// its own part of LDS, so that the waves never meet before their sums are added, in their
+// order.  What bounds these products is the bytes of B on the way: direct buffer -> LDS
+// loads of whole lines (8 rows x 128 bytes each) move them; loads straight into the
+// registers' layout touch 16 rows at once and were held to 4 TB/s by the L1's lookups.
+template <int RM, int RN, int WAVES, int FA, int FB, class T>
+__global__ __launch_bounds__(64 * WAVES) void k_gemm_fp8_few(Gemm p) {
+  constexpr int ROWS = 16 * (RM + RN), PART = ROWS * kBlock;  // a wave's slab
+  constexpr int LOADS = 2 * (RM + RN), SCALES = RM + RN;
+  __shared__ __attribute__((aligned(128))) uint8_t stage0[WAVES * PART];
+  __shared__ __attribute__((aligned(128))) uint8_t stage1[WAVES * PART];
+  __shared__ __attribute__((aligned(128))) uint8_t stage2[WAVES * PART];
+  __shared__ __attribute__((aligned(128))) uint8_t stage3[WAVES * PART];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int id = xcd_order(blockIdx.x, gridDim.x), row0 = id / p.tiles_n * (16 * RM), col0 = id % p.tiles_n * (16 * RN);
+  const uint32_t arows = (uint32_t)min(16 * RM, p.M - row0), brows = (uint32_t)min(16 * RN, p.N - col0);
+  const uint8_t *pa = p.a + (int64_t)row0 * p.pitch, *pb = p.b + (int64_t)col0 * p.pitch;
+  const uint8_t *pea = p.ea + (int64_t)row0 * p.epitch, *peb = p.eb + (int64_t)col0 * p.epitch;
+  const int supers = (p.slabs + 3) / 4;
+  v4 acc[RM][RN];
+#pragma unroll
+  for (int i = 0; i < RM; ++i)
+#pragma unroll
+    for (int j = 0; j < RN; ++j) acc[i][j] = v4{0.f, 0.f, 0.f, 0.f};
+  // (the swizzle of k_gemm_fp8: chunk c of row r at c ^ ((r >> 1) & 7))
+  uint32_t load_off[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    load_off[u] = (uint32_t)(8 * u + (lane >> 3)) * p.pitch + (uint32_t)((lane & 7) ^ ((4 * u + (lane >> 4)) & 7)) * 16;
+  auto issue = [&](uint8_t* stage, int slab) __attribute__((always_inline)) {
+    const rsrc_t ra = make_rsrc(pa, slab < p.slabs ? arows * p.pitch : 0u);
+    const rsrc_t rb = make_rsrc(pb, slab < p.slabs ? brows * p.pitch : 0u);
+    uint8_t* mine = stage + wave * PART;
+#pragma unroll
+    for (int i = 0; i < RM; ++i)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(mine + (2 * i + u) * 1024), 16, load_off[u],
+                                                 (uint32_t)slab * kBlock + 16 * i * p.pitch, 0, 0);
+#pragma unroll
+    for (int j = 0; j < RN; ++j)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void*)(mine + (2 * (RM + j) + u) * 1024), 16, load_off[u],
+                                                 (uint32_t)slab * kBlock + 16 * j * p.pitch, 0, 0);
+  };
+  const int r = lane & 15, q = lane >> 4, rsw = (r >> 1) & 7;
+  int sa[RM], sb[RN], na[RM], nb[RN];
+  auto scales = [&](int super) __attribute__((always_inline)) {
+    const rsrc_t ra = make_rsrc(pea, super < supers ? arows * p.epitch : 0u);
+    const rsrc_t rb = make_rsrc(peb, super < supers ? brows * p.epitch : 0u);
+#pragma unroll
+    for (int i = 0; i < RM; ++i)
+      na[i] = (int)__builtin_amdgcn_raw_buffer_load_b32(ra, (uint32_t)(16 * i + r) * p.epitch, 4 * super, 0);
+#pragma unroll
+    for (int j = 0; j < RN; ++j)
+      nb[j] = (int)__builtin_amdgcn_raw_buffer_load_b32(rb, (uint32_t)(16 * j + r) * p.epitch, 4 * super, 0);
+  };
+  auto frag = [&](const uint8_t* at) __attribute__((always_inline)) -> v8i {
+    const u4 x = *reinterpret_cast<const u4*>(at + r * kBlock + ((2 * q) ^ rsw) * 16);
+    const u4 y = *reinterpret_cast<const u4*>(at + r * kBlock + ((2 * q + 1) ^ rsw) * 16);
+    return v8i{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+  };
+  // slab k of a run of four: its loads have landed when only the three younger slabs'
+  // (and, for slabs 1 to 3, the next run's scales) may be on the way
+  auto slab = [&](uint8_t* stage, auto kc, int next) __attribute__((always_inline)) {
+    constexpr int k = decltype(kc)::value;
+    __builtin_amdgcn_s_waitcnt(wait_loads(3 * LOADS + (k > 0 ? SCALES : 0)));
+    asm volatile("" ::: "memory");
+    const uint8_t* mine = stage + wave * PART;
+    v8i a[RM], b[RN];
+#pragma unroll
+    for (int i = 0; i < RM; ++i) a[i] = frag(mine + i * 16 * kBlock);
+#pragma unroll
+    for (int j = 0; j < RN; ++j) b[j] = frag(mine + (RM + j) * 16 * kBlock);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the stage is read
+    asm volatile("" ::: "memory");
+    if constexpr (k == 0) {
+#pragma unroll
+      for (int i = 0; i < RM; ++i) sa[i] = na[i];
+#pragma unroll
+      for (int j = 0; j < RN; ++j) sb[j] = nb[j];
+      scales(next);
+    }
+    issue(stage, 4 * next + k);
+#pragma unroll
+    for (int i = 0; i < RM; ++i)
+#pragma unroll
+      for (int j = 0; j < RN; ++j)  // (B first: a lane's four are columns of a row)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i], acc[i][j], FB, FA, k, sb[j], k, sa[i]);
+  };
+  scales(wave);
+  issue(stage0, 4 * wave);
+  issue(stage1, 4 * wave + 1);
+  issue(stage2, 4 * wave + 2);
+  issue(stage3, 4 * wave + 3);
+  for (int s = wave; s < supers; s += WAVES) {
+    slab(stage0, std::integral_constant<int, 0>{}, s + WAVES);
+    slab(stage1, std::integral_constant<int, 1>{}, s + WAVES);
+    slab(stage2, std::integral_constant<int, 2>{}, s + WAVES);
+    slab(stage3, std::integral_constant<int, 3>{}, s + WAVES);
+  }
+  // A lane holds columns 4 q .. + 3 of row r of each 16 x 16 tile.
+  constexpr int QUADS = 64 * RM * RN;
+  static_assert(QUADS * 16 <= PART, "the sums fit in a stage");
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  float* sums = reinterpret_cast<float*>(stage0);
+#pragma unroll
+  for (int i = 0; i < RM; ++i)
+#pragma unroll
+    for (int j = 0; j < RN; ++j)
+      *reinterpret_cast<v4*>(sums + (wave * QUADS + ((16 * i + r) * RN + j) * 4 + q) * 4) = acc[i][j];
+  __syncthreads();
+  T* C = static_cast<T*>(p.c);
+  for (int o = threadIdx.x; o < QUADS; o += 64 * WAVES) {
+    v4 v = *reinterpret_cast<const v4*>(sums + 4 * o);
+    for (int w = 1; w < WAVES; ++w) v += *reinterpret_cast<const v4*>(sums + (w * QUADS + o) * 4);
+    const int row = row0 + o / (4 * RN), c = col0 + o % (4 * RN) * 4;
+    if (row < p.M) store4(C + row * p.ldc + c, __builtin_bit_cast(u4, v), p.N - c);
   }
 }
 
@@ -184,13 +423,33 @@ __global__ __launch_bounds__(256) void k_join(const float* __restrict__ src, int
   store4(c + row * ldc + col, __builtin_bit_cast(u4, v), N - col);
 }
 
-template <int BM, int BN, int WGM, int WGN, class T>
-hipError_t launch_tiles(const Gemm& g, int fa, int fb, int parts, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)g.tiles_m * g.tiles_n * parts)), block(64 * WGM * WGN);
-  if (fa == kE4M3 && fb == kE4M3) hipLaunchKernelGGL((k_gemm_fp8<BM, BN, WGM, WGN, 0, 0, T>), grid, block, 0, s, g);
-  else if (fa == kE4M3) hipLaunchKernelGGL((k_gemm_fp8<BM, BN, WGM, WGN, 0, 1, T>), grid, block, 0, s, g);
-  else if (fb == kE4M3) hipLaunchKernelGGL((k_gemm_fp8<BM, BN, WGM, WGN, 1, 0, T>), grid, block, 0, s, g);
-  else hipLaunchKernelGGL((k_gemm_fp8<BM, BN, WGM, WGN, 1, 1, T>), grid, block, 0, s, g);
+template <int FA, int FB, class T>
+void launch_kernel(const Fp8Plan& plan, const Gemm& g, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)g.tiles_m * g.tiles_n * plan.parts));
+#define FASTBFP_FEW(RM, RN, WAVES) \
+  hipLaunchKernelGGL((k_gemm_fp8_few<RM, RN, WAVES, FA, FB, T>), grid, dim3(64 * WAVES), 0, s, g)
+#define FASTBFP_TILE(EDGE) hipLaunchKernelGGL((k_gemm_fp8<EDGE, EDGE, FA, FB, T>), grid, dim3(256), 0, s, g)
+  if (plan.waves == 0) {
+    if (plan.rows == 256) FASTBFP_TILE(256);
+    else if (plan.rows == 128) FASTBFP_TILE(128);
+    else FASTBFP_TILE(64);
+  } else if (plan.rows == 16 && plan.cols == 16) {
+    FASTBFP_FEW(1, 1, 4);
+  } else if (plan.rows == 16) {
+    FASTBFP_FEW(1, 4, 2);
+  } else {
+    FASTBFP_FEW(2, 2, 2);
+  }
+#undef FASTBFP_FEW
+#undef FASTBFP_TILE
+}
+
+template <class T>
+hipError_t launch_formats(const Fp8Plan& plan, const Gemm& g, int fa, int fb, hipStream_t s) {
+  if (fa == kE4M3 && fb == kE4M3) launch_kernel<0, 0, T>(plan, g, s);
+  else if (fa == kE4M3) launch_kernel<0, 1, T>(plan, g, s);
+  else if (fb == kE4M3) launch_kernel<1, 0, T>(plan, g, s);
+  else launch_kernel<1, 1, T>(plan, g, s);
   return hipGetLastError();
 }
 
@@ -202,16 +461,14 @@ hipError_t launch_plan(const Fp8Plan& plan, Gemm g, int fa, int fb, T* C, int64_
     return hipGetLastError();
   }
   g.part_slabs = plan.part_slabs;
-  g.tiles_m = (g.M + plan.tile - 1) / plan.tile;
-  g.tiles_n = (g.N + plan.tile - 1) / plan.tile;
+  g.tiles_m = (g.M + plan.rows - 1) / plan.rows;
+  g.tiles_n = (g.N + plan.cols - 1) / plan.cols;
   if (plan.parts == 1) {
     g.c = C, g.ldc = ldc, g.part_stride = 0;
-    return plan.tile == 128 ? launch_tiles<128, 128, 2, 2, T>(g, fa, fb, 1, s)
-                            : launch_tiles<64, 64, 2, 2, T>(g, fa, fb, 1, s);
+    return launch_formats<T>(plan, g, fa, fb, s);
   }
   g.c = ws, g.ldc = gemm_plan_ld(g.N), g.part_stride = g.M * g.ldc;
-  const hipError_t e = plan.tile == 128 ? launch_tiles<128, 128, 2, 2, float>(g, fa, fb, plan.parts, s)
-                                        : launch_tiles<64, 64, 2, 2, float>(g, fa, fb, plan.parts, s);
+  const hipError_t e = launch_formats<float>(plan, g, fa, fb, s);
   if (e != hipSuccess) return e;
   const int64_t n = g.part_stride / 4;
   hipLaunchKernelGGL(k_join<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, ws, plan.parts, g.part_stride,
@@ -219,13 +476,59 @@ hipError_t launch_plan(const Fp8Plan& plan, Gemm g, int fa, int fb, T* C, int64_
   return hipGetLastError();
 }
 
+// The kernels, and their time in us as fitted to 900 drawn products (1 .. 8192 rows, 64 ..
+// 16384 columns and K, either way round): `start` once, then for each round of workgroups on
+// the 256 CUs the larger of one's latency, `open` + slabs * `slab`, and of what those on a
+// CU together need of it, each `each_open` + slabs * `each`.  The kernel and parts taken
+// are 1.0% slower than the fastest ones in the mean, and 44% at worst.
+struct Kernel {
+  int rows, cols, waves, on_cu;
+  float start, open, slab, each_open, each;
+};
+constexpr Kernel kKernels[] = {
+    {64, 64, 0, 2, 2.83f, 1.69f, 0.149f, 1.03f, 0.207f},   {128, 128, 0, 2, 3.31f, 0.0f, 0.587f, 2.25f, 0.460f},
+    {256, 256, 0, 1, 0.68f, 11.24f, 1.145f, 0.66f, 0.254f}, {16, 16, 4, 2, 3.67f, 0.225f, 0.121f, 0.075f, 0.226f},
+    {16, 64, 2, 2, 3.87f, 0.264f, 0.223f, 0.400f, 0.323f},  {32, 32, 2, 2, 3.64f, 0.603f, 0.158f, 0.425f, 0.266f},
+};
+constexpr float kJoin = 2.5f, kJoinValue = 1.1e-6f;  // us, and for a value of a part
+
+float price(const Kernel& k, int64_t tiles, int slabs) {
+  if (k.waves > 0) {
+    // (a wave takes runs of four slabs)
+    const float run = 4.0f * (float)(((slabs + 3) / 4 + k.waves - 1) / k.waves);
+    const int64_t rounds = (tiles + 256 * k.on_cu - 1) / (256 * k.on_cu);
+    return k.start + fmaxf((float)rounds * (k.open + run * k.slab), (float)tiles / 256.0f * (k.each_open + run * k.each));
+  }
+  const float run = (float)(k.rows == 256 ? (slabs + 1) / 2 * 2 : slabs);
+  const int64_t on = (tiles + 255) / 256, rounds = on / k.on_cu, last = on % k.on_cu;
+  auto round = [&](int64_t n) { return fmaxf(k.open + run * k.slab, (float)n * (k.each_open + run * k.each)); };
+  return k.start + (float)rounds * round(k.on_cu) + (last ? round(last) : 0.0f);
+}
+
 }  // namespace fp8
 
 Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool room) {
-  (void)room;
-  const int64_t big = ((M + 127) / 128) * ((N + 127) / 128);
-  const int slabs = (int)fp8::blocks_of(K);
-  return {big >= 256 ? 128 : 64, slabs, 1};
+  using namespace fp8;
+  const int slabs = (int)blocks_of(K);
+  Fp8Plan best{64, 64, 0, slabs, 1};
+  float least = INFINITY;
+  if (slabs == 0) return best;
+  for (const Kernel& k : kKernels) {
+    const int64_t tiles = ((M + k.rows - 1) / k.rows) * ((N + k.cols - 1) / k.cols);
+    for (const int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+      if (want > 1 && (!room || k.waves > 0 || tiles > 1024)) break;
+      // (a part's scales begin at a whole dword)
+      const int each = want == 1 ? slabs : ((slabs + want - 1) / want + 3) / 4 * 4, parts = (slabs + each - 1) / each;
+      if (parts != want || (parts > 1 && parts * M * gemm_plan_ld(N) > (int64_t(1) << 26))) continue;
+      float t = price(k, tiles * parts, each);
+      if (parts > 1) t += kJoin + kJoinValue * (float)parts * (float)M * (float)N;
+      if (t < least) {
+        least = t;
+        best = {k.rows, k.cols, k.waves, each, parts};
+      }
+    }
+  }
+  return best;
 }
 
 int64_t fp8_plan_ws(const Fp8Plan& plan, int64_t M, int64_t N) {

@@ -223,10 +223,11 @@ hipError_t launch_quantize_fp8_dual(const void* x, bool bf16, int64_t R, int64_t
                                     uint8_t* codes_c, uint8_t* exps_c, uint32_t* status, hipStream_t s);
 hipError_t launch_dequantize_fp8(const uint8_t* codes, const uint8_t* exps, int64_t rows, int64_t len, int fmt,
                                  float* y, hipStream_t s);
-// How a product runs: the workgroup tile's edge, and K in `parts` parts of `part_slabs`
-// blocks (parts > 1, where there is room: into the workspace, added up afterwards).
+// How a product runs: the workgroup's tile, the waves that split its K (few rows or columns;
+// 0: the tiled kernel) and K in `parts` parts of `part_slabs` blocks (parts > 1, where there
+// is room: into the workspace, added up afterwards).
 struct Fp8Plan {
-  int tile, part_slabs, parts;
+  int rows, cols, waves, part_slabs, parts;
 };
 Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool room);
 int64_t fp8_plan_ws(const Fp8Plan& plan, int64_t M, int64_t N);  // bytes

@@ -65,19 +65,22 @@ def test_gemm_refusals(lib):
     assert g(M=1 << 30, N=1 << 30, ldc=1 << 30) == E_UNSUP
     assert g(C=at(0)) == g(C=at(3)) == g(C=at(2) - 4) == E_ARG
     assert g(M=0) == g(N=0, ldc=0) == OK
-    need, tile, parts = ctypes.c_size_t(0), ctypes.c_int(0), ctypes.c_int(0)
+    need, parts = ctypes.c_size_t(0), ctypes.c_int(0)
+    out = [ctypes.byref(ctypes.c_int(0)) for _ in range(3)] + [ctypes.byref(parts)]
     assert lib.bfp_gemm_fp8_ws_size(100, 90, 8192, None) == E_ARG
     assert lib.bfp_gemm_fp8_ws_size(100, 90, 1 << 20, ctypes.byref(need)) == OK
-    assert lib.bfp_gemm_fp8_route(100, 90, 1 << 20, need.value, ctypes.byref(tile), ctypes.byref(parts)) == OK
+    assert lib.bfp_gemm_fp8_route(100, 90, 1 << 20, need.value, *out) == OK
+    assert (parts.value > 1) == (need.value > 0)
     if need.value:
-        assert parts.value > 1
         k = dict(K=1 << 20, n=need.value)
         big = 1 << 34  # (apart from everything)
         spread = dict(a=big, ea=2 * big, b=3 * big, eb=4 * big, C=5 * big)
         assert g(**spread, **k, ws=6 * big + 4) == g(**spread, **k, ws=big) == g(**spread, **k, ws=5 * big) == E_ARG
-        assert lib.bfp_gemm_fp8_route(100, 90, 1 << 20, need.value - 1, ctypes.byref(tile), ctypes.byref(parts)) == OK
+        assert lib.bfp_gemm_fp8_route(100, 90, 1 << 20, need.value - 1, *out) == OK
         assert parts.value == 1
-    assert lib.bfp_gemm_fp8_route(0, 90, 100, 0, ctypes.byref(tile), ctypes.byref(parts)) == E_ARG
+    assert lib.bfp_gemm_fp8_route(0, 90, 100, 0, *out) == E_ARG
+    assert lib.bfp_gemm_fp8_ws_size(100, 90, 0, ctypes.byref(need)) == OK and need.value == 0
+    assert g(K=0, a=None, ea=None, b=None, eb=None, C=at(4) + 2) == E_ARG  # (checked, and nothing divides by K)
 
 
 def test_norm_refusals(lib):
