@@ -26,6 +26,20 @@ __host__ __device__ constexpr int64_t exp_pitch(int64_t len) { return (blocks_of
 
 typedef float v4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint16_t h2 __attribute__((ext_vector_type(2)));
+typedef short s2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+typedef uint16_t bf16_t;  // a BF16 value's bits, the upper half of an FP32's
+
+// Four values as they are in memory.
+template <class T> struct Raw;
+template <> struct Raw<float> { typedef u4 type; };
+template <> struct Raw<bf16_t> { typedef u2 type; };
+// Their FP32 bits.
+__device__ __forceinline__ u4 wide(const u4& v) { return v; }
+__device__ __forceinline__ u4 wide(const u2& v) { return u4{v[0] << 16, v[0] & 0xFFFF0000u, v[1] << 16, v[1] & 0xFFFF0000u}; }
 
 // Magnitude bits of a value as the block's maximum takes them: subnormals, infinities
 // and NaN do not count.
@@ -62,6 +76,51 @@ __device__ __forceinline__ uint32_t convert4(const u4& b, float inv, int fmt) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(x2, x3, lo, true);
 }
 
+// The quick way through a conversion: `key`, twice the bits of a block's largest magnitude
+// as they are, and the hardware's scaled conversion.  It does not hold for blocks with
+// infinities or NaN, or whose scale would show FP32 subnormals as more than zero
+// (a subnormal over 2^(18 - 127) is below half of e5m2's least value, 2^-17).
+__device__ __forceinline__ uint32_t key4(const u4& b) {
+  return max(max(b[0] << 1, b[1] << 1), max(b[2] << 1, b[3] << 1));
+}
+__device__ __forceinline__ uint32_t key4(const u2& b) {
+  const h2 x = __builtin_bit_cast(h2, b[0] & 0x7FFF7FFFu), y = __builtin_bit_cast(h2, b[1] & 0x7FFF7FFFu);
+  const h2 m = __builtin_elementwise_max(x, y);
+  return (uint32_t)max(m[0], m[1]) << 17;
+}
+__device__ __forceinline__ bool key_finite(uint32_t key) { return key < 0xFF000000u; }
+__device__ __forceinline__ bool quick(uint32_t key, uint32_t scale) { return key_finite(key) && scale > 18u; }
+
+template <int FMT>
+__device__ __forceinline__ uint32_t quick4(const u4& b, uint32_t scale) {
+  const float f = __uint_as_float(scale << 23);
+  const float x0 = __uint_as_float(b[0]), x1 = __uint_as_float(b[1]), x2 = __uint_as_float(b[2]), x3 = __uint_as_float(b[3]);
+  s2 r{};
+  if constexpr (FMT == kE4M3) {
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, x0, x1, f, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, x2, x3, f, true);
+  } else {
+    r = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(r, x0, x1, f, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(r, x2, x3, f, true);
+  }
+  return __builtin_bit_cast(uint32_t, r);
+}
+template <int FMT>
+__device__ __forceinline__ uint32_t quick4(const u2& b, uint32_t scale) {
+  const float f = __uint_as_float(scale << 23);
+  const uint32_t lo = b[0], hi = b[1];  // (of b[1] itself the compiler's bit cast takes b[0])
+  const b2 x = __builtin_bit_cast(b2, lo), y = __builtin_bit_cast(b2, hi);
+  s2 r{};
+  if constexpr (FMT == kE4M3) {
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, x, f, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, y, f, true);
+  } else {
+    r = __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(r, x, f, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(r, y, f, true);
+  }
+  return __builtin_bit_cast(uint32_t, r);
+}
+
 template <int CTRL>
 __device__ __forceinline__ uint32_t max_dpp(uint32_t v) {
   return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false));
@@ -78,13 +137,25 @@ __device__ __forceinline__ uint32_t max4(const u4& b) {
   return max(max(counted(b[0]), counted(b[1])), max(counted(b[2]), counted(b[3])));
 }
 
-typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-typedef uint16_t bf16_t;  // a BF16 value's bits, the upper half of an FP32's
 
-// Bits (FP32) of four values from `left` (of a row) on: those past the row's end are
-// zeros.  Rows of any length begin at any multiple of a value's bytes.
-__device__ __forceinline__ u4 load4(const float* p, int64_t left) {
+// A block along a row, four values a lane of half a wave: its codes, and in `scale` its
+// scale's byte; bad: whether the lane has an infinity or NaN.
+template <int FMT, class V>
+__device__ __forceinline__ uint32_t convert_block(const V& v, uint32_t& scale, bool& bad) {
+  const uint32_t key = max_half_wave(key4(v));
+  scale = scale_of(key >> 1, FMT);
+  bad = false;
+  if (quick(key, scale)) return quick4<FMT>(v, scale);
+  const u4 b = wide(v);
+  scale = scale_of(max_half_wave(max4(b)), FMT);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) bad |= !finite(b[t]);
+  return convert4(b, inverse(scale), FMT);
+}
+
+// Four values from `left` (of a row) on, as they are: those past the row's end are zeros.
+// Rows of any length begin at any multiple of a value's bytes.
+__device__ __forceinline__ u4 raw4(const float* p, int64_t left) {
   typedef u4 __attribute__((aligned(4))) u4_any;
   if (left >= 4) return *reinterpret_cast<const u4_any*>(p);
   u4 v = u4{0u, 0u, 0u, 0u};
@@ -93,19 +164,19 @@ __device__ __forceinline__ u4 load4(const float* p, int64_t left) {
     if (t < left) v[t] = __float_as_uint(p[t]);
   return v;
 }
-__device__ __forceinline__ u4 load4(const bf16_t* p, int64_t left) {
+__device__ __forceinline__ u2 raw4(const bf16_t* p, int64_t left) {
   typedef u2 __attribute__((aligned(2))) u2_any;
-  if (left >= 4) {
-    const u2 v = *reinterpret_cast<const u2_any*>(p);
-    return u4{v[0] << 16, v[0] & 0xFFFF0000u, v[1] << 16, v[1] & 0xFFFF0000u};
-  }
-  u4 v = u4{0u, 0u, 0u, 0u};
+  if (left >= 4) return *reinterpret_cast<const u2_any*>(p);
+  u2 v = u2{0u, 0u};
 #pragma unroll
   for (int t = 0; t < 3; ++t)
-    if (t < left) v[t] = (uint32_t)p[t] << 16;
+    if (t < left) v[t / 2] |= (uint32_t)p[t] << (16 * (t & 1));
   return v;
 }
-// Stores them, rounded to the nearest (ties to even) for BF16.
+// Their FP32 bits.
+template <class T>
+__device__ __forceinline__ u4 load4(const T* p, int64_t left) { return wide(raw4(p, left)); }
+// Stores four values, rounded to the nearest (ties to even) for BF16.
 __device__ __forceinline__ void store4(float* p, const u4& v, int64_t left) {
   typedef u4 __attribute__((aligned(4))) u4_any;
   if (left >= 4) {

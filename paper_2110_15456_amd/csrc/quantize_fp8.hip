@@ -9,8 +9,8 @@ namespace fastbfp {
 namespace fp8 {
 
 // Blocks along the rows.  Half a wave takes four blocks of a row, a lane four values of
-// each: every load reads 512 contiguous bytes, every store writes a block's 128, and
-// the four scales leave as one dword.
+// each: every load reads 512 contiguous bytes (256 of BF16), every store writes a block's
+// 128, and the four scales leave as one dword.
 template <int FMT, class T>
 __global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int64_t len, uint32_t quads_row,
                                                   int64_t quads, uint8_t* __restrict__ codes,
@@ -21,88 +21,145 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int64
   const int64_t row = q / quads_row;
   const int64_t c0 = (q - row * quads_row) * (4 * kBlock) + 4 * lane;
   const T* src = x + row * len;
-  u4 v[4];
+  typename Raw<T>::type v[4];
 #pragma unroll
-  for (int b = 0; b < 4; ++b) v[b] = load4(src + c0 + b * kBlock, len - (c0 + b * kBlock));
-  uint32_t scales = 0, bad = 0;
+  for (int b = 0; b < 4; ++b) v[b] = raw4(src + c0 + b * kBlock, len - (c0 + b * kBlock));
+  uint32_t scales = 0;
+  bool any = false;
   uint8_t* out = codes + row * code_pitch(len);
 #pragma unroll
   for (int b = 0; b < 4; ++b) {
-    const uint32_t s = scale_of(max_half_wave(max4(v[b])), FMT);
+    uint32_t s;
+    bool bad;
+    const uint32_t w = convert_block<FMT>(v[b], s, bad);
+    any |= bad;
     scales |= s << (8 * b);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) bad |= finite(v[b][t]) ? 0u : 1u;
-    const uint32_t w = convert4(v[b], inverse(s), FMT);
     if (c0 - 4 * lane + b * kBlock < len) *reinterpret_cast<uint32_t*>(out + c0 + b * kBlock) = w;
   }
   if (lane == 0) *reinterpret_cast<uint32_t*>(exps + row * exp_pitch(len) + (c0 / kBlock)) = scales;
-  if (status && bad) atomicOr(status, 1u);
+  if (status && any) atomicOr(status, 1u);
 }
 
 // Blocks down the columns (transposed: output row c is column c), and with ROWS also
-// along the rows, by tiles of 128 x 128 in LDS: a tile holds a block of each of its rows
-// and of each of its columns.
-constexpr int kStride = kBlock + 4;     // of a tile's row in LDS, floats
-constexpr int kCodeStride = kBlock + 16;  // of a column's codes, bytes
+// along the rows, by tiles of 128 x 128: a tile holds a block of each of its rows and of
+// each of its columns.  Half a wave loads 16 rows, all on the way at once, converts them
+// where asked to and leaves them in LDS as they are; then a thread takes 64 values down
+// the columns (FP32: half of one; BF16: a quarter of two beside each other, a dword a row),
+// and the codes leave through LDS as whole lines.
+constexpr int kCodeStride = kBlock + 16;  // of a column's codes in LDS, bytes
 
 template <int FMT, bool ROWS, class T>
 __global__ __launch_bounds__(256) void k_fp8_tiles(const T* __restrict__ x, int64_t R, int64_t C, uint32_t tiles_c,
                                                    uint8_t* __restrict__ codes_r, uint8_t* __restrict__ exps_r,
                                                    uint8_t* __restrict__ codes_c, uint8_t* __restrict__ exps_c,
                                                    uint32_t* status) {
-  __shared__ __attribute__((aligned(16))) float tile[kBlock * kStride];
-  __shared__ uint32_t top[2][kBlock];
+  constexpr bool B = sizeof(T) == 2;
+  constexpr int RUNS = B ? 4 : 2;  // threads to a column
+  __shared__ __attribute__((aligned(16))) T tile[kBlock * kBlock];
+  __shared__ uint32_t top[RUNS][kBlock];
+  static_assert(sizeof(tile) >= kBlock * kCodeStride, "the codes fit where the tile was");
   const int tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
   const int64_t r0 = (int64_t)tr * kBlock, c0 = (int64_t)tc * kBlock;
-  const int half = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  uint32_t bad = 0;
-#pragma unroll 4
-  for (int i = 0; i < kBlock / 8; ++i) {
-    const int r = i * 8 + half;
-    u4 v = u4{0u, 0u, 0u, 0u};
-    if (r0 + r < R) v = load4(x + (r0 + r) * C + c0 + 4 * lane, C - (c0 + 4 * lane));
+  {
+    const int half = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    typedef typename Raw<T>::type V;
+    V v[16];
+    const bool whole = r0 + kBlock <= R && c0 + kBlock <= C;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) bad |= finite(v[t]) ? 0u : 1u;
-    *reinterpret_cast<u4*>(&tile[r * kStride + 4 * lane]) = v;
-    if constexpr (ROWS) {
-      const uint32_t s = scale_of(max_half_wave(max4(v)), FMT);
-      const uint32_t w = convert4(v, inverse(s), FMT);
-      if (r0 + r < R) {
-        *reinterpret_cast<uint32_t*>(codes_r + (r0 + r) * code_pitch(C) + c0 + 4 * lane) = w;
-        uint8_t* e = exps_r + (r0 + r) * exp_pitch(C) + tc;
-        if (lane == 0) *e = (uint8_t)s;
-        // (the scales behind a row's last block are zeros)
-        if (tc + 1 == (int)tiles_c && lane > 0 && lane < (int)(exp_pitch(C) - tc)) e[lane] = 0;
+    for (int i = 0; i < 16; ++i) {
+      const int64_t r = r0 + i * 8 + half;
+      const T* p = x + r * C + c0 + 4 * lane;
+      v[i] = whole ? raw4(p, 4) : r < R ? raw4(p, C - (c0 + 4 * lane)) : V{};
+    }
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int r = i * 8 + half;
+      *reinterpret_cast<V*>(&tile[r * kBlock + 4 * lane]) = v[i];
+      if constexpr (ROWS) {
+        uint32_t s;
+        bool bad;
+        const uint32_t w = convert_block<FMT>(v[i], s, bad);
+        any |= bad;
+        if (r0 + r < R) {
+          *reinterpret_cast<uint32_t*>(codes_r + (r0 + r) * code_pitch(C) + c0 + 4 * lane) = w;
+          uint8_t* e = exps_r + (r0 + r) * exp_pitch(C) + tc;
+          if (lane == 0) *e = (uint8_t)s;
+          // (the scales behind a row's last block are zeros)
+          if (tc + 1 == (int)tiles_c && lane > 0 && lane < (int)(exp_pitch(C) - tc)) e[lane] = 0;
+        }
       }
     }
+    if (ROWS && status && any) atomicOr(status, 1u);
   }
   __syncthreads();
-  const int c = threadIdx.x & 127, h = threadIdx.x >> 7;
-  u4 v[16];
-  uint32_t m = 0;
+  // Column c (with BF16 c and c + 1) from row run * 128 / RUNS on.
+  const int c = B ? 2 * (threadIdx.x & 63) : threadIdx.x & 127, run = threadIdx.x / (B ? 64 : 128);
+  constexpr int Q = B ? 8 : 16, COLS = B ? 2 : 1;  // quads of rows, columns
+  typename Raw<T>::type v[COLS][Q];
+  uint32_t key[COLS];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int j = 0; j < COLS; ++j) key[j] = 0;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) v[i][t] = __float_as_uint(tile[(64 * h + 4 * i + t) * kStride + c]);
-    m = max(m, max4(v[i]));
+  for (int i = 0; i < Q; ++i) {
+    const int r = run * (kBlock / RUNS) + 4 * i;
+    if constexpr (B) {
+      uint32_t w[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) w[t] = *reinterpret_cast<const uint32_t*>(&tile[(r + t) * kBlock + c]);
+      v[0][i] = u2{__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u)};
+      v[COLS - 1][i] = u2{__builtin_amdgcn_perm(w[1], w[0], 0x07060302u), __builtin_amdgcn_perm(w[3], w[2], 0x07060302u)};
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) v[0][i][t] = __float_as_uint(tile[(r + t) * kBlock + c]);
+    }
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) key[j] = max(key[j], key4(v[j][i]));
   }
-  top[h][c] = m;
-  __syncthreads();  // (also: the tile is read)
-  const uint32_t s = scale_of(max(top[0][c], top[1][c]), FMT);
-  const float inv = inverse(s);
+#pragma unroll
+  for (int j = 0; j < COLS; ++j) top[run][c + j] = key[j];
+  bool odd = false;
+#pragma unroll
+  for (int j = 0; j < COLS; ++j) odd |= !key_finite(key[j]);
+  // (also: the tile is read)
+  if (__syncthreads_or(odd)) {
+    // a tile with infinities or NaN: the maxima without them
+    if (odd && status) atomicOr(status, 1u);
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < Q; ++i) m = max(m, max4(wide(v[j][i])));
+      top[run][c + j] = m << 1;
+    }
+    __syncthreads();
+  }
   uint8_t* out = reinterpret_cast<uint8_t*>(tile);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    u4 w;
+  for (int j = 0; j < COLS; ++j) {
+    uint32_t m = top[0][c + j];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) w[t] = convert4(v[4 * i + t], inv, FMT);
-    *reinterpret_cast<u4*>(out + c * kCodeStride + 64 * h + 16 * i) = w;
-  }
-  if (c0 + c < C) {
-    uint8_t* e = exps_c + (c0 + c) * exp_pitch(R) + tr;
-    if (h == 0) *e = (uint8_t)s;
-    else if (r0 + kBlock >= R)
-      for (int k = 1; k < (int)(exp_pitch(R) - tr); ++k) e[k] = 0;
+    for (int k = 1; k < RUNS; ++k) m = max(m, top[k][c + j]);
+    const uint32_t s = scale_of(m >> 1, FMT);
+    uint32_t w[Q];
+    if (!odd && s > 18u) {
+#pragma unroll
+      for (int i = 0; i < Q; ++i) w[i] = quick4<FMT>(v[j][i], s);
+    } else {
+      const float inv = inverse(s);
+#pragma unroll
+      for (int i = 0; i < Q; ++i) w[i] = convert4(wide(v[j][i]), inv, FMT);
+    }
+#pragma unroll
+    for (int i = 0; i < Q / 4; ++i)
+      *reinterpret_cast<u4*>(out + (c + j) * kCodeStride + run * (kBlock / RUNS) + 16 * i) =
+          u4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+    if (c0 + c + j < C) {
+      uint8_t* e = exps_c + (c0 + c + j) * exp_pitch(R) + tr;
+      if (run == 0) *e = (uint8_t)s;
+      else if (run == 1 && r0 + kBlock >= R)
+        for (int k = 1; k < (int)(exp_pitch(R) - tr); ++k) e[k] = 0;
+    }
   }
   __syncthreads();
 #pragma unroll
@@ -112,7 +169,6 @@ __global__ __launch_bounds__(256) void k_fp8_tiles(const T* __restrict__ x, int6
       *reinterpret_cast<u4*>(codes_c + (c0 + cc) * code_pitch(R) + r0 + at) =
           *reinterpret_cast<const u4*>(out + cc * kCodeStride + at);
   }
-  if (status && bad) atomicOr(status, 1u);
 }
 
 // The values: codes times their block's scale (exact unless below FP32's range).

@@ -99,12 +99,12 @@ __global__ __launch_bounds__(NT) void k_rms_norm(Args p) {
       else if (d - c < 4)
 #pragma unroll
         for (int i = 1; i < 4; ++i) y[i] = c + i < d ? y[i] : 0u;
-      const uint32_t s = fp8::scale_of(fp8::max_half_wave(fp8::max4(y)), p.fmt);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) bad |= fp8::finite(y[i]) ? 0u : 1u;
+      uint32_t s;
+      bool b;
+      const uint32_t q = p.fmt == fp8::kE4M3 ? fp8::convert_block<fp8::kE4M3>(y, s, b) : fp8::convert_block<fp8::kE5M2>(y, s, b);
+      bad |= b ? 1u : 0u;
       const int64_t block = c / fp8::kBlock;
-      if (block * fp8::kBlock < d)
-        *reinterpret_cast<uint32_t*>(p.codes + row * fp8::code_pitch(d) + c) = fp8::convert4(y, fp8::inverse(s), p.fmt);
+      if (block * fp8::kBlock < d) *reinterpret_cast<uint32_t*>(p.codes + row * fp8::code_pitch(d) + c) = q;
       if ((t & 31) == 0 && block < fp8::exp_pitch(d)) p.exps[row * fp8::exp_pitch(d) + block] = (uint8_t)s;
     } else {
       // each wave gathers its 256 consecutive values, 16 groups, and converts a group a lane
