@@ -93,6 +93,7 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
   __shared__ __attribute__((aligned(128))) uint8_t stage1[STAGE];
   __shared__ __attribute__((aligned(128))) uint8_t stage2[ST == 4 ? STAGE : 16];
   __shared__ __attribute__((aligned(128))) uint8_t stage3[ST == 4 ? STAGE : 16];
+  __shared__ int scale_stage[2 * (BM + BN)];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int wr = wave >> 1, wc = wave & 1;
 
@@ -105,6 +106,7 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
 
   const int arows = min(BM, p.M - row0), brows = min(BN, p.N - col0);
   const uint8_t *pa = p.a + (int64_t)row0 * p.pitch, *pb = p.b + (int64_t)col0 * p.pitch;
+  const uint8_t *pea = p.ea + (int64_t)row0 * p.epitch, *peb = p.eb + (int64_t)col0 * p.epitch;
   const uint32_t size_a = (uint32_t)arows * p.pitch, size_b = (uint32_t)brows * p.pitch;
   v16 acc[TM][TN];
 #pragma unroll
@@ -138,17 +140,30 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
     const u4 y = *reinterpret_cast<const u4*>(at + (at1 ^ (64 * h)));
     return v8i{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
   };
-  // the scales of four slabs from s on, for each of the lane's rows (their rows are whole
-  // dwords; behind the last slab: zeros)
-  auto scales = [&](int s, int (&sa)[TM], int (&sb)[TN]) __attribute__((always_inline)) {
-    const rsrc_t ra = make_rsrc(p.ea + (int64_t)row0 * p.epitch, s < nslabs ? (uint32_t)arows * p.epitch : 0u);
-    const rsrc_t rb = make_rsrc(p.eb + (int64_t)col0 * p.epitch, s < nslabs ? (uint32_t)brows * p.epitch : 0u);
+  // The scales of slab s and its neighbours of a dword, for each row of A and then of B, to
+  // LDS: 64 rows at a time, which of them goes by the wave.  (A lane's
+  // own loads of its rows' dwords, each in a line of its own, took as long as half of the
+  // codes' loads.)
+  constexpr int RUNS = (BM + BN) / 64, LS = RUNS < NW ? 1 : RUNS / NW;  // loads of a wave
+  auto issue_scales = [&](int s) __attribute__((always_inline)) {
+    const int first = s & ~3, quad = (s >> 2) & 1;
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
-      sa[i] = (int)__builtin_amdgcn_raw_buffer_load_b32(ra, (uint32_t)(wr * WM + 32 * i + fr) * p.epitch, slab0 + s, 0);
+    for (int u = 0; u < LS; ++u) {
+      const int run = RUNS < NW ? wave % RUNS : wave + NW * u;
+      const bool of_b = run >= BM / 64;
+      const rsrc_t rs = make_rsrc(of_b ? peb : pea, first < nslabs ? (uint32_t)(of_b ? brows : arows) * p.epitch : 0u);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(scale_stage + quad * (BM + BN) + run * 64), 4,
+                                               (uint32_t)((of_b ? run - BM / 64 : run) * 64 + lane) * p.epitch,
+                                               slab0 + first, 0, 0);
+    }
+  };
+  auto read_scales = [&](int s, int (&sa)[TM], int (&sb)[TN]) __attribute__((always_inline)) {
+    const int* at = scale_stage + ((s >> 2) & 1) * (BM + BN) + fr;
+    const int down = 8 * (s & 3);  // (slab s's byte lowest)
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
-      sb[j] = (int)__builtin_amdgcn_raw_buffer_load_b32(rb, (uint32_t)(wc * WN + 32 * j + fr) * p.epitch, slab0 + s, 0);
+    for (int i = 0; i < TM; ++i) sa[i] = (int)((uint32_t)at[wr * WM + 32 * i] >> down);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) sb[j] = (int)((uint32_t)at[BM + wc * WN + 32 * j] >> down);
   };
   v8i a[2][TM], b[2][TN];
   int sa[TM], sb[TN], na[TM], nb[TN];
@@ -174,35 +189,33 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
     asm volatile("" ::: "memory");
   };
   constexpr std::integral_constant<int, 0> all{};
-  // slab s, the k-th of a run of ST: when its second step's fragments are read, slab s + 1
-  // has to have landed, while those of s + 2 .. s + ST - 1 (and the next run's scales,
-  // until they are older than slab s + 1) may be on the way
+  // Slab s, the k-th of a run of ST.  When its second step's fragments are read, slab s + 1
+  // has to have landed, while those of s + 2 .. s + ST - 1 (and the next scales, until they
+  // are older than slab s + 1) may be on the way.  The run's first slab asks for the scales
+  // of the slab four from it (with ST = 2 every second time for those that are there
+  // already, which does no harm), its last reads the next run's.
   auto slab = [&](uint8_t* cur, uint8_t* nxt, auto kc, int s) __attribute__((always_inline)) {
-    constexpr int YOUNGER = (ST - 2) * (LA + LB) + (ST == 4 && decltype(kc)::value < 3 ? TM + TN : 0);
+    constexpr int k = decltype(kc)::value;
+    constexpr int YOUNGER = (ST - 2) * (LA + LB) + (ST == 4 && (k == 1 || k == 2) ? LS : 0);
     __builtin_amdgcn_sched_barrier(0);
     read(cur, 1, a[1], b[1]);
     multiply(a[0], b[0]);
     spread<TM, TN, 0>();
     __builtin_amdgcn_sched_barrier(0);
     meet(std::integral_constant<int, YOUNGER>{});
+    if constexpr (k == 0) issue_scales(s + 4);
     issue(cur, s + ST);
     read(nxt, 0, a[0], b[0]);  // (behind the last slab: what lies there, unused)
+    if constexpr (k == ST - 1) read_scales(s + 1, na, nb);
     multiply(a[1], b[1]);
     spread<TM, TN, LA + LB>();
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < TM; ++i) sa[i] = (int)((uint32_t)sa[i] >> 8);
+    for (int i = 0; i < TM; ++i) sa[i] = k == ST - 1 ? na[i] : (int)((uint32_t)sa[i] >> 8);
 #pragma unroll
-    for (int j = 0; j < TN; ++j) sb[j] = (int)((uint32_t)sb[j] >> 8);
+    for (int j = 0; j < TN; ++j) sb[j] = k == ST - 1 ? nb[j] : (int)((uint32_t)sb[j] >> 8);
   };
-  auto next_scales = [&](int s) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < TM; ++i) sa[i] = na[i];
-#pragma unroll
-    for (int j = 0; j < TN; ++j) sb[j] = nb[j];
-    scales(s, na, nb);
-  };
-  scales(0, na, nb);
+  issue_scales(0);
   issue(stage0, 0);
   issue(stage1, 1);
   if constexpr (ST == 4) {
@@ -210,10 +223,10 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
     issue(stage3, 3);
   }
   meet(std::integral_constant<int, (ST - 1) * (LA + LB)>{});
+  read_scales(0, sa, sb);
   read(stage0, 0, a[0], b[0]);
   if constexpr (ST == 2) {
     for (int s = 0; s < nslabs; s += 2) {
-      if ((s & 2) == 0) next_scales(s + 4);
       slab(stage0, stage1, std::integral_constant<int, 0>{}, s);
       // (the 256 tile runs an odd slab's partner on zeros: around a branch here its
       // fragments would not stay in registers)
@@ -221,7 +234,6 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
     }
   } else {
     for (int s = 0; s < nslabs; s += 4) {
-      next_scales(s + 4);
       slab(stage0, stage1, std::integral_constant<int, 0>{}, s);
       if (s + 1 < nslabs) slab(stage1, stage2, std::integral_constant<int, 1>{}, s + 1);
       if (s + 2 < nslabs) slab(stage2, stage3, std::integral_constant<int, 2>{}, s + 2);
