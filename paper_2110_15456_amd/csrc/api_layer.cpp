@@ -82,16 +82,22 @@ bool norm_overlap(const void* o, uint64_t bytes, const void* x, int x_type, cons
          overlap(o, bytes, h, n) || overlap(o, bytes, rstd, rows * 4);
 }
 
-int check_list(const void* const* tensors, int type, const int64_t* sizes, int64_t count) {
-  if (!type_ok(type) || count < 0 || (count > 0 && (!tensors || !sizes))) return BFP_E_ARG;
-  int64_t pieces = 0;
+int check_sizes(const int64_t* sizes, int64_t count) {
+  if (count < 0 || (count > 0 && !sizes)) return BFP_E_ARG;
+  if (count > (int64_t(1) << 24)) return BFP_E_UNSUPPORTED;
+  int64_t total = 0;
   for (int64_t i = 0; i < count; ++i) {
-    if (sizes[i] < 0 || (sizes[i] > 0 && (!tensors[i] || !aligned(tensors[i], bytes_of(type))))) return BFP_E_ARG;
-    if (sizes[i] > (int64_t(1) << 42)) return BFP_E_UNSUPPORTED;
-    pieces += fastbfp::gradient_pieces(sizes + i, 1);
-    if (pieces > kGrid) return BFP_E_UNSUPPORTED;
+    if (sizes[i] < 0) return BFP_E_ARG;
+    if (sizes[i] > (int64_t(1) << 42) || (total += sizes[i]) > (int64_t(1) << 42)) return BFP_E_UNSUPPORTED;
   }
   return BFP_OK;
+}
+
+int check_list(const void* const* tensors, int type, const int64_t* sizes, int64_t count) {
+  if (!type_ok(type) || count < 0 || (count > 0 && (!tensors || !sizes))) return BFP_E_ARG;
+  for (int64_t i = 0; i < count; ++i)
+    if (sizes[i] > 0 && (!tensors[i] || !aligned(tensors[i], bytes_of(type)))) return BFP_E_ARG;
+  return check_sizes(sizes, count);
 }
 
 struct Span {
@@ -302,7 +308,7 @@ int bfp_rms_norm_grad_ws_size(int64_t rows, int64_t d, size_t* workspace_bytes) 
   const int st = check_norm(rows, d);
   if (st != BFP_OK) return st;
   if (!workspace_bytes) return BFP_E_ARG;
-  *workspace_bytes = (size_t)fastbfp::rms_norm_grad_parts(rows, d) * d * 4;
+  *workspace_bytes = (size_t)fastbfp::rms_norm_grad_parts(rows) * d * 4;
   return BFP_OK;
 }
 
@@ -312,7 +318,7 @@ int bfp_rms_norm_grad(const void* dy, int dy_type, const float* h, const float* 
   const int st = check_norm(rows, d);
   if (st != BFP_OK || d == 0) return st;
   if (!type_ok(dy_type) || !dweight || !aligned(dweight, 4)) return BFP_E_ARG;
-  const uint64_t n = (uint64_t)rows * d * 4, need = (uint64_t)fastbfp::rms_norm_grad_parts(rows, d) * d * 4;
+  const uint64_t n = (uint64_t)rows * d * 4, need = (uint64_t)fastbfp::rms_norm_grad_parts(rows) * d * 4;
   if (rows > 0) {
     if (!dy || !h || !rstd || !weight || !dx || !workspace || workspace_bytes < need) return BFP_E_ARG;
     if (!aligned(dy, bytes_of(dy_type)) || !aligned(h, 4) || !aligned(rstd, 4) || !aligned(weight, 4) || !aligned(dresidual, 4) ||
@@ -334,15 +340,10 @@ int bfp_rms_norm_grad(const void* dy, int dy_type, const float* h, const float* 
 }
 
 int bfp_sum_squares_ws_size(const int64_t* sizes, int64_t count, size_t* workspace_bytes) {
-  if (count < 0 || (count > 0 && !sizes) || !workspace_bytes) return BFP_E_ARG;
-  int64_t pieces = 0;
-  for (int64_t i = 0; i < count; ++i) {
-    if (sizes[i] < 0) return BFP_E_ARG;
-    if (sizes[i] > (int64_t(1) << 42)) return BFP_E_UNSUPPORTED;
-    pieces += fastbfp::gradient_pieces(sizes + i, 1);
-    if (pieces > kGrid) return BFP_E_UNSUPPORTED;
-  }
-  *workspace_bytes = (size_t)pieces * sizeof(double);
+  const int st = check_sizes(sizes, count);
+  if (st != BFP_OK) return st;
+  if (!workspace_bytes) return BFP_E_ARG;
+  *workspace_bytes = (size_t)fastbfp::gradient_pieces(sizes, count) * sizeof(double);
   return BFP_OK;
 }
 

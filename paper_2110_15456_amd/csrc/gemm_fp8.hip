@@ -492,14 +492,14 @@ hipError_t launch_plan(const Fp8Plan& plan, Gemm g, int fa, int fb, T* C, int64_
 // 16384 columns and K, either way round): `start` once, then for each round of workgroups on
 // the 256 CUs the larger of one's latency, `open` + slabs * `slab`, and of what those on a
 // CU together need of it, each `each_open` + slabs * `each`.  The kernel and parts taken
-// are 1.0% slower than the fastest ones in the mean, and 44% at worst.
+// are 1.4% slower than the fastest ones in the mean, and 77% at worst (2 us).
 struct Kernel {
   int rows, cols, waves, on_cu;
   float start, open, slab, each_open, each;
 };
 constexpr Kernel kKernels[] = {
-    {64, 64, 0, 2, 2.83f, 1.69f, 0.149f, 1.03f, 0.207f},   {128, 128, 0, 2, 3.31f, 0.0f, 0.587f, 2.25f, 0.460f},
-    {256, 256, 0, 1, 0.68f, 11.24f, 1.145f, 0.66f, 0.254f}, {16, 16, 4, 2, 3.67f, 0.225f, 0.121f, 0.075f, 0.226f},
+    {64, 64, 0, 2, 2.95f, 1.61f, 0.148f, 0.99f, 0.207f},  {128, 128, 0, 2, 3.32f, 0.0f, 0.540f, 2.24f, 0.418f},
+    {256, 256, 0, 1, 0.0f, 12.17f, 1.04f, 0.66f, 0.254f}, {16, 16, 4, 2, 3.67f, 0.225f, 0.121f, 0.075f, 0.226f},
     {16, 64, 2, 2, 3.87f, 0.264f, 0.223f, 0.400f, 0.323f},  {32, 32, 2, 2, 3.64f, 0.603f, 0.158f, 0.425f, 0.266f},
 };
 constexpr float kJoin = 2.5f, kJoinValue = 1.1e-6f;  // us, and for a value of a part

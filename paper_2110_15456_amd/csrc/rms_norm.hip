@@ -211,22 +211,33 @@ __global__ __launch_bounds__(NT) void k_rms_norm_grad(GradArgs p) {
   }
 }
 
-// dw[c] = the sum of part[b][c] over b, in 64 bits and a fixed order: 16 columns a
-// workgroup, 16 runs of rows each.
+// dw[c] = the sum of part[b][c] over b, in 64 bits and a fixed order: 64 columns a
+// workgroup, in 16 runs of rows.
 __global__ __launch_bounds__(256) void k_rms_norm_join(const float* __restrict__ part, int parts, int64_t d,
                                                        float* __restrict__ dw) {
-  __shared__ double red[16][17];
-  const int c = threadIdx.x & 15, run = threadIdx.x >> 4;
-  const int64_t col = (int64_t)blockIdx.x * 16 + c;
-  double v = 0.0;
-  if (col < d)
-    for (int b = run; b < parts; b += 16) v += (double)part[(int64_t)b * d + col];
-  red[run][c] = v;
-  __syncthreads();
-  if (run == 0 && col < d) {
+  __shared__ double red[16][64];
+  const int run = threadIdx.x >> 4;
+  const int64_t col = (int64_t)blockIdx.x * 64 + 4 * (threadIdx.x & 15), left = d - col;
+  double v[4] = {0.0, 0.0, 0.0, 0.0};
+  for (int b = run; b < parts; b += 16 * 8) {
+    u4 x[8];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) v += red[i][c];
-    dw[col] = (float)v;
+    for (int k = 0; k < 8; ++k)
+      x[k] = b + 16 * k < parts ? load4(part + (int64_t)(b + 16 * k) * d + col, left) : u4{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] += (double)__uint_as_float(x[k][i]);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) red[run][4 * (threadIdx.x & 15) + i] = v[i];
+  __syncthreads();
+  const int64_t c = (int64_t)blockIdx.x * 64 + threadIdx.x;
+  if (threadIdx.x < 64 && c < d) {
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += red[i][threadIdx.x];
+    dw[c] = (float)sum;
   }
 }
 
@@ -326,15 +337,17 @@ hipError_t launch_rms_norm_bfp(const void* x, bool bf16, const float* residual, 
   return norm::launch(a, bf16, norm::kToBfp, s);
 }
 
-int64_t rms_norm_grad_parts(int64_t rows, int64_t d) {
-  (void)d;
-  return rows < 512 ? rows : 512;
+// Workgroups of the gradient: one for each row up to 256, and for every fourth row up to 512.
+int64_t rms_norm_grad_parts(int64_t rows) {
+  if (rows <= 256) return rows;
+  const int64_t n = (rows + 3) / 4;
+  return n < 256 ? 256 : n < 512 ? n : 512;
 }
 
 hipError_t launch_rms_norm_grad(const void* dy, bool bf16, const float* h, const float* rstd, const float* w,
                                 const float* dresidual, int64_t rows, int64_t d, float* dx, float* dw, float* ws,
                                 hipStream_t s) {
-  const int parts = (int)rms_norm_grad_parts(rows, d);
+  const int parts = (int)rms_norm_grad_parts(rows);
   if (rows > 0) {
     const norm::GradArgs a{dy, h, rstd, w, dresidual, rows, d, dx, ws};
     if (bf16) norm::launch_grad_t<fp8::bf16_t>(a, parts, s);
@@ -342,7 +355,7 @@ hipError_t launch_rms_norm_grad(const void* dy, bool bf16, const float* h, const
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(norm::k_rms_norm_join, dim3((unsigned)((d + 15) / 16)), dim3(256), 0, s, ws, parts, d, dw);
+  hipLaunchKernelGGL(norm::k_rms_norm_join, dim3((unsigned)((d + 63) / 64)), dim3(256), 0, s, ws, parts, d, dw);
   return hipGetLastError();
 }
 
