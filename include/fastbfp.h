@@ -878,26 +878,30 @@ int bfp_rms_norm_grad(const void* dy, int dy_type, const float* h, const float* 
  * are exact there and none is out of range) and an order that depends on the sizes alone.
  *   tensors, sizes : HOST arrays of `count` device pointers (contiguous data of `type`,
  *                    aligned to a value) and numbers of values; read before the call returns.
- *   sumsq          : one double.   workspace : bfp_sum_squares_ws_size bytes, 8-byte
- *                    aligned; overwritten.
- * Sums of several cards or shards add up before bfp_clip_gradients.
+ *   sumsq          : one double, or NULL: the sum of the doubles that the call leaves in
+ *                    the workspace is the result then.
+ *   workspace      : bfp_sum_squares_ws_size bytes, 8-byte aligned; overwritten.
+ * Sums of several cards or shards add up before bfp_clip_gradients, or in it.
  */
 int bfp_sum_squares_ws_size(const int64_t* sizes, int64_t count, size_t* workspace_bytes);
 int bfp_sum_squares(const void* const* tensors, int type, const int64_t* sizes, int64_t count, double* sumsq,
                     void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * bfp_clip_gradients -- out[i] = tensors[i] * min(1, max_norm / norm), norm = sqrt(*sumsq):
+ * bfp_clip_gradients -- out[i] = tensors[i] * min(1, max_norm / norm), norm the root of
+ * sumsq[0] + ... + sumsq[sums - 1]:
  * factor and products in 64 bits, rounded to FP32 (and from there to BF16).
  *   out      : HOST array of device pointers; out[i] may be tensors[i] (in place: nothing
  *              moves then unless norm is above max_norm).  Other overlaps of an output with
  *              an input or another output are BFP_E_ARG.
- *   max_norm : not negative, not NaN.   sumsq : as bfp_sum_squares writes it.
+ *   max_norm : not negative, not NaN.
+ *   sumsq    : one double as bfp_sum_squares writes it, or `sums` of them, at most 1024
+ *              (BFP_E_UNSUPPORTED beyond).
  *   norm     : one double, written.
  * A norm that is infinite or NaN scales nothing: the tensors keep the values that made it.
  */
 int bfp_clip_gradients(const void* const* tensors, void* const* out, int type, const int64_t* sizes, int64_t count,
-                       double max_norm, const double* sumsq, double* norm, void* stream);
+                       double max_norm, const double* sumsq, int64_t sums, double* norm, void* stream);
 
 #ifdef __cplusplus
 }

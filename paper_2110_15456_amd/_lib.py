@@ -82,7 +82,7 @@ SIGNATURES = {
     "bfp_rms_norm_grad": (_I, [_P, _I, _P, _P, _P, _P, _I64, _I64, _P, _P, _P, ctypes.c_size_t, _P]),
     "bfp_sum_squares_ws_size": (_I, [_P, _I64, ctypes.POINTER(ctypes.c_size_t)]),
     "bfp_sum_squares": (_I, [_P, _I, _P, _I64, _P, _P, ctypes.c_size_t, _P]),
-    "bfp_clip_gradients": (_I, [_P, _P, _I, _P, _I64, ctypes.c_double, _P, _P, _P]),
+    "bfp_clip_gradients": (_I, [_P, _P, _I, _P, _I64, ctypes.c_double, _P, _I64, _P, _P]),
     "bfp_adaptive_mantissa": (_I, [ctypes.c_double, ctypes.c_double, ctypes.c_double]),
 }
 ABI_VERSION = 10

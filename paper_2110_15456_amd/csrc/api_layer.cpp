@@ -351,7 +351,7 @@ int bfp_sum_squares(const void* const* tensors, int type, const int64_t* sizes, 
                     size_t workspace_bytes, void* stream) {
   const int st = check_list(tensors, type, sizes, count);
   if (st != BFP_OK) return st;
-  if (!sumsq || !aligned(sumsq, 8)) return BFP_E_ARG;
+  if (!aligned(sumsq, 8)) return BFP_E_ARG;
   const uint64_t need = (uint64_t)fastbfp::gradient_pieces(sizes, count) * sizeof(double);
   if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 8))) return BFP_E_ARG;
   if (overlap(sumsq, 8, workspace, need)) return BFP_E_ARG;
@@ -364,20 +364,23 @@ int bfp_sum_squares(const void* const* tensors, int type, const int64_t* sizes, 
 }
 
 int bfp_clip_gradients(const void* const* tensors, void* const* out, int type, const int64_t* sizes, int64_t count,
-                       double max_norm, const double* sumsq, double* norm, void* stream) {
+                       double max_norm, const double* sumsq, int64_t sums, double* norm, void* stream) {
   int st = check_list(tensors, type, sizes, count);
   if (st == BFP_OK) st = check_list(const_cast<const void* const*>(out), type, sizes, count);
   if (st != BFP_OK) return st;
   if (!(max_norm >= 0.0) || !sumsq || !norm || !aligned(sumsq, 8) || !aligned(norm, 8)) return BFP_E_ARG;
-  if (overlap(sumsq, 8, norm, 8)) return BFP_E_ARG;
+  if (sums < 1) return BFP_E_ARG;
+  if (sums > fastbfp::kMostSums) return BFP_E_UNSUPPORTED;
+  const uint64_t sb = (uint64_t)sums * 8;
+  if (overlap(sumsq, sb, norm, 8)) return BFP_E_ARG;
   for (int64_t i = 0; i < count; ++i) {
     const uint64_t n = sizes[i] * bytes_of(type);
-    if (overlap(out[i], n, sumsq, 8) || overlap(out[i], n, norm, 8) || overlap(norm, 8, tensors[i], n)) return BFP_E_ARG;
+    if (overlap(out[i], n, sumsq, sb) || overlap(out[i], n, norm, 8) || overlap(norm, 8, tensors[i], n)) return BFP_E_ARG;
   }
   st = check_apart(tensors, out, bytes_of(type), sizes, count);
   if (st != BFP_OK) return st;
-  return status_of(fastbfp::launch_scale_gradients(tensors, out, type == BFP_BF16, sizes, count, max_norm, sumsq, norm,
-                                                   static_cast<hipStream_t>(stream)));
+  return status_of(fastbfp::launch_scale_gradients(tensors, out, type == BFP_BF16, sizes, count, max_norm, sumsq,
+                                                   (int)sums, norm, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

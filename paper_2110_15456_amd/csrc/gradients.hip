@@ -18,6 +18,7 @@ using fp8::u2;
 using fp8::u4;
 
 constexpr int kUnit = 4096, kPieces = 8192;
+constexpr int kSums = (int)kMostSums;  // that the scaling adds up itself
 
 // N tensors (that many fit in the 4 KB of a launch's arguments): piece of each one's start,
 // and the values of its last piece.
@@ -109,11 +110,19 @@ __global__ __launch_bounds__(256) void k_squares(List<kRead> l, double* __restri
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
-// out = the sum of part[0 .. n), in a fixed order.
+// A thread's share of the sum of v[0 .. n), n up to kSums, on the first 256 threads.
+__device__ __forceinline__ double few_of(const double* v, int n) {
+  double s = 0.0;
+#pragma unroll
+  for (int k = 0; k < kSums / 256; ++k) s += (int)threadIdx.x + 256 * k < n ? v[threadIdx.x + 256 * k] : 0.0;
+  return s;
+}
+
+// out = the sum of part[0 .. n), in a fixed order, of few that of the scaling.
 __global__ __launch_bounds__(1024) void k_squares_join(const double* __restrict__ part, int64_t n,
                                                        double* __restrict__ out) {
-  double sum = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += 8 * 1024) {
+  double sum = n <= kSums && threadIdx.x < 256 ? few_of(part, (int)n) : 0.0;
+  for (int64_t i = n <= kSums ? n : threadIdx.x; i < n; i += 8 * 1024) {
     double v[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = i + 1024 * k < n ? part[i + 1024 * k] : 0.0;
@@ -137,9 +146,9 @@ __host__ __device__ __forceinline__ int ahead(const void* p) {
 // on: what the norm read last is still in the caches behind HBM.
 template <class T>
 __global__ __launch_bounds__(256) void k_scale(List<kWrite> l, Outs o, double max_norm, const double* __restrict__ sumsq,
-                                               double* norm) {
+                                               int sums, double* norm) {
   constexpr int V = 16 / sizeof(T), AT_ONCE = sizeof(T) == 4 ? 4 : 2;
-  const double n2 = sqrt(*sumsq);
+  const double n2 = sqrt(sums == 1 ? *sumsq : block_sum<256>(few_of(sumsq, sums)));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = n2;
   const bool scale = n2 > max_norm && n2 < __builtin_inf();
   const double f = scale ? max_norm / n2 : 1.0;
@@ -199,7 +208,10 @@ __global__ __launch_bounds__(256) void k_scale(List<kWrite> l, Outs o, double ma
   }
 }
 
-__global__ void k_norm(const double* __restrict__ sumsq, double* norm) { *norm = sqrt(*sumsq); }
+__global__ __launch_bounds__(256) void k_norm(const double* __restrict__ sumsq, int sums, double* norm) {
+  const double s = block_sum<256>(few_of(sumsq, sums));
+  if (threadIdx.x == 0) *norm = sqrt(s);
+}
 
 // Values of a piece: 4096 << shift, for at most about kPieces of them.
 int shift_of(const int64_t* sizes, int64_t count) {
@@ -260,13 +272,14 @@ hipError_t launch_sum_squares(const void* const* in, bool bf16, const int64_t* s
     all = done + pieces;
     return hipGetLastError();
   });
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || !sumsq) return e;
   hipLaunchKernelGGL(k_squares_join, dim3(1), dim3(1024), 0, s, ws, all, sumsq);
   return hipGetLastError();
 }
 
 hipError_t launch_scale_gradients(const void* const* in, void* const* out, bool bf16, const int64_t* sizes,
-                                  int64_t count, double max_norm, const double* sumsq, double* norm, hipStream_t s) {
+                                  int64_t count, double max_norm, const double* sumsq, int sums, double* norm,
+                                  hipStream_t s) {
   using namespace grads;
   bool first = true;
   auto before = [&](int64_t i) { return bf16 ? ahead<fp8::bf16_t>(out[i]) : ahead<float>(out[i]); };
@@ -275,12 +288,12 @@ hipError_t launch_scale_gradients(const void* const* in, void* const* out, bool 
     Outs o;
     for (int i = 0; i < l.count; ++i) o.out[i] = out[from + i];
     hipLaunchKernelGGL(bf16 ? k_scale<fp8::bf16_t> : k_scale<float>, dim3((unsigned)pieces), dim3(256), 0, s, l, o,
-                       max_norm, sumsq, first ? norm : nullptr);
+                       max_norm, sumsq, sums, first ? norm : nullptr);
     first = false;
     return hipGetLastError();
   });
   if (e != hipSuccess || !first) return e;
-  hipLaunchKernelGGL(k_norm, dim3(1), dim3(1), 0, s, sumsq, norm);  // (no values)
+  hipLaunchKernelGGL(k_norm, dim3(1), dim3(256), 0, s, sumsq, sums, norm);  // (no values)
   return hipGetLastError();
 }
 

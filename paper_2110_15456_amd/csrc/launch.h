@@ -252,9 +252,11 @@ hipError_t launch_rms_norm_grad(const void* dy, bool bf16, const float* h, const
 
 // The norm over a list of tensors and their scaling (gradients.hip).
 int64_t gradient_pieces(const int64_t* sizes, int64_t count);  // doubles of the workspace
+constexpr int64_t kMostSums = 1024;
+// sumsq null: the pieces' sums stay in ws.
 hipError_t launch_sum_squares(const void* const* in, bool bf16, const int64_t* sizes, int64_t count, double* sumsq, double* ws,
                               hipStream_t s);
 hipError_t launch_scale_gradients(const void* const* in, void* const* out, bool bf16, const int64_t* sizes, int64_t count,
-                                  double max_norm, const double* sumsq, double* norm, hipStream_t s);
+                                  double max_norm, const double* sumsq, int sums, double* norm, hipStream_t s);
 
 }  // namespace fastbfp

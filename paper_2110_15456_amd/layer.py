@@ -6,7 +6,6 @@ from __future__ import annotations
 import ctypes
 import functools
 import math
-from dataclasses import dataclass
 
 import torch
 
@@ -43,7 +42,6 @@ def _on(device, **tensors):
 # ---- 8-bit blocks -------------------------------------------------------
 
 
-@dataclass
 class FP8Tensor:
     """A rows x len tensor of 8-bit codes with a power-of-two scale for each 128 values
     of a row (see include/fastbfp.h).
@@ -51,11 +49,25 @@ class FP8Tensor:
     data: float8 [rows, 128 * blocks], zeros behind a row's last value;
     scales: uint8 [rows, blocks rounded up to a multiple of 4], zeros behind the last.
     """
-    data: torch.Tensor
-    scales: torch.Tensor
-    rows: int
-    len: int
-    fmt: str
+    __slots__ = ("rows", "len", "fmt", "_data", "_scales", "_bytes")
+
+    def __init__(self, data: torch.Tensor, scales: torch.Tensor, rows: int, length: int, fmt: str):
+        self.rows, self.len, self.fmt = rows, length, fmt
+        self._data, self._scales, self._bytes = data, scales, None
+
+    @property
+    def data(self) -> torch.Tensor:
+        if self._data is None:
+            pitch = _pitches(self.len)[0]
+            self._data = self._bytes[:self.rows * pitch].view(self.rows, pitch).view(_format(self.fmt)[1])
+        return self._data
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._scales is None:
+            pitch, ep = _pitches(self.len)
+            self._scales = self._bytes[self.rows * pitch:].view(self.rows, ep)
+        return self._scales
 
     @property
     def codes(self) -> torch.Tensor:
@@ -70,22 +82,44 @@ class FP8Tensor:
 
     @property
     def device(self) -> torch.device:
-        return self.data.device
+        return (self._data if self._bytes is None else self._bytes).device
+
+    def _pointers(self):
+        """Device addresses of the codes and the scales."""
+        if self._bytes is None:
+            return self._data.data_ptr(), self._scales.data_ptr()
+        p = self._bytes.data_ptr()
+        return p, p + self.rows * _pitches(self.len)[0]
 
     @staticmethod
     def empty(rows: int, length: int, fmt: str, device) -> "FP8Tensor":
-        blocks = (length + 127) // 128
-        return FP8Tensor(torch.empty((rows, 128 * blocks), dtype=_format(fmt)[1], device=device),
-                         torch.empty((rows, (blocks + 3) // 4 * 4), dtype=torch.uint8, device=device), rows, length,
-                         fmt)
+        pitch, ep = _pitches(length)
+        return FP8Tensor(torch.empty((rows, pitch), dtype=_format(fmt)[1], device=device),
+                         torch.empty((rows, ep), dtype=torch.uint8, device=device), rows, length, fmt)
+
+    @staticmethod
+    def _one_buffer(rows, length, fmt, device) -> "FP8Tensor":
+        """As empty, both arrays in one allocation and views of them made when asked for:
+        for an operand that goes straight into a product."""
+        pitch, ep = _pitches(length)
+        t = FP8Tensor(None, None, rows, length, fmt)
+        t._bytes = torch.empty(rows * (pitch + ep), dtype=torch.uint8, device=device)
+        return t
 
 
-def _fp8_out(out, rows, length, fmt, device):
+def _pitches(length):
+    """Bytes from one row's codes, and scales, to the next one's."""
+    blocks = (length + 127) // 128
+    return 128 * blocks, (blocks + 3) // 4 * 4
+
+
+def _fp8_out(out, rows, length, fmt, device, make=FP8Tensor._one_buffer):
     if out is None:
-        return FP8Tensor.empty(rows, length, fmt, device)
+        return make(rows, length, fmt, device)
     if (out.rows, out.len, out.fmt) != (rows, length, fmt):
         raise ValueError("out has the wrong shape or format")
-    _on(device, out=out.data)
+    if out.device != device:
+        raise ValueError("out must be on %s" % device)
     return out
 
 
@@ -111,8 +145,8 @@ def quantize_fp8(x: torch.Tensor, axis: int = -1, fmt: str = "e4m3", status: tor
     else:
         raise ValueError("axis must be the last one, or 0 of a 2-D tensor")
     t = _fp8_out(out, rows, length, fmt, x.device)
-    check(load().bfp_quantize_fp8(x.data_ptr(), xt, R, C, 1 if ax == nd - 1 else 0, code, t.data.data_ptr(),
-                                  t.scales.data_ptr(), _status_ptr(status), _stream(x.device)), "bfp_quantize_fp8")
+    check(load().bfp_quantize_fp8(x.data_ptr(), xt, R, C, 1 if ax == nd - 1 else 0, code,
+                                  *t._pointers(), _status_ptr(status), _stream(x.device)), "bfp_quantize_fp8")
     return t
 
 
@@ -126,9 +160,8 @@ def quantize_fp8_dual(x: torch.Tensor, fmt: str = "e4m3", status: torch.Tensor |
         raise ValueError("x must be 2-D")
     R, C = x.shape
     tr, tc = _fp8_out(out_rows, R, C, fmt, x.device), _fp8_out(out_cols, C, R, fmt, x.device)
-    check(load().bfp_quantize_fp8_dual(x.data_ptr(), xt, R, C, code, tr.data.data_ptr(), tr.scales.data_ptr(),
-                                       tc.data.data_ptr(), tc.scales.data_ptr(), _status_ptr(status),
-                                       _stream(x.device)), "bfp_quantize_fp8_dual")
+    check(load().bfp_quantize_fp8_dual(x.data_ptr(), xt, R, C, code, *tr._pointers(), *tc._pointers(),
+                                       _status_ptr(status), _stream(x.device)), "bfp_quantize_fp8_dual")
     return tr, tc
 
 
@@ -139,7 +172,7 @@ def dequantize_fp8(t: FP8Tensor, out: torch.Tensor | None = None) -> torch.Tenso
     if tuple(y.shape) != (t.rows, t.len):
         raise ValueError("out must be [%d, %d]" % (t.rows, t.len))
     _on(t.device, out=y)
-    check(load().bfp_dequantize_fp8(t.data.data_ptr(), t.scales.data_ptr(), t.rows, t.len, _format(t.fmt)[0],
+    check(load().bfp_dequantize_fp8(*t._pointers(), t.rows, t.len, _format(t.fmt)[0],
                                     y.data_ptr(), _stream(t.device)), "bfp_dequantize_fp8")
     return y
 
@@ -170,7 +203,8 @@ def gemm_fp8(A: FP8Tensor, B: FP8Tensor, dtype: torch.dtype | None = None, out: 
     if A.len != B.len:
         raise ValueError("A and B must share K (A: %d, B: %d)" % (A.len, B.len))
     dev = A.device
-    _on(dev, B=B.data)
+    if B.device != dev:
+        raise ValueError("B must be on %s" % dev)
     M, N, K = A.rows, B.rows, A.len
     if out is None:
         C, ldc = torch.empty((M, N), dtype=torch.float32 if dtype is None else dtype, device=dev), N
@@ -202,8 +236,7 @@ def gemm_fp8(A: FP8Tensor, B: FP8Tensor, dtype: torch.dtype | None = None, out: 
                 ws = torch.empty(need, dtype=torch.uint8, device=dev)
             except torch.OutOfMemoryError:
                 need = 0
-    check(load().bfp_gemm_fp8(A.data.data_ptr(), A.scales.data_ptr(), _format(A.fmt)[0], B.data.data_ptr(),
-                              B.scales.data_ptr(), _format(B.fmt)[0], M, N, K, C.data_ptr(), TYPES[C.dtype], ldc,
+    check(load().bfp_gemm_fp8(*A._pointers(), _format(A.fmt)[0], *B._pointers(), _format(B.fmt)[0], M, N, K, C.data_ptr(), TYPES[C.dtype], ldc,
                               ws.data_ptr() if ws is not None else None, need if ws is not None else 0, _stream(dev)),
           "bfp_gemm_fp8")
     return C
@@ -261,9 +294,8 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
         check(load().bfp_rms_norm(*args, y.data_ptr(), _stream(dev)), "bfp_rms_norm")
     elif isinstance(to, str):
         code, _ = _format(to)
-        y = _fp8_out(out, rows, d, to, dev)
-        check(load().bfp_rms_norm_fp8(*args, code, y.data.data_ptr(), y.scales.data_ptr(), _status_ptr(status),
-                                      _stream(dev)), "bfp_rms_norm_fp8")
+        y = _fp8_out(out, rows, d, to, dev, FP8Tensor.empty)
+        check(load().bfp_rms_norm_fp8(*args, code, *y._pointers(), _status_ptr(status), _stream(dev)), "bfp_rms_norm_fp8")
     else:
         if rounding not in ROUNDING:
             raise ValueError("rounding must be one of %s" % sorted(ROUNDING))
@@ -346,7 +378,8 @@ class TensorList:
         self.sizes = (ctypes.c_int64 * n)(*[t.numel() for t in self.tensors])
         nb = ctypes.c_size_t(0)
         check(load().bfp_sum_squares_ws_size(self.sizes, n, ctypes.byref(nb)), "bfp_sum_squares_ws_size")
-        self.work = torch.empty(nb.value // 8, dtype=torch.float64, device=self.device)
+        self.pieces = nb.value // 8
+        self.work = torch.empty(self.pieces + 1, dtype=torch.float64, device=self.device)  # (and their sum)
 
     def __len__(self):
         return len(self.tensors)
@@ -367,7 +400,7 @@ def sum_squares(tensors) -> torch.Tensor:
     added up (all_reduce) before clip_gradients."""
     l = _as_list(tensors)
     out = torch.empty(1, dtype=torch.float64, device=l.device)
-    check(load().bfp_sum_squares(l.ptrs, l.type, l.sizes, len(l), out.data_ptr(), l.work.data_ptr(), 8 * l.work.numel(),
+    check(load().bfp_sum_squares(l.ptrs, l.type, l.sizes, len(l), out.data_ptr(), l.work.data_ptr(), 8 * l.pieces,
                                  _stream(l.device)), "bfp_sum_squares")
     return out
 
@@ -381,13 +414,20 @@ def clip_gradients(tensors, max_norm: float, sumsq: torch.Tensor | None = None) 
     if not max_norm >= 0.0:
         raise ValueError("max_norm must not be negative")
     if sumsq is None:
-        sumsq = sum_squares(l)
+        # (a few pieces' sums are added up by the scaling itself)
+        pieces = l.pieces
+        few = 0 < pieces <= 1024
+        at = l.work.data_ptr() if few else l.work.data_ptr() + 8 * pieces
+        check(load().bfp_sum_squares(l.ptrs, l.type, l.sizes, len(l), None if few else at, l.work.data_ptr(),
+                                     8 * pieces, _stream(l.device)), "bfp_sum_squares")
+        sums = pieces if few else 1
     else:
         _need_cuda(sumsq, "sumsq", torch.float64)
         if sumsq.numel() != 1:
             raise ValueError("sumsq must be one value")
         _on(l.device, sumsq=sumsq)
+        at, sums = sumsq.data_ptr(), 1
     norm = torch.empty(1, dtype=torch.float64, device=l.device)
-    check(load().bfp_clip_gradients(l.ptrs, l.out_ptrs, l.type, l.sizes, len(l), max_norm, sumsq.data_ptr(), norm.data_ptr(),
-                                    _stream(l.device)), "bfp_clip_gradients")
+    check(load().bfp_clip_gradients(l.ptrs, l.out_ptrs, l.type, l.sizes, len(l), max_norm, at, sums,
+                                    norm.data_ptr(), _stream(l.device)), "bfp_clip_gradients")
     return norm

@@ -127,18 +127,19 @@ def test_list_refusals(lib):
     assert lib.bfp_sum_squares_ws_size(sizes(-1), 1, ctypes.byref(need)) == E_ARG
     assert lib.bfp_sum_squares_ws_size(None, 1, ctypes.byref(need)) == E_ARG
     s = lambda p=ptrs(at(0), at(1)), n=sizes(100, 100), c=2, o=at(2), ws=at(3), nb=64, t=0: lib.bfp_sum_squares(p, t, n, c, o, ws, nb, None)  # noqa: E731
-    assert s(p=ptrs(at(0), None)) == s(n=sizes(100, -1)) == s(c=-1) == s(o=None) == s(ws=None) == s(nb=8) == E_ARG
+    assert s(p=ptrs(at(0), None)) == s(n=sizes(100, -1)) == s(c=-1) == s(ws=None) == s(nb=8) == E_ARG
     assert s(t=2) == s(t=1, p=ptrs(at(0), at(1) + 1)) == E_ARG
     assert s(p=ptrs(at(0), at(1) + 2)) == s(o=at(2) + 4) == s(o=at(0)) == s(ws=at(1)) == s(o=at(3)) == E_ARG
 
-    def c(p=ptrs(at(0), at(1)), o=ptrs(at(2), at(3)), n=sizes(100, 100), k=2, m=1.0, sq=at(4), norm=at(5), t=0):
-        return lib.bfp_clip_gradients(p, o, t, n, k, m, sq, norm, None)
+    def c(p=ptrs(at(0), at(1)), o=ptrs(at(2), at(3)), n=sizes(100, 100), k=2, m=1.0, sq=at(4), norm=at(5), t=0, sums=1):
+        return lib.bfp_clip_gradients(p, o, t, n, k, m, sq, sums, norm, None)
     assert c(m=-1.0) == c(m=math.nan) == c(sq=None) == c(norm=None) == c(norm=at(4)) == c(sq=at(4) + 4) == E_ARG
     assert c(p=ptrs(at(0), None)) == c(o=ptrs(None, at(3))) == c(o=None) == E_ARG
     # the same tensor twice in place, outputs over each other or over another input
     assert c(p=ptrs(at(0), at(0)), o=ptrs(at(0), at(0))) == E_ARG
     assert c(o=ptrs(at(2), at(2) + 396)) == c(o=ptrs(at(2), at(2) - 396)) == c(o=ptrs(at(1), at(2))) == E_ARG
     assert c(o=ptrs(at(0) + 4, at(2))) == c(o=ptrs(at(2), at(0) - 4)) == c(o=ptrs(at(0), at(0))) == E_ARG
+    assert c(sums=0) == c(sums=2, norm=at(4) + 8) == c(sums=2, o=ptrs(at(4) + 8, at(3))) == E_ARG and c(sums=1025) == E_UNSUP
     assert c(t=2) == c(t=1, o=ptrs(at(2), at(2) + 198)) == E_ARG
     assert c(norm=at(3)) == c(norm=at(1)) == c(sq=at(2)) == E_ARG
 
