@@ -94,8 +94,8 @@ class FP8Tensor:
     @staticmethod
     def empty(rows: int, length: int, fmt: str, device) -> "FP8Tensor":
         pitch, ep = _pitches(length)
-        return FP8Tensor(torch.empty((rows, pitch), dtype=_format(fmt)[1], device=device),
-                         torch.empty((rows, ep), dtype=torch.uint8, device=device), rows, length, fmt)
+        return FP8Tensor(torch.empty(rows, pitch, dtype=_format(fmt)[1], device=device),
+                         torch.empty(rows, ep, dtype=torch.uint8, device=device), rows, length, fmt)
 
     @staticmethod
     def _one_buffer(rows, length, fmt, device) -> "FP8Tensor":
@@ -207,7 +207,7 @@ def gemm_fp8(A: FP8Tensor, B: FP8Tensor, dtype: torch.dtype | None = None, out: 
         raise ValueError("B must be on %s" % dev)
     M, N, K = A.rows, B.rows, A.len
     if out is None:
-        C, ldc = torch.empty((M, N), dtype=torch.float32 if dtype is None else dtype, device=dev), N
+        C, ldc = torch.empty(M, N, dtype=torch.float32 if dtype is None else dtype, device=dev), N
     else:
         C = out
         if not isinstance(C, torch.Tensor) or not C.is_cuda:
@@ -337,13 +337,12 @@ def rms_norm_grad(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, weight:
             raise ValueError("%s must be %s" % (name, list(shape)))
         _on(dev, **{name: t})
     dx = out if out is not None else torch.empty_like(dy, dtype=torch.float32)
-    # dweight and, behind it, the workspace
     need = _norm_grad_ws(rows, d)
-    buf = torch.empty(d + need // 4, dtype=torch.float32, device=dev)
+    dw, ws = torch.empty(d, dtype=torch.float32, device=dev), torch.empty(need, dtype=torch.uint8, device=dev)
     check(load().bfp_rms_norm_grad(dy.data_ptr(), yt, h.data_ptr(), rstd.data_ptr(), weight.data_ptr(),
                                    dresidual.data_ptr() if dresidual is not None else None, rows, d, dx.data_ptr(),
-                                   buf.data_ptr(), buf.data_ptr() + 4 * d, need, _stream(dev)), "bfp_rms_norm_grad")
-    return dx, buf[:d]
+                                   dw.data_ptr(), ws.data_ptr(), need, _stream(dev)), "bfp_rms_norm_grad")
+    return dx, dw
 
 
 # ---- the gradients' clipping --------------------------------------------
