@@ -528,7 +528,7 @@ Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool room) {
   for (const Kernel& k : kKernels) {
     const int64_t tiles = ((M + k.rows - 1) / k.rows) * ((N + k.cols - 1) / k.cols);
     for (const int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
-      if (want > 1 && (!room || k.waves > 0 || tiles > 1024)) break;
+      if (want > 1 && (!room || k.waves > 0 || tiles > 1024 || 4 * (want - 1) >= slabs)) break;
       // (a part's scales begin at a whole dword)
       const int each = want == 1 ? slabs : ((slabs + want - 1) / want + 3) / 4 * 4, parts = (slabs + each - 1) / each;
       if (parts != want || (parts > 1 && parts * M * gemm_plan_ld(N) > (int64_t(1) << 26))) continue;

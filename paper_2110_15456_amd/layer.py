@@ -49,11 +49,13 @@ class FP8Tensor:
     data: float8 [rows, 128 * blocks], zeros behind a row's last value;
     scales: uint8 [rows, blocks rounded up to a multiple of 4], zeros behind the last.
     """
-    __slots__ = ("rows", "len", "fmt", "_data", "_scales", "_bytes")
+    __slots__ = ("rows", "len", "fmt", "device", "_data", "_scales", "_bytes", "_ptrs")
 
     def __init__(self, data: torch.Tensor, scales: torch.Tensor, rows: int, length: int, fmt: str):
-        self.rows, self.len, self.fmt = rows, length, fmt
+        self.rows, self.len, self.fmt, self.device = rows, length, fmt, data.device
         self._data, self._scales, self._bytes = data, scales, None
+        # what the library takes: the codes' and scales' addresses, and the format
+        self._ptrs = data.data_ptr(), scales.data_ptr(), _format(fmt)[0]
 
     @property
     def data(self) -> torch.Tensor:
@@ -80,17 +82,6 @@ class FP8Tensor:
         blocks = (self.len + 127) // 128
         return self.scales if self.scales.shape[1] == blocks else self.scales[:, :blocks]
 
-    @property
-    def device(self) -> torch.device:
-        return (self._data if self._bytes is None else self._bytes).device
-
-    def _pointers(self):
-        """Device addresses of the codes and the scales."""
-        if self._bytes is None:
-            return self._data.data_ptr(), self._scales.data_ptr()
-        p = self._bytes.data_ptr()
-        return p, p + self.rows * _pitches(self.len)[0]
-
     @staticmethod
     def empty(rows: int, length: int, fmt: str, device) -> "FP8Tensor":
         pitch, ep = _pitches(length)
@@ -102,8 +93,12 @@ class FP8Tensor:
         """As empty, both arrays in one allocation and views of them made when asked for:
         for an operand that goes straight into a product."""
         pitch, ep = _pitches(length)
-        t = FP8Tensor(None, None, rows, length, fmt)
+        t = FP8Tensor.__new__(FP8Tensor)
+        t.rows, t.len, t.fmt, t.device = rows, length, fmt, device
+        t._data = t._scales = None
         t._bytes = torch.empty(rows * (pitch + ep), dtype=torch.uint8, device=device)
+        p = t._bytes.data_ptr()
+        t._ptrs = p, p + rows * pitch, _format(fmt)[0]
         return t
 
 
@@ -131,22 +126,19 @@ def quantize_fp8(x: torch.Tensor, axis: int = -1, fmt: str = "e4m3", status: tor
     quantize's."""
     code, _ = _format(fmt)
     xt = _type(x, "x")
-    nd = x.dim()
+    shape = x.shape
+    nd = len(shape)
     if nd < 1 or not -nd <= axis < nd:
         raise ValueError("axis must be one of x's")
-    ax = axis % nd
-    if ax == nd - 1:
-        C = x.shape[-1]
-        R = math.prod(x.shape[:-1])
-        rows, length = R, C
-    elif nd == 2:
-        R, C = x.shape
-        rows, length = C, R
-    else:
+    along = axis == -1 or axis == nd - 1
+    C = shape[-1]
+    R = shape[0] if nd == 2 else math.prod(shape[:-1])
+    if not along and nd != 2:
         raise ValueError("axis must be the last one, or 0 of a 2-D tensor")
-    t = _fp8_out(out, rows, length, fmt, x.device)
-    check(load().bfp_quantize_fp8(x.data_ptr(), xt, R, C, 1 if ax == nd - 1 else 0, code,
-                                  *t._pointers(), _status_ptr(status), _stream(x.device)), "bfp_quantize_fp8")
+    t = _fp8_out(out, R if along else C, C if along else R, fmt, x.device)
+    codes, scales, _ = t._ptrs
+    check(load().bfp_quantize_fp8(x.data_ptr(), xt, R, C, 1 if along else 0, code, codes, scales, _status_ptr(status),
+                                  _stream(t.device)), "bfp_quantize_fp8")
     return t
 
 
@@ -160,7 +152,7 @@ def quantize_fp8_dual(x: torch.Tensor, fmt: str = "e4m3", status: torch.Tensor |
         raise ValueError("x must be 2-D")
     R, C = x.shape
     tr, tc = _fp8_out(out_rows, R, C, fmt, x.device), _fp8_out(out_cols, C, R, fmt, x.device)
-    check(load().bfp_quantize_fp8_dual(x.data_ptr(), xt, R, C, code, *tr._pointers(), *tc._pointers(),
+    check(load().bfp_quantize_fp8_dual(x.data_ptr(), xt, R, C, code, *tr._ptrs[:2], *tc._ptrs[:2],
                                        _status_ptr(status), _stream(x.device)), "bfp_quantize_fp8_dual")
     return tr, tc
 
@@ -172,7 +164,7 @@ def dequantize_fp8(t: FP8Tensor, out: torch.Tensor | None = None) -> torch.Tenso
     if tuple(y.shape) != (t.rows, t.len):
         raise ValueError("out must be [%d, %d]" % (t.rows, t.len))
     _on(t.device, out=y)
-    check(load().bfp_dequantize_fp8(*t._pointers(), t.rows, t.len, _format(t.fmt)[0],
+    check(load().bfp_dequantize_fp8(*t._ptrs[:2], t.rows, t.len, t._ptrs[2],
                                     y.data_ptr(), _stream(t.device)), "bfp_dequantize_fp8")
     return y
 
@@ -236,7 +228,7 @@ def gemm_fp8(A: FP8Tensor, B: FP8Tensor, dtype: torch.dtype | None = None, out: 
                 ws = torch.empty(need, dtype=torch.uint8, device=dev)
             except torch.OutOfMemoryError:
                 need = 0
-    check(load().bfp_gemm_fp8(*A._pointers(), _format(A.fmt)[0], *B._pointers(), _format(B.fmt)[0], M, N, K, C.data_ptr(), TYPES[C.dtype], ldc,
+    check(load().bfp_gemm_fp8(*A._ptrs, *B._ptrs, M, N, K, C.data_ptr(), TYPES[C.dtype], ldc,
                               ws.data_ptr() if ws is not None else None, need if ws is not None else 0, _stream(dev)),
           "bfp_gemm_fp8")
     return C
@@ -250,8 +242,9 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
              out=None, status: torch.Tensor | None = None):
     """The root-mean-square norm of x's rows (its last axis, at most 16384 values; the
     leading axes are the rows) with a residual's addition in front: ``(y, h, rstd)`` with
-    h = x + residual (without one, x, or x in FP32 where it is BF16 and save is set), rstd = (mean(h^2) + eps)^(-1/2) and y = h *
-    rstd * weight, computed in 64 bits and rounded once.
+    h = x + residual (without one, x, or x in FP32 where it is BF16 and save is set), rstd
+    = (mean(h^2) + eps)^(-1/2) and y = h * rstd * weight, computed in 64 bits and rounded
+    once.
 
     to        None: y in FP32, of x's shape; "e4m3" or "e5m2": an FP8Tensor; 1 .. 8: a
               BFPTensor of that width in groups of 16 (``rounding`` and ``seed`` as
@@ -261,41 +254,43 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
     h_out     where h goes; residual or an FP32 x: in place.
     out       a preallocated y.   status: as quantize's, of the converted y."""
     xt = _type(x, "x")
-    if x.dim() < 1:
+    shape = x.shape
+    if len(shape) < 1:
         raise ValueError("x must have at least one dimension")
-    d = x.shape[-1]
-    rows = x.numel() // d if d else math.prod(x.shape[:-1])
+    d = shape[-1]
+    rows = shape[0] if len(shape) == 2 else math.prod(shape[:-1])
     dev = x.device
     _need_cuda(weight, "weight", torch.float32)
     if weight.dim() != 1 or weight.shape[0] != d:
         raise ValueError("weight must be [%d]" % d)
-    _on(dev, weight=weight, h_out=h_out, status=status)
     h = h_out
     if residual is not None:
         _need_cuda(residual, "residual", torch.float32)
-        if residual.shape != x.shape:
+        if residual.shape != shape:
             raise ValueError("residual must have x's shape")
-        _on(dev, residual=residual)
-    if h is None and (residual is not None or (xt and save)):
-        h = torch.empty_like(x, dtype=torch.float32)
-    if h_out is not None:
-        _need_cuda(h_out, "h_out", torch.float32)
-        if h_out.shape != x.shape:
+    if h is None:
+        if residual is not None or (xt and save):
+            h = torch.empty_like(x, dtype=torch.float32)
+    else:
+        _need_cuda(h, "h_out", torch.float32)
+        if h.shape != shape:
             raise ValueError("h_out must have x's shape")
+    if weight.device != dev or (residual is not None and residual.device != dev) or h_out is not None or status is not None:
+        _on(dev, weight=weight, residual=residual, h_out=h_out, status=status)
     rstd = torch.empty(rows, dtype=torch.float32, device=dev) if save else None
     args = (x.data_ptr(), xt, residual.data_ptr() if residual is not None else None, weight.data_ptr(), rows, d, eps,
             h.data_ptr() if h is not None else None, rstd.data_ptr() if save else None)
     if to is None:
         y = out if out is not None else torch.empty_like(x, dtype=torch.float32)
         _need_cuda(y, "out", torch.float32)
-        if y.shape != x.shape:
+        if y.shape != shape:
             raise ValueError("out must have x's shape")
         _on(dev, out=y)
         check(load().bfp_rms_norm(*args, y.data_ptr(), _stream(dev)), "bfp_rms_norm")
     elif isinstance(to, str):
         code, _ = _format(to)
         y = _fp8_out(out, rows, d, to, dev, FP8Tensor.empty)
-        check(load().bfp_rms_norm_fp8(*args, code, *y._pointers(), _status_ptr(status), _stream(dev)), "bfp_rms_norm_fp8")
+        check(load().bfp_rms_norm_fp8(*args, code, *y._ptrs[:2], _status_ptr(status), _stream(dev)), "bfp_rms_norm_fp8")
     else:
         if rounding not in ROUNDING:
             raise ValueError("rounding must be one of %s" % sorted(ROUNDING))
