@@ -78,11 +78,12 @@ __device__ __forceinline__ void spread() {
 // takes as long as its loads do (1024 x 1024 x 8192 with two 34.8 us, with four 20.9; of 900
 // drawn products those on the 64 tile lose 1% with four alone).
 //
-// Measured: 4096 x 4096 x 16384 2.7 PFLOP/s, 8192 x 16384 x 4096 445 us, 2.47; a library's
-// FP8 product of 8192^3 reaches 2.64 on the same card.  The MFMAs alone, fed with nothing,
-// take 85% of that time (77% of the second's, which writes more): the clock falls under
-// them.  The 128 tile, two workgroups on a CU, is held to 1.95 by the LDS, which moves
-// 1.5 bytes for each of the 256 tile's.
+// Measured (BF16 out): 4096 x 4096 x 8192 97 us, 2.83 PFLOP/s; 8192 x 16384 x 4096 410 us,
+// 2.68; 8192 x 4096 x 4096 103 us, 2.66; a library's FP8 product of 8192^3 reaches 2.64 on
+// the same card.  The matrix units are busy for 73 to 78% of the cycles, at 1.6 to 1.7 GHz:
+// the power they draw holds the clock down, and faster feeding lowers it further.  A round
+// of tiles ends with 5.5 us of writing C.  The 128 tile, two workgroups on a CU, is held
+// to 1.95 by the LDS, which moves 1.5 bytes for each of the 256 tile's.
 template <int BM, int BN, int FA, int FB, class T>
 __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
   constexpr int ST = BM == 64 ? 4 : 2;
@@ -117,19 +118,20 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
   const uint32_t lane_off =
       (uint32_t)(8 * wave + (lane >> 3)) * p.pitch + (uint32_t)((lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7)) * 16;
   const uint32_t step_off = 8 * NW * p.pitch;  // from one of a wave's loads to the next
-  // (slabs behind the last one: the loads find an empty buffer and write zeros, so that the
-  // loop has no branch around them)
+  // (All of an offset is the lane's: the buffer's bound does not count a scalar one.  Slabs
+  // behind the last one: the loads find an empty buffer and write zeros, so that the loop
+  // has no branch around them.)
   auto issue = [&](uint8_t* stage, int s) __attribute__((always_inline)) {
     const uint32_t k0 = (uint32_t)(slab0 + s) * kBlock;
     const rsrc_t sa = make_rsrc(pa, s < nslabs ? size_a : 0u), sb = make_rsrc(pb, s < nslabs ? size_b : 0u);
 #pragma unroll
     for (int u = 0; u < LA; ++u)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(sa, (lds_void*)(stage + (wave + NW * u) * 1024), 16, lane_off,
-                                               k0 + u * step_off, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(sa, (lds_void*)(stage + (wave + NW * u) * 1024), 16,
+                                               lane_off + (k0 + u * step_off), 0, 0, 0);
 #pragma unroll
     for (int u = 0; u < LB; ++u)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(sb, (lds_void*)(stage + OFF_B + (wave + NW * u) * 1024), 16, lane_off,
-                                               k0 + u * step_off, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(sb, (lds_void*)(stage + OFF_B + (wave + NW * u) * 1024), 16,
+                                               lane_off + (k0 + u * step_off), 0, 0, 0);
   };
   const int fr = lane & 31, fk = lane >> 5, fsw = (fr >> 1) & 7;
   // (the chunks of a lane's 32 bytes of step h: 4 h + 2 fk and the one beside it)
@@ -143,7 +145,7 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
   // The scales of slab s and its neighbours of a dword, for each row of A and then of B, to
   // LDS: 64 rows at a time, which of them goes by the wave.  (A lane's
   // own loads of its rows' dwords, each in a line of its own, took as long as half of the
-  // codes' loads.)
+  // codes' loads: 8192 x 16384 x 4096 445 us with them, 404 so.)
   constexpr int RUNS = (BM + BN) / 64, LS = RUNS < NW ? 1 : RUNS / NW;  // loads of a wave
   auto issue_scales = [&](int s) __attribute__((always_inline)) {
     const int first = s & ~3, quad = (s >> 2) & 1;
@@ -153,8 +155,8 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
       const bool of_b = run >= BM / 64;
       const rsrc_t rs = make_rsrc(of_b ? peb : pea, first < nslabs ? (uint32_t)(of_b ? brows : arows) * p.epitch : 0u);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(scale_stage + quad * (BM + BN) + run * 64), 4,
-                                               (uint32_t)((of_b ? run - BM / 64 : run) * 64 + lane) * p.epitch,
-                                               slab0 + first, 0, 0);
+                                               (uint32_t)((of_b ? run - BM / 64 : run) * 64 + lane) * p.epitch +
+                                                   (uint32_t)(slab0 + first), 0, 0, 0);
     }
   };
   auto read_scales = [&](int s, int (&sa)[TM], int (&sb)[TN]) __attribute__((always_inline)) {
@@ -297,7 +299,8 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
 // its own part of LDS, so that the waves never meet before their sums are added, in their
 // order.  What bounds these products is the bytes of B on the way: direct buffer -> LDS
 // loads of whole lines (8 rows x 128 bytes each) move them; loads straight into the
-// registers' layout touch 16 rows at once and were held to 4 TB/s by the L1's lookups.
+// registers' layout touch 16 rows at once and were held to 4 TB/s by the L1's lookups
+// (16 x 16384 x 4096: 18.1 us with them, 12.4 so, 5.5 TB/s of B).
 template <int RM, int RN, int WAVES, int FA, int FB, class T>
 __global__ __launch_bounds__(64 * WAVES) void k_gemm_fp8_few(Gemm p) {
   constexpr int ROWS = 16 * (RM + RN), PART = ROWS * kBlock;  // a wave's slab
@@ -330,14 +333,14 @@ __global__ __launch_bounds__(64 * WAVES) void k_gemm_fp8_few(Gemm p) {
     for (int i = 0; i < RM; ++i)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(mine + (2 * i + u) * 1024), 16, load_off[u],
-                                                 (uint32_t)slab * kBlock + 16 * i * p.pitch, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(mine + (2 * i + u) * 1024), 16,
+                                                 load_off[u] + ((uint32_t)slab * kBlock + 16 * i * p.pitch), 0, 0, 0);
 #pragma unroll
     for (int j = 0; j < RN; ++j)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void*)(mine + (2 * (RM + j) + u) * 1024), 16, load_off[u],
-                                                 (uint32_t)slab * kBlock + 16 * j * p.pitch, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void*)(mine + (2 * (RM + j) + u) * 1024), 16,
+                                                 load_off[u] + ((uint32_t)slab * kBlock + 16 * j * p.pitch), 0, 0, 0);
   };
   const int r = lane & 15, q = lane >> 4, rsw = (r >> 1) & 7;
   int sa[RM], sb[RN], na[RM], nb[RN];
@@ -346,10 +349,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_gemm_fp8_few(Gemm p) {
     const rsrc_t rb = make_rsrc(peb, super < supers ? brows * p.epitch : 0u);
 #pragma unroll
     for (int i = 0; i < RM; ++i)
-      na[i] = (int)__builtin_amdgcn_raw_buffer_load_b32(ra, (uint32_t)(16 * i + r) * p.epitch, 4 * super, 0);
+      na[i] = (int)__builtin_amdgcn_raw_buffer_load_b32(ra, (uint32_t)(16 * i + r) * p.epitch + 4 * super, 0, 0);
 #pragma unroll
     for (int j = 0; j < RN; ++j)
-      nb[j] = (int)__builtin_amdgcn_raw_buffer_load_b32(rb, (uint32_t)(16 * j + r) * p.epitch, 4 * super, 0);
+      nb[j] = (int)__builtin_amdgcn_raw_buffer_load_b32(rb, (uint32_t)(16 * j + r) * p.epitch + 4 * super, 0, 0);
   };
   auto frag = [&](const uint8_t* at) __attribute__((always_inline)) -> v8i {
     const u4 x = *reinterpret_cast<const u4*>(at + r * kBlock + ((2 * q) ^ rsw) * 16);
