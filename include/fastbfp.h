@@ -21,7 +21,7 @@
  *     (hipMalloc'd or torch CUDA tensors); pointers to size_t outputs are HOST
  *     pointers.  The caller owns every buffer; the library allocates nothing
  *     and keeps no state besides a per-device properties cache.
- *   - stream is a hipStream_t passed as void* (NULL = the default stream).
+ *   - stream is a hipStream_t passed as void* (NULL = the current device's default stream).
  *     Calls enqueue work on it and return without synchronising.
  *   - Every argument and shape check happens on the host before any launch;
  *     a failed check returns a non-zero bfp_status_t and enqueues nothing.
@@ -766,7 +766,8 @@ int bfp_orthogonalize_route(int64_t batch, int64_t rows, int64_t cols, int* tile
  * value is at most the format's; codes are the nearest ones to value / scale, ties to
  * even.  FP32 subnormals read as zero.  Infinities and NaN are stored as NaN, do not
  * count for the scale, and set bit 0 of the status word.
- * len is at most 2^23 (BFP_E_UNSUPPORTED beyond).
+ * len is at most 2^23 (BFP_E_UNSUPPORTED beyond, as in these entry points wherever a launch
+ * would need 2^32 threads: some 2^34 values or more).
  */
 typedef enum {
   BFP_FP8_E4M3 = 0,
@@ -860,6 +861,7 @@ int bfp_rms_norm_bfp(const void* x, int x_type, const float* residual, const flo
 /*
  * bfp_rms_norm_grad -- its gradients, with u = weight dy:
  *   dx = r u - h r^3 mean(u h) + dresidual,  dweight = sum over the rows of dy h r
+ *   (as r (u - n mean(u n)) with n = h r, which is in range for any h)
  *   dy        : dy_type [rows][d].   h, rstd : of the forward pass.   dresidual : optional, the gradient that reaches h
  *               beside the norm; dx is the gradient of x and of the residual alike.
  *   dx        : FP32 [rows][d]; may be an FP32 dy or dresidual (in place).

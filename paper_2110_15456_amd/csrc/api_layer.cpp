@@ -23,6 +23,7 @@ using fastbfp::fp8::exp_pitch;
 
 constexpr int64_t kMost = int64_t(1) << 23;  // of a row's values: 256 rows of codes within 2^31 bytes
 constexpr int64_t kGrid = 0x7fffffff;
+using fastbfp::kMostThreads;
 
 bool type_ok(int t) { return t == BFP_F32 || t == BFP_BF16; }
 uint64_t bytes_of(int t) { return t == BFP_F32 ? 4 : 2; }
@@ -46,13 +47,13 @@ bool codes_ok(const uint8_t* codes, const uint8_t* exps) {
 int check_product(int64_t M, int64_t N, int64_t K) {
   if (M < 0 || N < 0 || K < 0) return BFP_E_ARG;
   if (K > kMost || M > kGrid || N > kGrid) return BFP_E_UNSUPPORTED;
-  if (((M + 63) / 64) * ((N + 63) / 64) > kGrid / 64 || (K == 0 && N > 0 && M > kGrid / N * 256)) return BFP_E_UNSUPPORTED;
+  if (((M + 63) / 64) * ((N + 63) / 64) > kGrid / 64 || (K == 0 && N > 0 && M > kMostThreads / N)) return BFP_E_UNSUPPORTED;
   return BFP_OK;
 }
 
 int check_norm(int64_t rows, int64_t d) {
   if (rows < 0 || d < 0) return BFP_E_ARG;
-  if (d > fastbfp::kMaxNorm || rows > kGrid) return BFP_E_UNSUPPORTED;
+  if (d > fastbfp::kMaxNorm || rows > kMostThreads / fastbfp::rms_norm_threads(d)) return BFP_E_UNSUPPORTED;
   return BFP_OK;
 }
 
@@ -162,7 +163,8 @@ int bfp_quantize_fp8(const void* x, int x_type, int64_t R, int64_t C, int group_
   if (rows == 0 || len == 0) return BFP_OK;
   if (!x || !aligned(x, bytes_of(x_type)) || !codes_ok(codes, exp) || !aligned(status_word, 4)) return BFP_E_ARG;
   const int64_t quads = (fastbfp::fp8::blocks_of(len) + 3) / 4;
-  if (group_axis == 1 ? R > kGrid / quads : fastbfp::fp8::blocks_of(C) > kGrid / fastbfp::fp8::blocks_of(R))
+  if (group_axis == 1 ? R > kMostThreads / 32 / quads
+                      : fastbfp::fp8::blocks_of(C) > kMostThreads / 256 / fastbfp::fp8::blocks_of(R))
     return BFP_E_UNSUPPORTED;
   const uint64_t n = (uint64_t)R * C * bytes_of(x_type), cb = code_bytes(rows, len), eb = exp_bytes(rows, len);
   if (overlap(codes, cb, x, n) || overlap(exp, eb, x, n) || overlap(codes, cb, exp, eb)) return BFP_E_ARG;
@@ -179,7 +181,7 @@ int bfp_quantize_fp8_dual(const void* x, int x_type, int64_t R, int64_t C, int f
   if (R == 0 || C == 0) return BFP_OK;
   if (!x || !aligned(x, bytes_of(x_type)) || !codes_ok(codes_r, exp_r) || !codes_ok(codes_c, exp_c) || !aligned(status_word, 4))
     return BFP_E_ARG;
-  if (fastbfp::fp8::blocks_of(C) > kGrid / fastbfp::fp8::blocks_of(R)) return BFP_E_UNSUPPORTED;
+  if (fastbfp::fp8::blocks_of(C) > kMostThreads / 256 / fastbfp::fp8::blocks_of(R)) return BFP_E_UNSUPPORTED;
   const uint64_t n = (uint64_t)R * C * bytes_of(x_type);
   const void* o[4] = {codes_r, exp_r, codes_c, exp_c};
   const uint64_t b[4] = {code_bytes(R, C), exp_bytes(R, C), code_bytes(C, R), exp_bytes(C, R)};
@@ -198,7 +200,7 @@ int bfp_dequantize_fp8(const uint8_t* codes, const uint8_t* exp, int64_t rows, i
   if (st != BFP_OK) return st;
   if (rows == 0 || len == 0) return BFP_OK;
   if (!codes_ok(codes, exp) || !y || !aligned(y, 4)) return BFP_E_ARG;
-  if (rows > kGrid * 256 / ((len + 3) / 4)) return BFP_E_UNSUPPORTED;
+  if (rows > kMostThreads / ((len + 3) / 4)) return BFP_E_UNSUPPORTED;
   const uint64_t n = (uint64_t)rows * len * 4;
   if (overlap(y, n, codes, code_bytes(rows, len)) || overlap(y, n, exp, exp_bytes(rows, len))) return BFP_E_ARG;
   return status_of(

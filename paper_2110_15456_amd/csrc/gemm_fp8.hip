@@ -535,6 +535,7 @@ Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool room) {
       // (a part's scales begin at a whole dword)
       const int each = want == 1 ? slabs : ((slabs + want - 1) / want + 3) / 4 * 4, parts = (slabs + each - 1) / each;
       if (parts != want || (parts > 1 && parts * M * gemm_plan_ld(N) > (int64_t(1) << 26))) continue;
+      if (tiles * parts * (k.waves ? 64 * k.waves : 256) > kMostThreads) continue;
       float t = price(k, tiles * parts, each);
       if (parts > 1) t += kJoin + kJoinValue * (float)parts * (float)M * (float)N;
       if (t < least) {

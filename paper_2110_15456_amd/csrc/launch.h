@@ -236,6 +236,9 @@ hipError_t launch_gemm_fp8(const Fp8Plan& plan, const uint8_t* a, const uint8_t*
                            float* ws, hipStream_t s);
 
 // The norm (rms_norm.hip).  residual, h and rstd may be null.
+// Threads of a launch, which HIP wants below 2^32 (what a whole workgroup adds left over).
+constexpr int64_t kMostThreads = (int64_t(1) << 32) - 1024;
+
 constexpr int64_t kMaxNorm = 16384;  // values of a row
 hipError_t launch_rms_norm(const void* x, bool bf16, const float* residual, const float* w, int64_t rows, int64_t d, double eps,
                            float* h, float* rstd, float* y, hipStream_t s);
@@ -245,6 +248,7 @@ hipError_t launch_rms_norm_fp8(const void* x, bool bf16, const float* residual, 
 hipError_t launch_rms_norm_bfp(const void* x, bool bf16, const float* residual, const float* w, int64_t rows, int64_t d,
                                double eps, float* h, float* rstd, int m, int mode, uint64_t seed, uint8_t* mant,
                                uint8_t* exps, uint32_t* status, hipStream_t s);
+int64_t rms_norm_threads(int64_t d);  // of a row
 int64_t rms_norm_grad_parts(int64_t rows);  // rows of d values in the workspace
 hipError_t launch_rms_norm_grad(const void* dy, bool bf16, const float* h, const float* rstd, const float* w,
                                 const float* dresidual, int64_t rows, int64_t d, float* dx, float* dw, float* ws,

@@ -138,8 +138,9 @@ __global__ __launch_bounds__(NT) void k_rms_norm(Args p) {
   }
 }
 
-// The gradients, for u = w dy and h, r of the forward pass:
-//   dx = r u - h r^3 mean(u h) (+ dresidual),  dw = sum over rows of dy h r
+// The gradients, for u = w dy, h and r of the forward pass and n = h r (at most sqrt(d),
+// so that nothing leaves FP32's range on the way, however large or small h is):
+//   dx = r (u - n mean(u n)) (+ dresidual),  dw = sum over rows of dy n
 // A workgroup takes rows b, b + gridDim, ...; its share of dw stays in registers, in 64
 // bits, and goes to part[b] in FP32.
 struct GradArgs {
@@ -178,15 +179,15 @@ __global__ __launch_bounds__(NT) void k_rms_norm_grad(GradArgs p) {
       float s4 = 0.0f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float dy = __uint_as_float(g[k][i]), hv = __uint_as_float(h[k][i]);
-        s4 = __builtin_fmaf(dy * __uint_as_float(w[k][i]), hv, s4);
-        dw[k][i] += (double)(dy * (hv * r));
+        const float dy = __uint_as_float(g[k][i]), n = __uint_as_float(h[k][i]) * r;
+        s4 = __builtin_fmaf(dy * __uint_as_float(w[k][i]), n, s4);
+        dw[k][i] += (double)(dy * n);
       }
       sum += (double)s4;
     }
     // (two places for the waves' sums: a wave may be a row ahead of one that still reads)
     sum = block_sum<NT>(sum, red[turn]);
-    const float a = (float)((double)r * (double)r * (double)r * (sum / (double)d));
+    const float a = (float)((double)r * (sum / (double)d));
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int64_t c = 4 * (t + NT * k);
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(NT) void k_rms_norm_grad(GradArgs p) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float u = __uint_as_float(g[k][i]) * __uint_as_float(w[k][i]);
-        float v = __builtin_fmaf(-__uint_as_float(h[k][i]), a, u * r);
+        float v = __builtin_fmaf(-(__uint_as_float(h[k][i]) * r), a, u * r);
         if constexpr (RES) v += __uint_as_float(z[k][i]);
         o[i] = __float_as_uint(v);
       }
@@ -336,6 +337,8 @@ hipError_t launch_rms_norm_bfp(const void* x, bool bf16, const float* residual, 
            (uint32_t)(seed >> 32)};
   return norm::launch(a, bf16, norm::kToBfp, s);
 }
+
+int64_t rms_norm_threads(int64_t d) { return norm::shape_of(d).nt; }
 
 // Workgroups of the gradient: one for each row up to 256, and for every fourth row up to 512.
 int64_t rms_norm_grad_parts(int64_t rows) {

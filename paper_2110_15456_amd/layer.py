@@ -9,7 +9,7 @@ import math
 
 import torch
 
-from . import ROUNDING, BFPTensor, _need_cuda, _status_ptr, _stream
+from . import ROUNDING, BFPTensor, _need_cuda, _stream
 from ._lib import check, load
 
 # Of a format: the ABI's number and torch's type.
@@ -25,6 +25,31 @@ def _type(t, name):
     if t.dtype not in TYPES:
         raise TypeError("%s must have dtype torch.float32 or torch.bfloat16, got %s" % (name, t.dtype))
     return TYPES[t.dtype]
+
+
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _call(name, dev, *args):
+    """The library's ``name`` on dev's current stream.  dev is the current device for the
+    call: the default stream's handle names the current device's."""
+    f = getattr(load(), name)
+    if _current_device() == dev.index:
+        check(f(*args, _stream(dev)), name)
+    else:
+        with torch.cuda.device(dev):
+            check(f(*args, _stream(dev)), name)
+
+
+def _status(status, dev):
+    """The address of a status word, or None."""
+    if status is None:
+        return None
+    _need_cuda(status, "status")
+    if status.dtype not in (torch.int32, torch.uint32) or status.numel() != 1:
+        raise TypeError("status must be one int32 or uint32 value")
+    _on(dev, status=status)
+    return status.data_ptr()
 
 
 def _format(fmt):
@@ -52,6 +77,14 @@ class FP8Tensor:
     __slots__ = ("rows", "len", "fmt", "device", "_data", "_scales", "_bytes", "_ptrs")
 
     def __init__(self, data: torch.Tensor, scales: torch.Tensor, rows: int, length: int, fmt: str):
+        for name, t, dtype, pitch in (("data", data, _format(fmt)[1], _pitches(length)[0]),
+                                      ("scales", scales, torch.uint8, _pitches(length)[1])):
+            if t.dtype != dtype:
+                raise TypeError("%s must have dtype %s, got %s" % (name, dtype, t.dtype))
+            if tuple(t.shape) != (rows, pitch) or not t.is_contiguous():
+                raise ValueError("%s must be [%d, %d], contiguous" % (name, rows, pitch))
+        if scales.device != data.device:
+            raise ValueError("scales must be on %s" % data.device)
         self.rows, self.len, self.fmt, self.device = rows, length, fmt, data.device
         self._data, self._scales, self._bytes = data, scales, None
         # what the library takes: the codes' and scales' addresses, and the format
@@ -137,8 +170,8 @@ def quantize_fp8(x: torch.Tensor, axis: int = -1, fmt: str = "e4m3", status: tor
         raise ValueError("axis must be the last one, or 0 of a 2-D tensor")
     t = _fp8_out(out, R if along else C, C if along else R, fmt, x.device)
     codes, scales, _ = t._ptrs
-    check(load().bfp_quantize_fp8(x.data_ptr(), xt, R, C, 1 if along else 0, code, codes, scales, _status_ptr(status),
-                                  _stream(t.device)), "bfp_quantize_fp8")
+    _call("bfp_quantize_fp8", x.device, x.data_ptr(), xt, R, C, 1 if along else 0, code, codes, scales,
+          _status(status, x.device))
     return t
 
 
@@ -152,8 +185,8 @@ def quantize_fp8_dual(x: torch.Tensor, fmt: str = "e4m3", status: torch.Tensor |
         raise ValueError("x must be 2-D")
     R, C = x.shape
     tr, tc = _fp8_out(out_rows, R, C, fmt, x.device), _fp8_out(out_cols, C, R, fmt, x.device)
-    check(load().bfp_quantize_fp8_dual(x.data_ptr(), xt, R, C, code, *tr._ptrs[:2], *tc._ptrs[:2],
-                                       _status_ptr(status), _stream(x.device)), "bfp_quantize_fp8_dual")
+    _call("bfp_quantize_fp8_dual", x.device, x.data_ptr(), xt, R, C, code, *tr._ptrs[:2], *tc._ptrs[:2],
+          _status(status, x.device))
     return tr, tc
 
 
@@ -164,8 +197,7 @@ def dequantize_fp8(t: FP8Tensor, out: torch.Tensor | None = None) -> torch.Tenso
     if tuple(y.shape) != (t.rows, t.len):
         raise ValueError("out must be [%d, %d]" % (t.rows, t.len))
     _on(t.device, out=y)
-    check(load().bfp_dequantize_fp8(*t._ptrs[:2], t.rows, t.len, t._ptrs[2],
-                                    y.data_ptr(), _stream(t.device)), "bfp_dequantize_fp8")
+    _call("bfp_dequantize_fp8", t.device, *t._ptrs[:2], t.rows, t.len, t._ptrs[2], y.data_ptr())
     return y
 
 
@@ -195,6 +227,8 @@ def gemm_fp8(A: FP8Tensor, B: FP8Tensor, dtype: torch.dtype | None = None, out: 
     if A.len != B.len:
         raise ValueError("A and B must share K (A: %d, B: %d)" % (A.len, B.len))
     dev = A.device
+    if dev.type != "cuda":
+        raise TypeError("A and B must be on a CUDA (HIP) device")
     if B.device != dev:
         raise ValueError("B must be on %s" % dev)
     M, N, K = A.rows, B.rows, A.len
@@ -228,9 +262,8 @@ def gemm_fp8(A: FP8Tensor, B: FP8Tensor, dtype: torch.dtype | None = None, out: 
                 ws = torch.empty(need, dtype=torch.uint8, device=dev)
             except torch.OutOfMemoryError:
                 need = 0
-    check(load().bfp_gemm_fp8(*A._ptrs, *B._ptrs, M, N, K, C.data_ptr(), TYPES[C.dtype], ldc,
-                              ws.data_ptr() if ws is not None else None, need if ws is not None else 0, _stream(dev)),
-          "bfp_gemm_fp8")
+    _call("bfp_gemm_fp8", dev, *A._ptrs, *B._ptrs, M, N, K, C.data_ptr(), TYPES[C.dtype], ldc,
+          ws.data_ptr() if ws is not None else None, need if ws is not None else 0)
     return C
 
 
@@ -275,9 +308,11 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
         _need_cuda(h, "h_out", torch.float32)
         if h.shape != shape:
             raise ValueError("h_out must have x's shape")
-    if weight.device != dev or (residual is not None and residual.device != dev) or h_out is not None or status is not None:
-        _on(dev, weight=weight, residual=residual, h_out=h_out, status=status)
-    rstd = torch.empty(rows, dtype=torch.float32, device=dev) if save else None
+    if weight.device != dev or (residual is not None and residual.device != dev) or h_out is not None:
+        _on(dev, weight=weight, residual=residual, h_out=h_out)
+    rstd = None
+    if save:  # (the mean of no values: NaN)
+        rstd = torch.empty(rows, device=dev, dtype=torch.float32) if d else torch.full((rows,), math.nan, device=dev)
     args = (x.data_ptr(), xt, residual.data_ptr() if residual is not None else None, weight.data_ptr(), rows, d, eps,
             h.data_ptr() if h is not None else None, rstd.data_ptr() if save else None)
     if to is None:
@@ -286,11 +321,11 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
         if y.shape != shape:
             raise ValueError("out must have x's shape")
         _on(dev, out=y)
-        check(load().bfp_rms_norm(*args, y.data_ptr(), _stream(dev)), "bfp_rms_norm")
+        _call("bfp_rms_norm", dev, *args, y.data_ptr())
     elif isinstance(to, str):
         code, _ = _format(to)
         y = _fp8_out(out, rows, d, to, dev, FP8Tensor.empty)
-        check(load().bfp_rms_norm_fp8(*args, code, *y._ptrs[:2], _status_ptr(status), _stream(dev)), "bfp_rms_norm_fp8")
+        _call("bfp_rms_norm_fp8", dev, *args, code, *y._ptrs[:2], _status(status, dev))
     else:
         if rounding not in ROUNDING:
             raise ValueError("rounding must be one of %s" % sorted(ROUNDING))
@@ -298,8 +333,8 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
         if (y.rows, y.len, y.g, y.m) != (rows, d, 16, to):
             raise ValueError("out has the wrong shape or format")
         _on(dev, out=y.mant)
-        check(load().bfp_rms_norm_bfp(*args, to, ROUNDING[rounding], seed & 0xFFFFFFFFFFFFFFFF, y.mant.data_ptr(),
-                                      y.exp.data_ptr(), _status_ptr(status), _stream(dev)), "bfp_rms_norm_bfp")
+        _call("bfp_rms_norm_bfp", dev, *args, to, ROUNDING[rounding], seed & 0xFFFFFFFFFFFFFFFF, y.mant.data_ptr(),
+              y.exp.data_ptr(), _status(status, dev))
     return y, h if h is not None else x, rstd
 
 
@@ -334,9 +369,8 @@ def rms_norm_grad(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, weight:
     dx = out if out is not None else torch.empty_like(dy, dtype=torch.float32)
     need = _norm_grad_ws(rows, d)
     dw, ws = torch.empty(d, dtype=torch.float32, device=dev), torch.empty(need, dtype=torch.uint8, device=dev)
-    check(load().bfp_rms_norm_grad(dy.data_ptr(), yt, h.data_ptr(), rstd.data_ptr(), weight.data_ptr(),
-                                   dresidual.data_ptr() if dresidual is not None else None, rows, d, dx.data_ptr(),
-                                   dw.data_ptr(), ws.data_ptr(), need, _stream(dev)), "bfp_rms_norm_grad")
+    _call("bfp_rms_norm_grad", dev, dy.data_ptr(), yt, h.data_ptr(), rstd.data_ptr(), weight.data_ptr(),
+          dresidual.data_ptr() if dresidual is not None else None, rows, d, dx.data_ptr(), dw.data_ptr(), ws.data_ptr(), need)
     return dx, dw
 
 
@@ -346,8 +380,9 @@ def rms_norm_grad(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, weight:
 class TensorList:
     """A list of FP32 (or of BF16) tensors with where their scaled values go (themselves unless ``out``
     is given), checked once: for a program whose gradients stay in place from step to
-    step.  It holds the tensors, and a workspace of its own, so calls with one list must
-    not overlap."""
+    step.  It holds their memory (a tensor that is given other memory afterwards, as by
+    ``t.data = u``, needs a new list), and a workspace of its own, so calls with one list
+    must not overlap."""
 
     def __init__(self, tensors, out=None):
         self.tensors = list(tensors)
@@ -374,6 +409,14 @@ class TensorList:
         check(load().bfp_sum_squares_ws_size(self.sizes, n, ctypes.byref(nb)), "bfp_sum_squares_ws_size")
         self.pieces = nb.value // 8
         self.work = torch.empty(self.pieces + 1, dtype=torch.float64, device=self.device)  # (and their sum)
+        self._memory = [t.detach() for t in (self.tensors if out is None else self.tensors + self.out)]
+        self._stream = _stream(self.device)
+
+    def _call(self, name, *args):
+        """A call that uses the workspace, which is its own stream's unless that is told."""
+        if _stream(self.device) != self._stream:
+            self.work.record_stream(torch.cuda.current_stream(self.device))
+        _call(name, self.device, *args)
 
     def __len__(self):
         return len(self.tensors)
@@ -394,8 +437,7 @@ def sum_squares(tensors) -> torch.Tensor:
     added up (all_reduce) before clip_gradients."""
     l = _as_list(tensors)
     out = torch.empty(1, dtype=torch.float64, device=l.device)
-    check(load().bfp_sum_squares(l.ptrs, l.type, l.sizes, len(l), out.data_ptr(), l.work.data_ptr(), 8 * l.pieces,
-                                 _stream(l.device)), "bfp_sum_squares")
+    l._call("bfp_sum_squares", l.ptrs, l.type, l.sizes, len(l), out.data_ptr(), l.work.data_ptr(), 8 * l.pieces)
     return out
 
 
@@ -412,8 +454,7 @@ def clip_gradients(tensors, max_norm: float, sumsq: torch.Tensor | None = None) 
         pieces = l.pieces
         few = 0 < pieces <= 1024
         at = l.work.data_ptr() if few else l.work.data_ptr() + 8 * pieces
-        check(load().bfp_sum_squares(l.ptrs, l.type, l.sizes, len(l), None if few else at, l.work.data_ptr(),
-                                     8 * pieces, _stream(l.device)), "bfp_sum_squares")
+        l._call("bfp_sum_squares", l.ptrs, l.type, l.sizes, len(l), None if few else at, l.work.data_ptr(), 8 * pieces)
         sums = pieces if few else 1
     else:
         _need_cuda(sumsq, "sumsq", torch.float64)
@@ -422,6 +463,5 @@ def clip_gradients(tensors, max_norm: float, sumsq: torch.Tensor | None = None) 
         _on(l.device, sumsq=sumsq)
         at, sums = sumsq.data_ptr(), 1
     norm = torch.empty(1, dtype=torch.float64, device=l.device)
-    check(load().bfp_clip_gradients(l.ptrs, l.out_ptrs, l.type, l.sizes, len(l), max_norm, at, sums,
-                                    norm.data_ptr(), _stream(l.device)), "bfp_clip_gradients")
+    _call("bfp_clip_gradients", l.device, l.ptrs, l.out_ptrs, l.type, l.sizes, len(l), max_norm, at, sums, norm.data_ptr())
     return norm

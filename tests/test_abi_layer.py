@@ -45,12 +45,15 @@ def test_quantize_refusals(lib):
     assert q(c=at(0) + 16) == q(e=at(0)) == q(c=at(1), e=at(1) + 128) == E_ARG
     assert q(xt=2) == q(xt=-1) == q(xt=1, x=at(0) + 1) == q(xt=1, c=at(0) + 5984) == E_ARG
     assert q(R=0) == q(C=0) == OK
+    # launches of 2^32 threads: 32 for four blocks of a row, 256 for a tile of 128 x 128
+    assert q(R=1 << 27, C=5) == q(R=1 << 25, C=2048, x=at(0)) == q(ax=0, R=1, C=1 << 31) == E_UNSUP
     d = lambda *p: lib.bfp_quantize_fp8_dual(at(0), 0, 10, 300, 0, *p, None, None)  # noqa: E731
     assert d(None, at(2), at(3), at(4)) == d(at(1), at(2), at(3), None) == E_ARG
     assert d(at(1), at(2), at(1), at(4)) == d(at(1), at(2), at(3), at(2)) == E_ARG
     v = lambda c=at(1), e=at(2), rows=10, n=300, f=0, y=at(0): lib.bfp_dequantize_fp8(c, e, rows, n, f, y, None)  # noqa: E731
     assert v(c=None) == v(y=None) == v(f=3) == v(y=at(1)) == v(rows=-1) == E_ARG
     assert v(rows=0) == v(n=0) == OK
+    assert v(rows=1 << 32, n=1) == v(rows=1 << 30, n=13) == E_UNSUP
 
 
 def test_gemm_refusals(lib):
@@ -79,6 +82,14 @@ def test_gemm_refusals(lib):
         assert lib.bfp_gemm_fp8_route(100, 90, 1 << 20, need.value - 1, *out) == OK
         assert parts.value == 1
     assert lib.bfp_gemm_fp8_route(0, 90, 100, 0, *out) == E_ARG
+    # a launch has fewer than 2^32 threads, whatever the sizes
+    v = [ctypes.c_int(0) for _ in range(4)]
+    for M, N, K in ((1, 1 << 28, 128), (1, (1 << 31) - 64, 128), (1 << 28, 3, 1), (1 << 18, 1 << 18, 128), (16, 1 << 30, 4096)):
+        if lib.bfp_gemm_fp8_route(M, N, K, 1 << 40, *map(ctypes.byref, v)) == E_UNSUP:
+            continue
+        rows, cols, waves, parts = (x.value for x in v)
+        assert -(-M // rows) * -(-N // cols) * parts * (64 * waves if waves else 256) < 1 << 32, (M, N, K)
+    assert g(M=1 << 20, N=1 << 12, ldc=1 << 12, K=0) == E_UNSUP
     assert lib.bfp_gemm_fp8_ws_size(100, 90, 0, ctypes.byref(need)) == OK and need.value == 0
     assert g(K=0, a=None, ea=None, b=None, eb=None, C=at(4) + 2) == E_ARG  # (checked, and nothing divides by K)
 
@@ -89,6 +100,7 @@ def test_norm_refusals(lib):
     assert n(x=None) == n(w=None) == n(y=None) == n(rows=-1) == n(d=-1) == E_ARG
     assert n(eps=-1.0) == n(eps=math.nan) == n(eps=math.inf) == E_ARG
     assert n(d=16385) == n(rows=1 << 31) == E_UNSUP
+    assert n(rows=1 << 26, d=1) == n(rows=1 << 24, d=1025) == n(rows=1 << 22, d=4097) == E_UNSUP
     assert n(x=at(0) + 2) == n(h=at(3) + 1) == n(y=at(5) + 2) == E_ARG
     assert n(h=at(0) + 4) == n(h=at(1) - 4) == n(h=at(2)) == n(h=at(4)) == n(y=at(3)) == n(y=at(2)) == E_ARG
     assert n(y=at(0) + 4) == n(r=at(0)) == n(r=at(5)) == E_ARG
@@ -159,4 +171,42 @@ def test_binding_refusals():
     a, b = fb.FP8Tensor.empty(4, 256, "e4m3", "cpu"), fb.FP8Tensor.empty(4, 128, "e4m3", "cpu")
     with pytest.raises(ValueError):
         fb.gemm_fp8(a, b)
+    with pytest.raises(TypeError):  # (on the host)
+        fb.gemm_fp8(a, a)
+    data, scales = a.data, a.scales
+    for args, err in (((data.view(torch.uint8), scales, 4, 256, "e4m3"), TypeError), ((data, scales, 4, 256, "e5m2"), TypeError),
+                      ((data, scales, 4, 384, "e4m3"), ValueError), ((data, scales, 5, 256, "e4m3"), ValueError),
+                      ((data, scales[:, :2], 4, 256, "e4m3"), ValueError), ((data, scales.T, 4, 256, "e4m3"), ValueError),
+                      ((data, scales.to(torch.int8), 4, 256, "e4m3"), TypeError)):
+        with pytest.raises(err):
+            fb.FP8Tensor(*args)
     assert a.codes.shape == (4, 256) and b.exp.shape == (4, 1) and b.scales.shape == (4, 4)
+
+
+def test_calls_run_with_their_tensors_device_current(monkeypatch):
+    """The default stream's handle is the same for every device: a call for tensors of
+    another device than the current one makes it current."""
+    from paper_2110_15456_amd import layer
+    now, seen = [0], []
+
+    class Device:
+        def __init__(self, dev):
+            self.dev = dev
+
+        def __enter__(self):
+            self.old, now[0] = now[0], self.dev.index
+
+        def __exit__(self, *e):
+            now[0] = self.old
+
+    class Lib:
+        def entry(self, *args):
+            seen.append((now[0], args))
+            return 0
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(layer, "_current_device", lambda: now[0])
+    monkeypatch.setattr(layer, "_stream", lambda dev: 0)
+    monkeypatch.setattr(layer, "load", Lib)
+    for index in (0, 3):
+        layer._call("entry", torch.device("cuda", index), 7)
+        assert seen[-1] == (index, (7, 0)) and now[0] == 0

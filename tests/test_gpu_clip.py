@@ -93,6 +93,29 @@ def test_a_norm_that_is_not_finite_scales_nothing(bad):
         assert np.array_equal(g.cpu().numpy(), x, equal_nan=True)
 
 
+def test_a_list_outlives_its_tensors_memory_and_its_stream():
+    """A tensor that is given other memory leaves the list with the old one; the list's
+    workspace, used on another stream, is not handed out while that stream still runs."""
+    g = torch.ones(1000, device=DEV)
+    held = fb.tensor_list([g])
+    old = g.detach()
+    g.data = torch.full((1000,), 3.0, device=DEV)
+    assert abs(float(fb.clip_gradients(held, 1.0)) - math.sqrt(1000.0)) <= 1e-12 * math.sqrt(1000.0)
+    assert bool((g == 3.0).all()) and bool((old < 1.0).all())
+    big = torch.ones(1 << 22, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    held = fb.tensor_list([big])
+    with torch.cuda.stream(side):
+        norms = [fb.clip_gradients(held, 1e9) for _ in range(20)]
+    n = held.work.numel()
+    del held
+    for _ in range(20):  # (what takes the workspace's place if it were free)
+        torch.full((n,), 7.0, dtype=torch.float64, device=DEV)
+    torch.cuda.synchronize()
+    assert all(float(v) == 2048.0 for v in norms)
+
+
 def test_shapes_and_strides_of_a_model():
     gs = [torch.randn(s, device=DEV) for s in ((3, 5), (7,), (2, 3, 4), ())]
     n = math.sqrt(sum(float((g.double() ** 2).sum()) for g in gs))

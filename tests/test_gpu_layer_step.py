@@ -182,3 +182,43 @@ def test_one_list_of_far_more_tensors_than_a_launch_takes():
     assert abs(float(norm) - float(want)) <= 1e-12 * float(want)
     got = torch.cat(gs).double()
     assert bool(((got - flat.double() / want).abs() <= 2.0 ** -23 * (flat.double() / want).abs()).all())
+
+
+def test_step_with_another_device_current(monkeypatch):
+    """The path that makes the tensors' device current for a call gives the same step."""
+    from paper_2110_15456_amd import layer as L
+    layer, v = Layer(272, 400, 1), inputs(70, 272, 400, 2)
+    want = layer.step(*v, lr=0.1, max_norm=0.5)
+    made = []
+
+    class MadeCurrent(torch.cuda.device):
+        def __init__(self, dev):
+            made.append(dev)
+            super().__init__(dev)
+    monkeypatch.setattr(torch.cuda, "device", MadeCurrent)
+    monkeypatch.setattr(L, "_current_device", lambda: -1)
+    got = layer.step(*v, lr=0.1, max_norm=0.5)
+    assert len(made) >= 10 and set(made) == {torch.device(DEV)}
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def test_status_words_and_other_refusals():
+    x, w = torch.randn(4, 256, device=DEV), torch.ones(256, device=DEV)
+    for bad in (torch.zeros(1, dtype=torch.uint8, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV),
+                torch.zeros(0, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32)):
+        for call in (lambda: fb.quantize_fp8(x, status=bad), lambda: fb.quantize_fp8_dual(x, status=bad),
+                     lambda: fb.rms_norm(x, w, to="e4m3", status=bad), lambda: fb.rms_norm(x, w, to=4, status=bad)):
+            with pytest.raises((TypeError, ValueError)):
+                call()
+    a = fb.quantize_fp8(x)
+    host = fb.FP8Tensor(a.data.cpu(), a.scales.cpu(), 4, 256, "e4m3")
+    for call in (lambda: fb.gemm_fp8(a, host), lambda: fb.gemm_fp8(host, host), lambda: fb.dequantize_fp8(host),
+                 lambda: fb.quantize_fp8(x, out=host), lambda: fb.rms_norm(x, w, to="e4m3", out=host),
+                 lambda: fb.gemm_fp8(a, a, out=torch.empty(4, 4, device=DEV).t()[:, :3]),
+                 lambda: fb.gemm_fp8(a, a, out=torch.empty(4, 4, device=DEV)[:, ::2]),
+                 lambda: fb.gemm_fp8(a, a, dtype=torch.float16)):
+        with pytest.raises((TypeError, ValueError)):
+            call()
+    with pytest.raises(fb.BFPError):  # (a product over its own operand)
+        fb.gemm_fp8(a, a, out=a.data.view(torch.float32)[:, :4])

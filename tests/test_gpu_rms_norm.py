@@ -181,6 +181,29 @@ def test_gradient(rows, d, residual):
         assert torch.equal(fb.rms_norm_grad(gpu(dy), h, rstd, gpu(w), dresidual=g, out=g)[0], dx)
 
 
+@pytest.mark.parametrize("scale", [1e-28, 1e-18, 1e18, 1e30])
+def test_gradient_of_far_values(scale):
+    """h whose square, or whose r^3, leaves FP32's range (bounds as above; with eps 0)."""
+    x, z, w = inputs(9, 300, 11)
+    x = x * np.float32(scale)
+    dy = np.float32(np.random.default_rng(3).laplace(0, 1e-4, x.shape))
+    _, h, rstd = fb.rms_norm(gpu(x), gpu(w), eps=0.0, save=True)
+    dx, dw = fb.rms_norm_grad(gpu(dy), h, rstd, gpu(w))
+    want_dx, want_dw, S, Sw = gradient(dy, x, w, None, eps=0.0)
+    # (below FP32's normal range: a unit of its least step for each of the two terms' roundings)
+    assert np.all(np.abs(dx.cpu().numpy() - want_dx) <= 16 * 2.0 ** -24 * S + 2.0 ** -148)
+    assert np.all(np.abs(dw.cpu().numpy() - want_dw) <= 6 * 2.0 ** -24 * Sw + 1e-45)
+
+
+def test_no_values_in_a_row():
+    """The mean of nothing is NaN, its gradient nothing."""
+    e, w = torch.empty((4, 0), device=DEV), torch.ones(0, device=DEV)
+    y, h, rstd = fb.rms_norm(e, w, save=True)
+    assert y.shape == (4, 0) and h.shape == (4, 0) and bool(torch.isnan(rstd).all()) and rstd.shape == (4,)
+    dx, dw = fb.rms_norm_grad(e, h, rstd, w)
+    assert dx.shape == (4, 0) and dw.shape == (0,)
+
+
 def test_gradient_against_differences():
     """Central differences of sum(dy y) of the formula in 64 bits along random directions."""
     rng = np.random.default_rng(7)
