@@ -1,6 +1,10 @@
-// quantize_fp8.hip -- FP32 -> 8-bit floating-point blocks (fp8.h) along either axis, or
-// both from one read, and the inverse.  HBM-bound: 4 bytes read and 1 + 1/128 written a
-// value (2 + 1/64 with both).
+// quantize_fp8.hip -- FP32 or BF16 -> 8-bit floating-point blocks (fp8.h) along either axis,
+// or both from one read, and the inverse.  HBM-bound: 4 or 2 bytes read and 1 + 1/128
+// written a value (2 + 1/64 with both).
+//
+// Measured, 8192 x 4096 of BF16: rows 17.5 us (5.8 TB/s read and written), columns 18.9,
+// both 31.6 (4.4); with a wave to a block and FP32 arithmetic for scale and rounding they
+// took 30, 60 and 79.
 #include "fp8.h"
 #include "launch.h"
 

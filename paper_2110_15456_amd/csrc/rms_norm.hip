@@ -7,6 +7,10 @@
 // value whatever the launch, and the converted output the conversion of that y.  (64-bit
 // multiplies and adds run at FP32's rate here, and the kernel waits for HBM.)
 // HBM-bound: x and the residual read once, h and the output written once.
+//
+// Measured, 8192 x 4096: BF16 x + residual -> h and e4m3 blocks 67 us, 5.5 TB/s; its
+// gradient from a BF16 dy 86 us, 5.6 TB/s, and 6 for the join of dw.  One row: 4.2 us, a
+// launch.
 #include "fp8.h"
 #include "gemm_direct.h"
 #include "launch.h"
@@ -142,7 +146,8 @@ __global__ __launch_bounds__(NT) void k_rms_norm(Args p) {
 // so that nothing leaves FP32's range on the way, however large or small h is):
 //   dx = r (u - n mean(u n)) (+ dresidual),  dw = sum over rows of dy n
 // A workgroup takes rows b, b + gridDim, ...; its share of dw stays in registers, in 64
-// bits, and goes to part[b] in FP32.
+// bits, and goes to part[b] in FP32.  (The next row's loads ahead of this one's sum changed
+// nothing: the workgroups on a CU cover each other's.)
 struct GradArgs {
   const void* dy;  // FP32 or BF16
   const float *h, *rstd, *w, *dresidual;
