@@ -310,7 +310,7 @@ int bfp_rms_norm_grad_ws_size(int64_t rows, int64_t d, size_t* workspace_bytes) 
   const int st = check_norm(rows, d);
   if (st != BFP_OK) return st;
   if (!workspace_bytes) return BFP_E_ARG;
-  *workspace_bytes = (size_t)fastbfp::rms_norm_grad_parts(rows) * d * 4;
+  *workspace_bytes = (size_t)fastbfp::rms_norm_grad_parts(rows, d) * d * 4;
   return BFP_OK;
 }
 
@@ -320,7 +320,7 @@ int bfp_rms_norm_grad(const void* dy, int dy_type, const float* h, const float* 
   const int st = check_norm(rows, d);
   if (st != BFP_OK || d == 0) return st;
   if (!type_ok(dy_type) || !dweight || !aligned(dweight, 4)) return BFP_E_ARG;
-  const uint64_t n = (uint64_t)rows * d * 4, need = (uint64_t)fastbfp::rms_norm_grad_parts(rows) * d * 4;
+  const uint64_t n = (uint64_t)rows * d * 4, need = (uint64_t)fastbfp::rms_norm_grad_parts(rows, d) * d * 4;
   if (rows > 0) {
     if (!dy || !h || !rstd || !weight || !dx || !workspace || workspace_bytes < need) return BFP_E_ARG;
     if (!aligned(dy, bytes_of(dy_type)) || !aligned(h, 4) || !aligned(rstd, 4) || !aligned(weight, 4) || !aligned(dresidual, 4) ||

@@ -249,7 +249,7 @@ hipError_t launch_rms_norm_bfp(const void* x, bool bf16, const float* residual, 
                                double eps, float* h, float* rstd, int m, int mode, uint64_t seed, uint8_t* mant,
                                uint8_t* exps, uint32_t* status, hipStream_t s);
 int64_t rms_norm_threads(int64_t d);  // of a row
-int64_t rms_norm_grad_parts(int64_t rows);  // rows of d values in the workspace
+int64_t rms_norm_grad_parts(int64_t rows, int64_t d);  // rows of d values in the workspace
 hipError_t launch_rms_norm_grad(const void* dy, bool bf16, const float* h, const float* rstd, const float* w,
                                 const float* dresidual, int64_t rows, int64_t d, float* dx, float* dw, float* ws,
                                 hipStream_t s);

@@ -145,30 +145,41 @@ __global__ __launch_bounds__(NT) void k_rms_norm(Args p) {
 // The gradients, for u = w dy, h and r of the forward pass and n = h r (at most sqrt(d),
 // so that nothing leaves FP32's range on the way, however large or small h is):
 //   dx = r (u - n mean(u n)) (+ dresidual),  dw = sum over rows of dy n
-// A workgroup takes rows b, b + gridDim, ...; its share of dw stays in registers, in 64
-// bits, and goes to part[b] in FP32.  (The next row's loads ahead of this one's sum changed
-// nothing: the workgroups on a CU cover each other's.)
+// NT threads take a row, W rows side by side in a workgroup, and then every gridDim W-th one;
+// their share of dw stays in registers, in 64 bits, and goes to part[b] in FP32.  (The next
+// row's loads ahead of this one's sum changed nothing: the workgroups on a CU cover each
+// other's.)  W is 8 for rows of one wave: with one of them to a workgroup 16384 x 512 took
+// 40.6 us.  Rows of more than 8192 values leave no registers for their share: it is in LDS
+// (2000 x 9698: 162 us with spills).
 struct GradArgs {
   const void* dy;  // FP32 or BF16
   const float *h, *rstd, *w, *dresidual;
   int64_t rows, d;
   float *dx, *part;
 };
+constexpr int rows_of(int nt) { return nt == 64 ? 8 : 1; }  // W
 template <int NT, int NV, bool RES, class T>
-__global__ __launch_bounds__(NT) void k_rms_norm_grad(GradArgs p) {
+__global__ __launch_bounds__(NT * rows_of(NT)) void k_rms_norm_grad(GradArgs p) {
+  constexpr int W = rows_of(NT);
+  static_assert(W == 1 || NT == 64, "waves that take rows of their own meet nowhere in the loop");
+  constexpr bool LDS = NT * NV >= 4096;
   __shared__ double red[2][NT > 64 ? NT / 64 : 1];
   const int64_t d = p.d;
-  const int t = threadIdx.x;
+  const int t = threadIdx.x % NT, slot = threadIdx.x / NT;
   u4 w[NV];
-  double dw[NV][4];
+  double mine[LDS ? 1 : NV][4];
+  __shared__ double share[LDS ? NV * 4 * NT : 1];  // (a thread's own places: nothing to wait for)
+  auto dw = [&](int k, int i) __attribute__((always_inline)) -> double& {
+    return LDS ? share[(4 * k + i) * NT + t] : mine[LDS ? 0 : k][i];
+  };
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     w[k] = load4(p.w + 4 * (t + NT * k), d - 4 * (t + NT * k));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) dw[k][i] = 0.0;
+    for (int i = 0; i < 4; ++i) dw(k, i) = 0.0;
   }
   int turn = 0;
-  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+  for (int64_t row = (int64_t)blockIdx.x * W + slot; row < p.rows; row += (int64_t)gridDim.x * W, turn ^= 1) {
     const float r = p.rstd[row];
     u4 g[NV], h[NV], z[NV];
 #pragma unroll
@@ -186,7 +197,7 @@ __global__ __launch_bounds__(NT) void k_rms_norm_grad(GradArgs p) {
       for (int i = 0; i < 4; ++i) {
         const float dy = __uint_as_float(g[k][i]), n = __uint_as_float(h[k][i]) * r;
         s4 = __builtin_fmaf(dy * __uint_as_float(w[k][i]), n, s4);
-        dw[k][i] += (double)(dy * n);
+        dw(k, i) += (double)(dy * n);
       }
       sum += (double)s4;
     }
@@ -207,13 +218,32 @@ __global__ __launch_bounds__(NT) void k_rms_norm_grad(GradArgs p) {
       store4(p.dx + row * d + c, o, d - c);
     }
   }
+  float* part = p.part + (int64_t)blockIdx.x * d;
+  if constexpr (W == 1) {
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int64_t c = 4 * (t + NT * k);
-    u4 o;
+    for (int k = 0; k < NV; ++k) {
+      const int64_t c = 4 * (t + NT * k);
+      u4 o;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = __float_as_uint((float)dw[k][i]);
-    store4(p.part + (int64_t)blockIdx.x * d + c, o, d - c);
+      for (int i = 0; i < 4; ++i) o[i] = __float_as_uint((float)dw(k, i));
+      store4(part + c, o, d - c);
+    }
+  } else {
+    __shared__ double rows[W][4 * NT];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      if (k > 0) __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rows[slot][4 * t + i] = dw(k, i);
+      __syncthreads();
+      const int64_t c = 4 * NT * k + threadIdx.x;
+      if (threadIdx.x < 4 * NT && c < d) {
+        double sum = 0.0;
+#pragma unroll
+        for (int s = 0; s < W; ++s) sum += rows[s][threadIdx.x];
+        part[c] = (float)sum;
+      }
+    }
   }
 }
 
@@ -292,7 +322,7 @@ hipError_t launch(const Args& a, bool bf16, int to, hipStream_t s) {
 
 template <int NT, class T>
 void launch_grad(const GradArgs& a, int nv, int parts, hipStream_t s) {
-  const dim3 grid((unsigned)parts), block(NT);
+  const dim3 grid((unsigned)parts), block(NT * rows_of(NT));
 #define FASTBFP_GRAD(NV)                                                                    \
   if (a.dresidual) hipLaunchKernelGGL((k_rms_norm_grad<NT, NV, true, T>), grid, block, 0, s, a); \
   else hipLaunchKernelGGL((k_rms_norm_grad<NT, NV, false, T>), grid, block, 0, s, a)
@@ -345,9 +375,11 @@ hipError_t launch_rms_norm_bfp(const void* x, bool bf16, const float* residual, 
 
 int64_t rms_norm_threads(int64_t d) { return norm::shape_of(d).nt; }
 
-// Workgroups of the gradient: one for each row up to 256, and for every fourth row up to 512.
-int64_t rms_norm_grad_parts(int64_t rows) {
-  if (rows <= 256) return rows;
+// Workgroups of the gradient, up to 512: enough for all rows at once where a wave takes one,
+// else one for each row up to 256 and for every fourth row from there on.
+int64_t rms_norm_grad_parts(int64_t rows, int64_t d) {
+  const int64_t w = norm::rows_of(norm::shape_of(d).nt), all = (rows + w - 1) / w;
+  if (w > 1 || all <= 256) return all < 512 ? all : 512;
   const int64_t n = (rows + 3) / 4;
   return n < 256 ? 256 : n < 512 ? n : 512;
 }
@@ -355,7 +387,7 @@ int64_t rms_norm_grad_parts(int64_t rows) {
 hipError_t launch_rms_norm_grad(const void* dy, bool bf16, const float* h, const float* rstd, const float* w,
                                 const float* dresidual, int64_t rows, int64_t d, float* dx, float* dw, float* ws,
                                 hipStream_t s) {
-  const int parts = (int)rms_norm_grad_parts(rows);
+  const int parts = (int)rms_norm_grad_parts(rows, d);
   if (rows > 0) {
     const norm::GradArgs a{dy, h, rstd, w, dresidual, rows, d, dx, ws};
     if (bf16) norm::launch_grad_t<fp8::bf16_t>(a, parts, s);

@@ -118,8 +118,13 @@ class FP8Tensor:
     @staticmethod
     def empty(rows: int, length: int, fmt: str, device) -> "FP8Tensor":
         pitch, ep = _pitches(length)
-        return FP8Tensor(torch.empty(rows, pitch, dtype=_format(fmt)[1], device=device),
-                         torch.empty(rows, ep, dtype=torch.uint8, device=device), rows, length, fmt)
+        code, dtype = _format(fmt)
+        t = FP8Tensor.__new__(FP8Tensor)
+        t.rows, t.len, t.fmt = rows, length, fmt
+        t._data, t._bytes = torch.empty(rows, pitch, dtype=dtype, device=device), None
+        t._scales = torch.empty(rows, ep, dtype=torch.uint8, device=device)
+        t.device, t._ptrs = t._data.device, (t._data.data_ptr(), t._scales.data_ptr(), code)
+        return t
 
     @staticmethod
     def _one_buffer(rows, length, fmt, device) -> "FP8Tensor":

@@ -157,7 +157,7 @@ def gradient(dy, h, w, dres, eps=EPS):
 
 
 @pytest.mark.parametrize("residual", [False, True])
-@pytest.mark.parametrize("rows,d", SHAPES + [(700, 1155), (2000, 48), (5000, 7)])
+@pytest.mark.parametrize("rows,d", SHAPES + [(700, 1155), (2000, 48), (5000, 7), (4101, 260), (1030, 8300)])
 def test_gradient(rows, d, residual):
     print(rows, d, residual, flush=True)
     x, z, w = inputs(rows, d, d + 1)
