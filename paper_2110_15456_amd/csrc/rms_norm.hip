@@ -8,7 +8,8 @@
 // multiplies and adds run at FP32's rate here, and the kernel waits for HBM.)
 // HBM-bound: x and the residual read once, h and the output written once.
 //
-// Measured, 8192 x 4096: BF16 x + residual -> h and e4m3 blocks 67 us, 5.5 TB/s; its
+// Measured, 8192 x 4096: BF16 x + residual -> h and e4m3 blocks 66 us, 5.6 TB/s; FP32 x +
+// residual -> h and BFP of width 4 78 us (120 when 16 lanes of a wave converted); the
 // gradient from a BF16 dy 86 us, 5.6 TB/s, and 6 for the join of dw.  One row: 4.2 us, a
 // launch.
 #include "fp8.h"
@@ -56,13 +57,15 @@ struct Args {
 template <int NT, int NV, bool RES, int TO, class T>
 __global__ __launch_bounds__(NT) void k_rms_norm(Args p) {
   __shared__ double red[NT > 64 ? NT / 64 : 1];
-  __shared__ __attribute__((aligned(16))) float stage[TO == kToBfp ? 4 * NT : 4];
+  __shared__ __attribute__((aligned(16))) float stage[TO == kToBfp ? 4 * NT * NV : 4];
   const int64_t row = blockIdx.x, d = p.d;
   const int t = threadIdx.x;
   const T* x = static_cast<const T*>(p.x) + row * d;
-  u4 v[NV];
+  u4 v[NV], w[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) v[k] = load4(x + 4 * (t + NT * k), d - 4 * (t + NT * k));
+#pragma unroll
+  for (int k = 0; k < NV; ++k) w[k] = load4(p.w + 4 * (t + NT * k), d - 4 * (t + NT * k));
   if constexpr (RES) {
     u4 z[NV];
 #pragma unroll
@@ -87,14 +90,14 @@ __global__ __launch_bounds__(NT) void k_rms_norm(Args p) {
   const double r = 1.0 / sqrt(sum / (double)d + p.eps);
   if (p.rstd && t == 0) p.rstd[row] = (float)r;
   uint32_t bad = 0;
+  float* mine = stage + (TO == kToBfp ? 256 * NV * (t >> 6) : 0);
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int64_t c = 4 * (t + NT * k);
-    const u4 w = load4(p.w + c, d - c);
     u4 y;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      y[i] = __float_as_uint((float)((double)__uint_as_float(v[k][i]) * r * (double)__uint_as_float(w[i])));
+      y[i] = __float_as_uint((float)((double)__uint_as_float(v[k][i]) * r * (double)__uint_as_float(w[k][i])));
     if constexpr (TO == kToF32) {
       store4(p.y + row * d + c, y, d - c);
     } else if constexpr (TO == kToFp8) {
@@ -111,26 +114,30 @@ __global__ __launch_bounds__(NT) void k_rms_norm(Args p) {
       if (block * fp8::kBlock < d) *reinterpret_cast<uint32_t*>(p.codes + row * fp8::code_pitch(d) + c) = q;
       if ((t & 31) == 0 && block < fp8::exp_pitch(d)) p.exps[row * fp8::exp_pitch(d) + block] = (uint8_t)s;
     } else {
-      // each wave gathers its 256 consecutive values, 16 groups, and converts a group a lane
-      float* mine = stage + 256 * (t >> 6);
-      *reinterpret_cast<u4*>(mine + 4 * (t & 63)) = y;
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-      __builtin_amdgcn_wave_barrier();
-      const int64_t g0 = 16 * (int64_t)((t >> 6) + NT / 64 * k);  // the wave's first group
-      if ((t & 63) < 16 && 16 * (g0 + (t & 63)) < d) {
-        uint32_t b[16];
+      const int q = 64 * k + (t & 63);
+      *reinterpret_cast<u4*>(mine + 4 * (q ^ ((q >> 4) & 3))) = y;
+    }
+  }
+  if constexpr (TO == kToBfp) {
+    // A wave's 256 consecutive values for each k, 16 groups, are in its part of LDS; a lane
+    // converts a group.  (Quad q sits at q ^ ((q >> 4) & 3): 16 lanes that read a quad of
+    // 16 groups hit all banks.)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+    const int lane = t & 63;
+    const int64_t g = 16 * (int64_t)((t >> 6) + NT / 64 * (lane >> 4)) + (lane & 15);
+    if (lane < 16 * NV && 16 * g < d) {
+      uint32_t b[16];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const u4 q = *reinterpret_cast<const u4*>(mine + 16 * (t & 63) + 4 * i);
+      for (int i = 0; i < 4; ++i) {
+        const int q = 4 * lane + i;
+        const u4 x = *reinterpret_cast<const u4*>(mine + 4 * (q ^ ((q >> 4) & 3)));
 #pragma unroll
-          for (int e = 0; e < 4; ++e) b[4 * i + e] = q[e];
-        }
-        bad |= direct::convert(b, row * (d / 16) + g0 + (t & 63), p.bfp) ? 1u : 0u;
+        for (int e = 0; e < 4; ++e) b[4 * i + e] = x[e];
       }
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_s_waitcnt(0xC07F);
-      __builtin_amdgcn_wave_barrier();
+      bad |= direct::convert(b, row * (d / 16) + g, p.bfp) ? 1u : 0u;
     }
   }
   if constexpr (TO != kToF32) {

@@ -13,6 +13,7 @@ import tempfile
 import pytest
 
 from paper_2110_15456_amd import build as B
+from tests.test_wave_lds_order import unordered
 
 MARK = re.compile(r"^;;#ASMSTART")
 TO_LDS = re.compile(r"^buffer_load_dword(x4)?\b.*\blds\b")
@@ -42,15 +43,24 @@ def segments(asm):
     return found
 
 
-@pytest.fixture(scope="module")
-def kernels():
+def assembly(source):
     with tempfile.TemporaryDirectory() as d:
         out = os.path.join(d, "k.s")
         cmd = [os.path.join(B.ROCM, "bin", "hipcc"), *B.HIPFLAGS, "--cuda-device-only", "-S",
-               os.path.join(B.CSRC, "gemm_fp8.hip"), "-o", out]
+               os.path.join(B.CSRC, source), "-o", out]
         subprocess.run(cmd, check=True, capture_output=True)
         with open(out) as f:
-            return segments(f.read())
+            return f.read()
+
+
+@pytest.fixture(scope="module")
+def products():
+    return assembly("gemm_fp8.hip")
+
+
+@pytest.fixture(scope="module")
+def kernels(products):
+    return segments(products)
 
 
 def test_few_rows(kernels):
@@ -89,3 +99,13 @@ def test_audit_sees_a_moved_load():
     asm = "_Zk:\n\tbuffer_load_dwordx4 v0, s[4:7], 0 offen lds\n\t;;#ASMSTART\n%s\t;;#ASMSTART\n\ts_endpgm\n"
     assert segments(asm % "")["_Zk"] == [[1, 0, 0], [0, 0, 0], [0, 0, 0]]
     assert segments(asm % "\tbuffer_load_dword v1, v2, s[4:7], 0 offen\n")["_Zk"][1] == [0, 0, 1]
+
+
+def test_lanes_meet_between_lds_writes_and_reads(products):
+    """Rows of a tile on their way out, and values that a norm converts to BFP, pass from
+    lane to lane of a wave through LDS: every turn has its mark."""
+    kernels, turns = unordered(products)
+    assert kernels >= 48 and not turns, turns[:3]
+    # (norms of one wave a row: in the others the waves' sums pass through LDS of their own)
+    turns = [t for t in unordered(assembly("rms_norm.hip"))[1] if re.search(r"10k_rms_normILi64E", t[0])]
+    assert not turns, turns[:3]
