@@ -131,7 +131,10 @@ __device__ __forceinline__ uint32_t max_half_wave(uint32_t v) {
   v = max_dpp<0x4E>(v);   // quad_perm 2 3 0 1
   v = max_dpp<0x141>(v);  // mirrored within eight lanes
   v = max_dpp<0x140>(v);  // mirrored within sixteen
-  return max(v, (uint32_t)__shfl_xor((int)v, 16));
+  // (rows of 16 lanes: of each pair the first one's in both, and the second one's)
+  typedef uint32_t pair __attribute__((ext_vector_type(2)));
+  const pair p = __builtin_bit_cast(pair, __builtin_amdgcn_permlane16_swap(v, v, false, false));
+  return max(p[0], p[1]);
 }
 __device__ __forceinline__ uint32_t max4(const u4& b) {
   return max(max(counted(b[0]), counted(b[1])), max(counted(b[2]), counted(b[3])));
@@ -153,6 +156,30 @@ __device__ __forceinline__ uint32_t convert_block(const V& v, uint32_t& scale, b
   return convert4(b, inverse(scale), FMT);
 }
 
+// N blocks at once, with one branch for all of them.
+template <int FMT, int N, class V>
+__device__ __forceinline__ void convert_blocks(const V (&v)[N], uint32_t (&code)[N], uint32_t (&scale)[N], bool& bad) {
+  bool all = true;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t key = max_half_wave(key4(v[i]));
+    scale[i] = scale_of(key >> 1, FMT);
+    all &= quick(key, scale[i]);
+  }
+  bad = false;
+  if (all) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) code[i] = quick4<FMT>(v[i], scale[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      bool b;
+      code[i] = convert_block<FMT>(v[i], scale[i], b);
+      bad |= b;
+    }
+  }
+}
+
 // Four values from `left` (of a row) on, as they are: those past the row's end are zeros.
 // Rows of any length begin at any multiple of a value's bytes.
 __device__ __forceinline__ u4 raw4(const float* p, int64_t left) {
@@ -172,6 +199,15 @@ __device__ __forceinline__ u2 raw4(const bf16_t* p, int64_t left) {
   for (int t = 0; t < 3; ++t)
     if (t < left) v[t / 2] |= (uint32_t)p[t] << (16 * (t & 1));
   return v;
+}
+// Four values moved down by `n` places (0 to 3), zeros behind them.
+__device__ __forceinline__ u4 down(u4 v, int n) {
+  if (n & 1) v = u4{v[1], v[2], v[3], 0u};
+  if (n & 2) v = u4{v[2], v[3], 0u, 0u};
+  return v;
+}
+__device__ __forceinline__ u2 down(const u2& v, int n) {
+  return __builtin_bit_cast(u2, __builtin_bit_cast(uint64_t, v) >> (16 * n));
 }
 // Their FP32 bits.
 template <class T>

@@ -2,9 +2,11 @@
 // or both from one read, and the inverse.  HBM-bound: 4 or 2 bytes read and 1 + 1/128
 // written a value (2 + 1/64 with both).
 //
-// Measured, 8192 x 4096 of BF16: rows 17.5 us (5.8 TB/s read and written), columns 18.9,
-// both 31.6 (4.4); with a wave to a block and FP32 arithmetic for scale and rounding they
-// took 30, 60 and 79.
+// Measured, 8192 x 4096 of BF16: rows 17.5 us (5.8 TB/s read and written), columns 19, both
+// 27 (5.0); with a wave to a block and FP32 arithmetic for scale and rounding they took 30,
+// 60 and 79.  Small ones take as long as their code's way through the instruction caches:
+// with a branch for each block, and the slow ways beside the quick one, both conversions
+// of 16 x 4096 took 10.9 us, now 6.4.
 #include "fp8.h"
 #include "launch.h"
 
@@ -28,17 +30,14 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int64
   typename Raw<T>::type v[4];
 #pragma unroll
   for (int b = 0; b < 4; ++b) v[b] = raw4(src + c0 + b * kBlock, len - (c0 + b * kBlock));
-  uint32_t scales = 0;
-  bool any = false;
+  uint32_t scales = 0, w[4], s[4];
+  bool any;
   uint8_t* out = codes + row * code_pitch(len);
+  convert_blocks<FMT>(v, w, s, any);
 #pragma unroll
   for (int b = 0; b < 4; ++b) {
-    uint32_t s;
-    bool bad;
-    const uint32_t w = convert_block<FMT>(v[b], s, bad);
-    any |= bad;
-    scales |= s << (8 * b);
-    if (c0 - 4 * lane + b * kBlock < len) *reinterpret_cast<uint32_t*>(out + c0 + b * kBlock) = w;
+    scales |= s[b] << (8 * b);
+    if (c0 - 4 * lane + b * kBlock < len) *reinterpret_cast<uint32_t*>(out + c0 + b * kBlock) = w[b];
   }
   if (lane == 0) *reinterpret_cast<uint32_t*>(exps + row * exp_pitch(len) + (c0 / kBlock)) = scales;
   if (status && any) atomicOr(status, 1u);
@@ -67,34 +66,64 @@ __global__ __launch_bounds__(256) void k_fp8_tiles(const T* __restrict__ x, int6
   {
     const int half = threadIdx.x >> 5, lane = threadIdx.x & 31;
     typedef typename Raw<T>::type V;
-    V v[16];
-    const bool whole = r0 + kBlock <= R && c0 + kBlock <= C;
+    const int rows = (int)min((int64_t)kBlock, R - r0);
+    const T* src = x + (r0 + half) * C + c0 + 4 * lane;
+    T* mine = tile + half * kBlock + 4 * lane;
+    uint8_t* codes = codes_r + (r0 + half) * code_pitch(C) + c0 + 4 * lane;
+    uint8_t* exps = exps_r + (r0 + half) * exp_pitch(C) + tc + lane;
+    // (a row's scale, and in its last tile the zeros behind it)
+    const bool scales = lane < (tc + 1 == (int)tiles_c ? (int)(exp_pitch(C) - tc) : 1);
+    bool any = false, done = false;
+    if (C >= 4) {
+      // (of a lane that the rows' end leaves some of its four, the row's last four, moved
+      // down: no branch among the loads)
+      const int left = (int)max(min(C - (c0 + 4 * lane), (int64_t)4), (int64_t)0), past = left > 0 ? 4 - left : 0;
+      V v[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int64_t r = r0 + i * 8 + half;
-      const T* p = x + r * C + c0 + 4 * lane;
-      v[i] = whole ? raw4(p, 4) : r < R ? raw4(p, C - (c0 + 4 * lane)) : V{};
-    }
-    bool any = false;
+      for (int i = 0; i < 16; ++i) v[i] = 8 * i + half < rows && left > 0 ? raw4(src - past + 8 * i * C, 4) : V{};
+      if (c0 + kBlock > C && C % 4 != 0) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int r = i * 8 + half;
-      *reinterpret_cast<V*>(&tile[r * kBlock + 4 * lane]) = v[i];
+        for (int i = 0; i < 16; ++i) v[i] = down(v[i], past);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) *reinterpret_cast<V*>(mine + 8 * i * kBlock) = v[i];
       if constexpr (ROWS) {
-        uint32_t s;
-        bool bad;
-        const uint32_t w = convert_block<FMT>(v[i], s, bad);
-        any |= bad;
-        if (r0 + r < R) {
-          *reinterpret_cast<uint32_t*>(codes_r + (r0 + r) * code_pitch(C) + c0 + 4 * lane) = w;
-          uint8_t* e = exps_r + (r0 + r) * exp_pitch(C) + tc;
-          if (lane == 0) *e = (uint8_t)s;
-          // (the scales behind a row's last block are zeros)
-          if (tc + 1 == (int)tiles_c && lane > 0 && lane < (int)(exp_pitch(C) - tc)) e[lane] = 0;
+        uint32_t key[16];
+        done = true;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          key[i] = max_half_wave(key4(v[i]));
+          done &= quick(key[i], scale_of(key[i] >> 1, FMT));
+        }
+        if (done) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t s = scale_of(key[i] >> 1, FMT);
+            if (8 * i + half < rows) {
+              *reinterpret_cast<uint32_t*>(codes + 8 * i * code_pitch(C)) = quick4<FMT>(v[i], s);
+              if (scales) exps[8 * i * exp_pitch(C)] = lane == 0 ? (uint8_t)s : 0;
+            }
+          }
         }
       }
+    } else {
+#pragma unroll 4
+      for (int i = 0; i < 16; ++i)
+        *reinterpret_cast<V*>(mine + 8 * i * kBlock) = 8 * i + half < rows ? raw4(src + 8 * i * C, C - (c0 + 4 * lane)) : V{};
     }
-    if (ROWS && status && any) atomicOr(status, 1u);
+    if (ROWS && !done) {
+      // (not unrolled, from LDS: in the quick way's path its code would be fetched too)
+#pragma unroll 1
+      for (int i = 0; 8 * i + half < rows; ++i) {
+        uint32_t s;
+        bool bad;
+        const uint32_t w = convert_block<FMT>(*reinterpret_cast<const V*>(mine + 8 * i * kBlock), s, bad);
+        any |= bad;
+        *reinterpret_cast<uint32_t*>(codes + 8 * i * code_pitch(C)) = w;
+        if (scales) exps[8 * i * exp_pitch(C)] = lane == 0 ? (uint8_t)s : 0;
+      }
+      if (status && any) atomicOr(status, 1u);
+    }
   }
   __syncthreads();
   // Column c (with BF16 c and c + 1) from row run * 128 / RUNS on.

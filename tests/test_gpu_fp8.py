@@ -36,7 +36,8 @@ def spread(shape, seed):
     return x
 
 
-SHAPES = [(1, 1), (1, 127), (3, 128), (2, 129), (5, 512), (7, 513), (64, 777), (129, 1050), (300, 4096), (2, 5000)]
+SHAPES = [(1, 1), (1, 127), (3, 128), (2, 129), (5, 512), (7, 513), (64, 777), (129, 1050), (300, 4096), (2, 5000),
+          (9, 2), (200, 3), (131, 4), (130, 5), (33, 6), (17, 7), (140, 130), (300, 131), (257, 257)]
 
 
 @pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
@@ -75,9 +76,10 @@ def test_every_code_comes_back(fmt):
         F.check_tensor(fb.quantize_fp8(gpu(x), fmt=fmt), x, fmt)
 
 
+@pytest.mark.parametrize("n", [300, 301, 302, 303])
 @pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
-def test_infinities_and_nan(fmt):
-    x = synth.draw("weights", (140, 300), 3)
+def test_infinities_and_nan(fmt, n):
+    x = synth.draw("weights", (140, n), 3)
     x[3, 5], x[3, 200], x[77, 299], x[130, 0] = np.inf, -np.inf, np.nan, np.nan
     x[50, 128:256] = np.nan  # a block of nothing else
     for call in (lambda s: [(fb.quantize_fp8(gpu(x), fmt=fmt, status=s), x)],
