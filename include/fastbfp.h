@@ -760,7 +760,8 @@ int bfp_orthogonalize_route(int64_t batch, int64_t rows, int64_t cols, int* tile
  *   codes : uint8 [rows][128 * blocks], blocks = len / 128 rounded up; zeros behind a
  *           row's last value.  16-byte aligned.
  *   exp   : uint8 [rows][blocks rounded up to a multiple of 4], zeros behind a row's last
- *           block: a block's values are its codes' times 2^(exp - 127).  4-byte aligned.
+ *           block: a block's values are its codes' times 2^(exp - 127), exp at most 254.
+ *           4-byte aligned.
  *
  * A block's scale is the least power of two (not below 2^-127) by which its largest
  * value is at most the format's; codes are the nearest ones to value / scale, ties to

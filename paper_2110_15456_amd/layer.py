@@ -64,6 +64,16 @@ def _on(device, **tensors):
             raise ValueError("%s must be on %s" % (name, device))
 
 
+def _f32(t, name, shape, dev):
+    """t is a contiguous FP32 tensor of that shape on dev."""
+    if isinstance(t, torch.Tensor) and t.dtype is torch.float32 and t.shape == shape and t.device == dev and t.is_contiguous():
+        return
+    _need_cuda(t, name, torch.float32)
+    if t.shape != shape:
+        raise ValueError("%s must be %s" % (name, list(shape)))
+    _on(dev, **{name: t})
+
+
 # ---- 8-bit blocks -------------------------------------------------------
 
 
@@ -198,10 +208,8 @@ def quantize_fp8_dual(x: torch.Tensor, fmt: str = "e4m3", status: torch.Tensor |
 def dequantize_fp8(t: FP8Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
     """8-bit blocks -> FP32 [rows, len]."""
     y = out if out is not None else torch.empty((t.rows, t.len), dtype=torch.float32, device=t.device)
-    _need_cuda(y, "out", torch.float32)
-    if tuple(y.shape) != (t.rows, t.len):
-        raise ValueError("out must be [%d, %d]" % (t.rows, t.len))
-    _on(t.device, out=y)
+    _need_cuda(y, "out", torch.float32)  # (and so t, whose device it shares)
+    _f32(y, "out", (t.rows, t.len), t.device)
     _call("bfp_dequantize_fp8", t.device, *t._ptrs[:2], t.rows, t.len, t._ptrs[2], y.data_ptr())
     return y
 
@@ -298,34 +306,25 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
     d = shape[-1]
     rows = shape[0] if len(shape) == 2 else math.prod(shape[:-1])
     dev = x.device
-    _need_cuda(weight, "weight", torch.float32)
-    if weight.dim() != 1 or weight.shape[0] != d:
-        raise ValueError("weight must be [%d]" % d)
-    h = h_out
+    _f32(weight, "weight", (d,), dev)
     if residual is not None:
-        _need_cuda(residual, "residual", torch.float32)
-        if residual.shape != shape:
-            raise ValueError("residual must have x's shape")
-    if h is None:
-        if residual is not None or (xt and save):
-            h = torch.empty_like(x, dtype=torch.float32)
-    else:
-        _need_cuda(h, "h_out", torch.float32)
-        if h.shape != shape:
-            raise ValueError("h_out must have x's shape")
-    if weight.device != dev or (residual is not None and residual.device != dev) or h_out is not None:
-        _on(dev, weight=weight, residual=residual, h_out=h_out)
+        _f32(residual, "residual", shape, dev)
+    h = h_out
+    if h is not None:
+        _f32(h, "h_out", shape, dev)
+    elif residual is not None or (xt and save):
+        h = torch.empty_like(x, dtype=torch.float32)
     rstd = None
     if save:  # (the mean of no values: NaN)
         rstd = torch.empty(rows, device=dev, dtype=torch.float32) if d else torch.full((rows,), math.nan, device=dev)
     args = (x.data_ptr(), xt, residual.data_ptr() if residual is not None else None, weight.data_ptr(), rows, d, eps,
             h.data_ptr() if h is not None else None, rstd.data_ptr() if save else None)
     if to is None:
-        y = out if out is not None else torch.empty_like(x, dtype=torch.float32)
-        _need_cuda(y, "out", torch.float32)
-        if y.shape != shape:
-            raise ValueError("out must have x's shape")
-        _on(dev, out=y)
+        y = out
+        if y is None:
+            y = torch.empty_like(x, dtype=torch.float32)
+        else:
+            _f32(y, "out", shape, dev)
         _call("bfp_rms_norm", dev, *args, y.data_ptr())
     elif isinstance(to, str):
         code, _ = _format(to)
@@ -360,18 +359,19 @@ def rms_norm_grad(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, weight:
     yt = _type(dy, "dy")
     if dy.dim() < 1:
         raise ValueError("dy must have at least one dimension")
-    d = dy.shape[-1]
-    rows = dy.numel() // d if d else math.prod(dy.shape[:-1])
-    dev = dy.device
-    for name, t, shape in (("h", h, dy.shape), ("rstd", rstd, (rows,)), ("weight", weight, (d,)),
-                           ("dresidual", dresidual, dy.shape), ("out", out, dy.shape)):
-        if t is None and name in ("dresidual", "out"):
-            continue
-        _need_cuda(t, name, torch.float32)
-        if tuple(t.shape) != tuple(shape):
-            raise ValueError("%s must be %s" % (name, list(shape)))
-        _on(dev, **{name: t})
-    dx = out if out is not None else torch.empty_like(dy, dtype=torch.float32)
+    shape, dev = dy.shape, dy.device
+    d = shape[-1]
+    rows = shape[0] if len(shape) == 2 else math.prod(shape[:-1])
+    _f32(h, "h", shape, dev)
+    _f32(rstd, "rstd", (rows,), dev)
+    _f32(weight, "weight", (d,), dev)
+    if dresidual is not None:
+        _f32(dresidual, "dresidual", shape, dev)
+    dx = out
+    if dx is None:
+        dx = torch.empty_like(dy, dtype=torch.float32)
+    else:
+        _f32(dx, "out", shape, dev)
     need = _norm_grad_ws(rows, d)
     dw, ws = torch.empty(d, dtype=torch.float32, device=dev), torch.empty(need, dtype=torch.uint8, device=dev)
     _call("bfp_rms_norm_grad", dev, dy.data_ptr(), yt, h.data_ptr(), rstd.data_ptr(), weight.data_ptr(),
@@ -387,7 +387,7 @@ class TensorList:
     is given), checked once: for a program whose gradients stay in place from step to
     step.  It holds their memory (a tensor that is given other memory afterwards, as by
     ``t.data = u``, needs a new list), and a workspace of its own, so calls with one list
-    must not overlap."""
+    must not overlap, and it lives as long as a graph that was captured with it."""
 
     def __init__(self, tensors, out=None):
         self.tensors = list(tensors)
