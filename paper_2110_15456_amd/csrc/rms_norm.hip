@@ -54,8 +54,12 @@ struct Args {
 };
 
 // A workgroup of NT threads takes a row, thread t its values 4 (t + NT k) .. + 3.
+// Rows of 8193 to 12288 values are kept to 64 registers, and so two of them on a CU, at the
+// price of weights that are not on the way with the values (with 16384's registers 2781 x
+// 9408 took 55 us).
 template <int NT, int NV, bool RES, int TO, class T>
-__global__ __launch_bounds__(NT) void k_rms_norm(Args p) {
+__global__ __launch_bounds__(NT, NV == 3 ? 8 : 1) void k_rms_norm(Args p) {
+  constexpr bool EARLY = NV != 3;
   __shared__ double red[NT > 64 ? NT / 64 : 1];
   __shared__ __attribute__((aligned(16))) float stage[TO == kToBfp ? 4 * NT * NV : 4];
   const int64_t row = blockIdx.x, d = p.d;
@@ -64,8 +68,10 @@ __global__ __launch_bounds__(NT) void k_rms_norm(Args p) {
   u4 v[NV], w[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) v[k] = load4(x + 4 * (t + NT * k), d - 4 * (t + NT * k));
+  if constexpr (EARLY) {
 #pragma unroll
-  for (int k = 0; k < NV; ++k) w[k] = load4(p.w + 4 * (t + NT * k), d - 4 * (t + NT * k));
+    for (int k = 0; k < NV; ++k) w[k] = load4(p.w + 4 * (t + NT * k), d - 4 * (t + NT * k));
+  }
   if constexpr (RES) {
     u4 z[NV];
 #pragma unroll
@@ -94,6 +100,7 @@ __global__ __launch_bounds__(NT) void k_rms_norm(Args p) {
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int64_t c = 4 * (t + NT * k);
+    if constexpr (!EARLY) w[k] = load4(p.w + c, d - c);
     u4 y;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -291,7 +298,7 @@ struct Shape {
 Shape shape_of(int64_t d) {
   const int nt = d <= 1024 ? 64 : d <= 4096 ? 256 : 1024;
   const int64_t v = (d + 4 * nt - 1) / (4 * nt);
-  return {nt, v <= 1 ? 1 : v <= 2 ? 2 : 4};
+  return {nt, v <= 1 ? 1 : v <= 2 ? 2 : v <= 3 && nt == 1024 ? 3 : 4};
 }
 
 template <int NT, int NV, class T>
@@ -314,6 +321,7 @@ template <int NT, class T>
 hipError_t launch_norm_nv(const Args& a, int nv, int to, hipStream_t s) {
   return nv == 1   ? launch_norm<NT, 1, T>(a, to, s)
          : nv == 2 ? launch_norm<NT, 2, T>(a, to, s)
+         : nv == 3 ? launch_norm<1024, 3, T>(a, to, s)
                    : launch_norm<NT, 4, T>(a, to, s);
 }
 template <class T>
@@ -383,9 +391,11 @@ hipError_t launch_rms_norm_bfp(const void* x, bool bf16, const float* residual, 
 int64_t rms_norm_threads(int64_t d) { return norm::shape_of(d).nt; }
 
 // Workgroups of the gradient, up to 512: enough for all rows at once where a wave takes one,
-// else one for each row up to 256 and for every fourth row from there on.
+// else one for each row up to 256 and for every fourth row from there on.  One takes up to
+// three rows alone, whose share is dw: a second launch would take longer than the rows.
 int64_t rms_norm_grad_parts(int64_t rows, int64_t d) {
   const int64_t w = norm::rows_of(norm::shape_of(d).nt), all = (rows + w - 1) / w;
+  if (w == 1 && rows <= 3) return rows < 1 ? 0 : 1;
   if (w > 1 || all <= 256) return all < 512 ? all : 512;
   const int64_t n = (rows + 3) / 4;
   return n < 256 ? 256 : n < 512 ? n : 512;
@@ -396,11 +406,11 @@ hipError_t launch_rms_norm_grad(const void* dy, bool bf16, const float* h, const
                                 hipStream_t s) {
   const int parts = (int)rms_norm_grad_parts(rows, d);
   if (rows > 0) {
-    const norm::GradArgs a{dy, h, rstd, w, dresidual, rows, d, dx, ws};
+    const norm::GradArgs a{dy, h, rstd, w, dresidual, rows, d, dx, parts == 1 ? dw : ws};
     if (bf16) norm::launch_grad_t<fp8::bf16_t>(a, parts, s);
     else norm::launch_grad_t<float>(a, parts, s);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || parts == 1) return e;
   }
   hipLaunchKernelGGL(norm::k_rms_norm_join, dim3((unsigned)((d + 63) / 64)), dim3(256), 0, s, ws, parts, d, dw);
   return hipGetLastError();

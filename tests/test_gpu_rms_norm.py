@@ -36,7 +36,7 @@ def formula(h, w, eps=EPS):
 # FP32's rounding of the formula's value, and another place where 64 bits round to its border
 ONE = 2.0 ** -24 * (1 + 1e-6)
 SHAPES = [(1, 1), (3, 3), (1, 16), (5, 255), (2, 256), (4, 257), (7, 777), (3, 1024), (2, 1025), (33, 2048), (2, 4095),
-          (64, 4096), (3, 4097), (2, 8200), (2, 16384), (1, 16383)]
+          (64, 4096), (3, 4097), (2, 8200), (2, 8208), (3, 12288), (2, 12290), (2, 16384), (1, 16383)]
 
 
 @pytest.mark.parametrize("residual", [False, True])
@@ -157,7 +157,7 @@ def gradient(dy, h, w, dres, eps=EPS):
 
 
 @pytest.mark.parametrize("residual", [False, True])
-@pytest.mark.parametrize("rows,d", SHAPES + [(700, 1155), (2000, 48), (5000, 7), (4101, 260), (1030, 8300)])
+@pytest.mark.parametrize("rows,d", SHAPES + [(700, 1155), (2000, 48), (5000, 7), (4101, 260), (1030, 8300), (8, 1000), (9, 1024), (4, 5000)])
 def test_gradient(rows, d, residual):
     print(rows, d, residual, flush=True)
     x, z, w = inputs(rows, d, d + 1)
