@@ -179,6 +179,19 @@ def test_output_slices_rows_behind_and_no_k():
     assert fb.gemm_fp8(fb.quantize_fp8(torch.empty((0, 300), device=DEV)), B).shape == (0, 50)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,N,K", [(300, 511, 700), (1100, 1301, 1024), (2300, 2201, 640)])
+def test_output_slices_of_large_products(M, N, K, dtype):
+    A, B = (fb.quantize_fp8(gpu(synth.draw("weights", (r, K), r))) for r in (M, N))
+    want = fb.gemm_fp8(A, B, dtype=dtype)
+    wide = torch.full((M + 3, N + 20), 7.0, device=DEV, dtype=dtype)
+    for at in (1, 3, 8):
+        fb.gemm_fp8(A, B, out=wide[1:M + 1, at:at + N])
+        assert torch.equal(wide[1:M + 1, at:at + N], want)
+        wide[1:M + 1, at:at + N] = 7.0
+        assert bool((wide == 7.0).all())
+
+
 def test_nan_stays_in_its_row():
     a, b = synth.draw("weights", (70, 300), 1), synth.draw("weights", (80, 300), 2)
     B = fb.quantize_fp8(gpu(b))
