@@ -74,6 +74,12 @@ def _f32(t, name, shape, dev):
     _on(dev, **{name: t})
 
 
+def _same_start(a, b):
+    """Whether a is a tensor that begins where b does (others that share memory are refused
+    by the library)."""
+    return isinstance(a, torch.Tensor) and a.data_ptr() == b.data_ptr()
+
+
 # ---- 8-bit blocks -------------------------------------------------------
 
 
@@ -298,7 +304,9 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
     save      whether rstd (FP32 [rows]) is written, for rms_norm_grad; else it is None.
     x         FP32 or BF16 (h is FP32 either way; y as well).
     h_out     where h goes; residual or an FP32 x: in place.
-    out       a preallocated y.   status: as quantize's, of the converted y."""
+    out       a preallocated y.  An FP32 one may be an FP32 x or residual, where h is not: in
+              place (without a residual, h is then a copy of x).
+    status    as quantize's, of the converted y."""
     xt = _type(x, "x")
     shape = x.shape
     if len(shape) < 1:
@@ -312,7 +320,7 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
     h = h_out
     if h is not None:
         _f32(h, "h_out", shape, dev)
-    elif residual is not None or (xt and save):
+    elif residual is not None or (xt and save) or (to is None and _same_start(out, x)):
         h = torch.empty_like(x, dtype=torch.float32)
     rstd = None
     if save:  # (the mean of no values: NaN)

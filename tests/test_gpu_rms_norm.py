@@ -109,6 +109,28 @@ def test_in_place_and_leading_axes():
     assert (t.rows, t.len) == (6, 300)
 
 
+@pytest.mark.parametrize("rows,d", [(1, 3), (6, 300), (5, 4096), (2, 9001)])
+@pytest.mark.parametrize("save", [False, True])
+def test_in_place_without_a_residual_keeps_h(rows, d, save):
+    """y over x: h is still what x was, and the gradients are those of a norm elsewhere."""
+    x, _, w = inputs(rows, d, 12)
+    dy = gpu(np.random.default_rng(6).standard_normal((rows, d)))
+    want, want_h, want_r = fb.rms_norm(gpu(x), gpu(w), save=True)
+    a = gpu(x)
+    y, h, r = fb.rms_norm(a, gpu(w), out=a, save=save)
+    assert y is a and torch.equal(a, want) and torch.equal(h, gpu(x)) and (r is not None) == save
+    if save:
+        assert torch.equal(r, want_r)
+        for p, q in zip(fb.rms_norm_grad(dy, h, r, gpu(w)), fb.rms_norm_grad(dy, want_h, want_r, gpu(w))):
+            assert torch.equal(p, q)
+    a = gpu(x)
+    y, h, _ = fb.rms_norm(a, gpu(w), out=a.view(rows, d), save=save)  # (another tensor on the same memory)
+    assert torch.equal(a, want) and torch.equal(h, gpu(x))
+    mine = torch.empty((rows, d), device=DEV)
+    y, h, _ = fb.rms_norm(gpu(x), gpu(w), out=mine, save=save)
+    assert y is mine and torch.equal(mine, want) and torch.equal(h, gpu(x))
+
+
 def test_far_values_zeros_and_empty():
     x, _, w = inputs(8, 200, 3)
     x[0], x[1], x[2], x[3] = 0.0, x[1] * np.float32(1e30), x[2] * np.float32(1e-30), 1e-42
