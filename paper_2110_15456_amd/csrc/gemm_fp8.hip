@@ -227,19 +227,56 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
   meet(std::integral_constant<int, (ST - 1) * (LA + LB)>{});
   read_scales(0, sa, sb);
   read(stage0, 0, a[0], b[0]);
-  if constexpr (ST == 2) {
-    for (int s = 0; s < nslabs; s += 2) {
-      slab(stage0, stage1, std::integral_constant<int, 0>{}, s);
-      // (the 256 tile runs an odd slab's partner on zeros: around a branch here its
-      // fragments would not stay in registers)
-      if (BM == 256 || s + 1 < nslabs) slab(stage1, stage0, std::integral_constant<int, 1>{}, s + 1);
+  // Whole runs of ST slabs have no branch among them, and the slabs that are left, all of which
+  // are on the way by then, run behind the loop: the compiler waits by itself for loads to a
+  // stage that some path leaves on the way, and on a path from a run's first slab back to
+  // the loop's head that is all of them (with branches in one loop 64 tiles waited for
+  // all they had on the way once in four slabs, 128 tiles half a slab early in every second).
+  constexpr std::integral_constant<int, 0> k0{};
+  constexpr std::integral_constant<int, 1> k1{};
+  // The j-th slab behind the loop, its `next` one's loads older than those of ST - 2 - j more.
+  auto last = [&](const uint8_t* cur, const uint8_t* nxt, auto jc, bool next) __attribute__((always_inline)) {
+    read(cur, 1, a[1], b[1]);
+    multiply(a[0], b[0]);
+    if (next) {
+      meet(std::integral_constant<int, (ST - 2 - decltype(jc)::value) * (LA + LB)>{});
+      read(nxt, 0, a[0], b[0]);
     }
+    multiply(a[1], b[1]);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = (int)((uint32_t)sa[i] >> 8);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) sb[j] = (int)((uint32_t)sb[j] >> 8);
+  };
+  int s = 0;
+  if constexpr (BM == 256) {
+    // (an odd slab's partner runs on zeros: with another slab behind the loop the fragments
+    // would not stay in registers)
+    for (; s < nslabs; s += 2) {
+      slab(stage0, stage1, k0, s);
+      slab(stage1, stage0, k1, s + 1);
+    }
+  } else if constexpr (ST == 2) {
+    for (; s + 1 < nslabs; s += 2) {
+      slab(stage0, stage1, k0, s);
+      slab(stage1, stage0, k1, s + 1);
+    }
+    if (s < nslabs) last(stage0, stage1, k0, false);
   } else {
-    for (int s = 0; s < nslabs; s += 4) {
-      slab(stage0, stage1, std::integral_constant<int, 0>{}, s);
-      if (s + 1 < nslabs) slab(stage1, stage2, std::integral_constant<int, 1>{}, s + 1);
-      if (s + 2 < nslabs) slab(stage2, stage3, std::integral_constant<int, 2>{}, s + 2);
-      if (s + 3 < nslabs) slab(stage3, stage0, std::integral_constant<int, 3>{}, s + 3);
+    constexpr std::integral_constant<int, 2> k2{};
+    constexpr std::integral_constant<int, 3> k3{};
+    for (; s + 3 < nslabs; s += 4) {
+      slab(stage0, stage1, k0, s);
+      slab(stage1, stage2, k1, s + 1);
+      slab(stage2, stage3, k2, s + 2);
+      slab(stage3, stage0, k3, s + 3);
+    }
+    if (s < nslabs) {
+      last(stage0, stage1, k0, s + 1 < nslabs);
+      if (s + 1 < nslabs) {
+        last(stage1, stage2, k1, s + 2 < nslabs);
+        if (s + 2 < nslabs) last(stage2, stage3, k2, false);
+      }
     }
   }
 
