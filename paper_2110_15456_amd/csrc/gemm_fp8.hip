@@ -424,8 +424,12 @@ __global__ __launch_bounds__(64 * WAVES) void k_gemm_fp8_few(Gemm p) {
       for (int j = 0; j < RN; ++j)  // (B first: a lane's four are columns of a row)
         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i], acc[i][j], FB, FA, k, sb[j], k, sa[i]);
   };
-  scales(wave);
+  // (the first run's scales go in front of all slabs but the first: behind them, the wait for
+  // them in the loop would be one for all but the youngest slab, in every run)
   issue(stage0, 4 * wave);
+  __builtin_amdgcn_sched_barrier(0);
+  scales(wave);
+  __builtin_amdgcn_sched_barrier(0);
   issue(stage1, 4 * wave + 1);
   issue(stage2, 4 * wave + 2);
   issue(stage3, 4 * wave + 3);

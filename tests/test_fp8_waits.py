@@ -63,3 +63,15 @@ def test_audit_sees_a_wait():
     assert loops(asm % "") == {"_Zk": []}
     assert loops(asm % "\ts_waitcnt vmcnt(0)\n\tds_read_b128 v1, v2\n") == {"_Zk": [0]}
     assert loops(asm % "\ts_waitcnt lgkmcnt(0)\n") == {"_Zk": []}
+
+
+def test_few_rows_keep_three_slabs_on_the_way(products):
+    seen = 0
+    for name, own in products.items():
+        m = re.search(r"k_gemm_fp8_fewILi(\d+)ELi(\d+)ELi\d+E", name)
+        if not m:
+            continue
+        seen += 1
+        loads = 2 * (int(m.group(1)) + int(m.group(2)))  # of a slab
+        assert all(n >= 3 * loads for n in own), (name, own)
+    assert seen == 24  # three tiles, four pairs of formats, two types
