@@ -79,7 +79,10 @@ __device__ __forceinline__ uint32_t convert4(const u4& b, float inv, int fmt) {
 // The quick way through a conversion: `key`, twice the bits of a block's largest magnitude
 // as they are, and the hardware's scaled conversion.  It does not hold for blocks with
 // infinities or NaN, or whose scale would show FP32 subnormals as more than zero
-// (a subnormal over 2^(18 - 127) is below half of e5m2's least value, 2^-17).
+// (a subnormal over 2^(18 - 127) is below half of e5m2's least value, 2^-17).  It does for
+// blocks of zeros, and of rows or blocks that are not there, whose scale byte is 0: their
+// codes are the zeros' signs by any scale (kQuickLeast's in quick4).
+constexpr uint32_t kQuickLeast = 19;
 __device__ __forceinline__ uint32_t key4(const u4& b) {
   return max(max(b[0] << 1, b[1] << 1), max(b[2] << 1, b[3] << 1));
 }
@@ -89,11 +92,13 @@ __device__ __forceinline__ uint32_t key4(const u2& b) {
   return (uint32_t)max(m[0], m[1]) << 17;
 }
 __device__ __forceinline__ bool key_finite(uint32_t key) { return key < 0xFF000000u; }
-__device__ __forceinline__ bool quick(uint32_t key, uint32_t scale) { return key_finite(key) && scale > 18u; }
+__device__ __forceinline__ bool quick(uint32_t key, uint32_t scale) {
+  return key == 0u || (key_finite(key) && scale >= kQuickLeast);
+}
 
 template <int FMT>
 __device__ __forceinline__ uint32_t quick4(const u4& b, uint32_t scale) {
-  const float f = __uint_as_float(scale << 23);
+  const float f = __uint_as_float(max(scale, kQuickLeast) << 23);
   const float x0 = __uint_as_float(b[0]), x1 = __uint_as_float(b[1]), x2 = __uint_as_float(b[2]), x3 = __uint_as_float(b[3]);
   s2 r{};
   if constexpr (FMT == kE4M3) {
@@ -107,7 +112,7 @@ __device__ __forceinline__ uint32_t quick4(const u4& b, uint32_t scale) {
 }
 template <int FMT>
 __device__ __forceinline__ uint32_t quick4(const u2& b, uint32_t scale) {
-  const float f = __uint_as_float(scale << 23);
+  const float f = __uint_as_float(max(scale, kQuickLeast) << 23);
   const uint32_t lo = b[0], hi = b[1];  // (of b[1] itself the compiler's bit cast takes b[0])
   const b2 x = __builtin_bit_cast(b2, lo), y = __builtin_bit_cast(b2, hi);
   s2 r{};

@@ -2,11 +2,13 @@
 // or both from one read, and the inverse.  HBM-bound: 4 or 2 bytes read and 1 + 1/128
 // written a value (2 + 1/64 with both).
 //
-// Measured, 8192 x 4096 of BF16: rows 17.5 us (5.8 TB/s read and written), columns 19, both
-// 27 (5.0); with a wave to a block and FP32 arithmetic for scale and rounding they took 30,
-// 60 and 79.  Small ones take as long as their code's way through the instruction caches:
-// with a branch for each block, and the slow ways beside the quick one, both conversions
-// of 16 x 4096 took 10.9 us, now 6.4.
+// Measured, 8192 x 4096 of BF16: rows 16.7 us (6.1 TB/s read and written), columns 19, both
+// 26.6 (5.1); with a wave to a block and FP32 arithmetic for scale and rounding they took 30,
+// 60 and 79.  Small ones take as long as their code's way through the instruction caches
+// (both conversions of 16 x 4096 5.8).  Zeros, and what lies past the tensor's ends,
+// decide no branch: while they did, both conversions of 1531 x 1050 FP32 took 11.3 us and
+// those along its rows 5.1, now 7.6 and 3.5; with zeros in every seventh row of 8192 x 4096
+// both took 33, now 26.
 #include "fp8.h"
 #include "launch.h"
 
@@ -175,7 +177,7 @@ __global__ __launch_bounds__(256) void k_fp8_tiles(const T* __restrict__ x, int6
     for (int k = 1; k < RUNS; ++k) m = max(m, top[k][c + j]);
     const uint32_t s = scale_of(m >> 1, FMT);
     uint32_t w[Q];
-    if (!odd && s > 18u) {
+    if (!odd && quick(m, s)) {
 #pragma unroll
       for (int i = 0; i < Q; ++i) w[i] = quick4<FMT>(v[j][i], s);
     } else {
