@@ -868,7 +868,9 @@ int bfp_rms_norm_bfp(const void* x, int x_type, const float* residual, const flo
  *   dx        : FP32 [rows][d]; may be an FP32 dy or dresidual (in place).
  *   dweight   : FP32 [d]; zeros where rows is 0.
  *   workspace : bfp_rms_norm_grad_ws_size bytes, 4-byte aligned; overwritten.
- * Sums along rows and over rows are 64 bits; their order depends on the sizes alone.
+ * u and n are rounded to FP32; their products and sums, and those of dy n, are 64 bits. Of
+ * dweight each workgroup's share (up to 512 of them) is rounded to FP32 before the shares are
+ * added in 64 bits.  All orders depend on the sizes alone.
  * Other overlaps are BFP_E_ARG.
  */
 int bfp_rms_norm_grad_ws_size(int64_t rows, int64_t d, size_t* workspace_bytes);

@@ -159,12 +159,15 @@ __global__ __launch_bounds__(NT, NV == 3 ? 8 : 1) void k_rms_norm(Args p) {
 // The gradients, for u = w dy, h and r of the forward pass and n = h r (at most sqrt(d),
 // so that nothing leaves FP32's range on the way, however large or small h is):
 //   dx = r (u - n mean(u n)) (+ dresidual),  dw = sum over rows of dy n
-// NT threads take a row, W rows side by side in a workgroup, and then every gridDim W-th one;
-// their share of dw stays in registers, in 64 bits, and goes to part[b] in FP32.  (The next
-// row's loads ahead of this one's sum changed nothing: the workgroups on a CU cover each
-// other's.)  W is 8 for rows of one wave: with one of them to a workgroup 16384 x 512 took
-// 40.6 us.  Rows of more than 8192 values leave no registers for their share: it is in LDS
-// (2000 x 9698: 162 us with spills).
+// u and n are rounded to FP32; their products, dy n and the sums of both are 64 bits (FP32
+// products, and sums of four of them, took as long: 8192 x 4096 with a residual 91.5 us
+// and 91.6).  NT threads take a row, W rows side by side in a workgroup, and then every
+// gridDim W-th one; their share of dw stays in registers, in 64 bits, and goes to part[b]
+// in FP32 (in 64 bits the shares would move 8 MB more each way at d = 4096).  (The next
+// row's loads ahead of this one's sum changed nothing up to 8192 values, where the workgroups
+// on a CU cover each other's.)  W is 8 for rows of one wave: with one of them to a workgroup
+// 16384 x 512 took 40.6 us.  Rows of more than 8192 values leave no registers for their share:
+// it is in LDS (2000 x 9698: 162 us with spills).
 struct GradArgs {
   const void* dy;  // FP32 or BF16
   const float *h, *rstd, *w, *dresidual;
@@ -206,14 +209,13 @@ __global__ __launch_bounds__(NT * rows_of(NT)) void k_rms_norm_grad(GradArgs p) 
     double sum = 0.0;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      float s4 = 0.0f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float dy = __uint_as_float(g[k][i]), n = __uint_as_float(h[k][i]) * r;
-        s4 = __builtin_fmaf(dy * __uint_as_float(w[k][i]), n, s4);
-        dw(k, i) += (double)(dy * n);
+        const float dy = __uint_as_float(g[k][i]);
+        const double n = (double)(__uint_as_float(h[k][i]) * r);
+        sum = __builtin_fma((double)(dy * __uint_as_float(w[k][i])), n, sum);
+        dw(k, i) = __builtin_fma((double)dy, n, dw(k, i));
       }
-      sum += (double)s4;
     }
     // (two places for the waves' sums: a wave may be a row ahead of one that still reads)
     sum = block_sum<NT>(sum, red[turn]);

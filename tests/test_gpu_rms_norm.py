@@ -217,6 +217,21 @@ def test_gradient_of_far_values(scale):
     assert np.all(np.abs(dw.cpu().numpy() - want_dw) <= 6 * 2.0 ** -24 * Sw + 1e-45)
 
 
+@pytest.mark.parametrize("d", [4, 64, 1024, 4096, 8200, 16384])
+def test_sums_along_a_row_are_64_bits(d):
+    """Terms 2^24, 1, -2^24, 0 over and over, with h, r and the weights 1: their mean is 1/4,
+    of which sums of any four in FP32 leave 0."""
+    dy = np.float32(np.tile([2.0 ** 24, 1.0, -(2.0 ** 24), 0.0], d // 4))[None].repeat(3, axis=0)
+    one = torch.ones(d, device=DEV)
+    _, h, rstd = fb.rms_norm(torch.ones((3, d), device=DEV), one, eps=0.0, save=True)
+    assert bool((rstd == 1.0).all())
+    dx, dw = fb.rms_norm_grad(gpu(dy), h, rstd, one)
+    want = dy.astype(np.float64) - 0.25
+    # (r, u, n, the mean and their product are exact; dx is rounded once)
+    assert np.all(np.abs(dx.cpu().numpy() - want) <= 2.0 ** -24 * np.abs(want))
+    assert np.array_equal(dw.cpu().numpy(), 3 * dy[0])
+
+
 def test_no_values_in_a_row():
     """The mean of nothing is NaN, its gradient nothing."""
     e, w = torch.empty((4, 0), device=DEV), torch.ones(0, device=DEV)
