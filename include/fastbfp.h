@@ -862,7 +862,9 @@ int bfp_rms_norm_bfp(const void* x, int x_type, const float* residual, const flo
 /*
  * bfp_rms_norm_grad -- its gradients, with u = weight dy:
  *   dx = r u - h r^3 mean(u h) + dresidual,  dweight = sum over the rows of dy h r
- *   (as r (u - n mean(u n)) with n = h r, which is in range for any h)
+ *   (as r (u - n mean(u n)) with n = h r, which stays in range while rstd does: with eps = 0
+ *   rstd is infinite for a row whose root mean square is below 2^-128, 2.9e-39, and its
+ *   gradients are not finite; above 2^126, 8.5e37, rstd is subnormal and off by up to 2^-22)
  *   dy        : dy_type [rows][d].   h, rstd : of the forward pass.   dresidual : optional, the gradient that reaches h
  *               beside the norm; dx is the gradient of x and of the residual alike.
  *   dx        : FP32 [rows][d]; may be an FP32 dy or dresidual (in place).

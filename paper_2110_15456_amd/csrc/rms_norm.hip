@@ -157,7 +157,7 @@ __global__ __launch_bounds__(NT, NV == 3 ? 8 : 1) void k_rms_norm(Args p) {
 }
 
 // The gradients, for u = w dy, h and r of the forward pass and n = h r (at most sqrt(d),
-// so that nothing leaves FP32's range on the way, however large or small h is):
+// so that nothing leaves FP32's range on the way while r is in it):
 //   dx = r (u - n mean(u n)) (+ dresidual),  dw = sum over rows of dy n
 // u and n are rounded to FP32; their products, dy n and the sums of both are 64 bits (FP32
 // products, and sums of four of them, took as long: 8192 x 4096 with a residual 91.5 us

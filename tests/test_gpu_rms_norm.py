@@ -232,6 +232,25 @@ def test_sums_along_a_row_are_64_bits(d):
     assert np.array_equal(dw.cpu().numpy(), 3 * dy[0])
 
 
+@pytest.mark.parametrize("rms,dy_scale", [(4e-39, 1e-4), (2.5e38, 1e30)])
+def test_gradient_at_the_ends_of_rstds_range(rms, dy_scale):
+    rng = np.random.default_rng(12)
+    x = np.float32(rng.choice([-1.0, 1.0], (7, 300)) * rng.uniform(0.8, 1.2, (7, 300)) * rms)
+    w = np.float32(1.0 + 0.1 * rng.standard_normal(300))
+    dy = np.float32(rng.standard_normal(x.shape) * dy_scale)
+    _, h, rstd = fb.rms_norm(gpu(x), gpu(w), eps=0.0, save=True)
+    _, r = formula(x, w, 0.0)
+    off = np.maximum(2.0 ** -24 * r, 2.0 ** -150) * (1 + 1e-6)  # (half of rstd's last place)
+    assert np.all(np.abs(rstd.cpu().numpy() - r) <= off)
+    dx, dw = fb.rms_norm_grad(gpu(dy), h, rstd, gpu(w))
+    want_dx, want_dw, S, Sw = gradient(dy, x, w, None, eps=0.0)
+    # test_gradient's bounds, and rstd's own error where it enters: once in r u, three times
+    # in the other term, once in dw
+    far = 3 * (off / r)[:, None]
+    assert np.all(np.abs(dx.cpu().numpy() - want_dx) <= (16 * 2.0 ** -24 + far) * S)
+    assert np.all(np.abs(dw.cpu().numpy() - want_dw) <= (6 * 2.0 ** -24 + far.max()) * Sw)
+
+
 def test_no_values_in_a_row():
     """The mean of nothing is NaN, its gradient nothing."""
     e, w = torch.empty((4, 0), device=DEV), torch.ones(0, device=DEV)
