@@ -801,8 +801,9 @@ int bfp_quantize_fp8(const void* x, int x_type, int64_t R, int64_t C, int group_
 int bfp_quantize_fp8_dual(const void* x, int x_type, int64_t R, int64_t C, int format, uint8_t* codes_r,
                           uint8_t* exp_r, uint8_t* codes_c, uint8_t* exp_c, uint32_t* status_word, void* stream);
 
-/* bfp_dequantize_fp8 -- the values, FP32 [rows][len] (exact, but for those below FP32's
- * range, which are rounded). */
+/* bfp_dequantize_fp8 -- the values, FP32 [rows][len]: exact, but for those below FP32's
+ * range, which are rounded, and those of 2^128 or more, which are infinite (of converted
+ * values e4m3's from 1.9375 * 2^127 on and e5m2's from 1.875 * 2^127: 2^128 is nearest). */
 int bfp_dequantize_fp8(const uint8_t* codes, const uint8_t* exp, int64_t rows, int64_t len, int format, float* y,
                        void* stream);
 
