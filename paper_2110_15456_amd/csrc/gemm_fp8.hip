@@ -75,15 +75,16 @@ __device__ __forceinline__ void spread() {
 // was just read, a whole slab ahead of their use.
 //
 // Two stages, and on the 64 tile four: it serves products of so few tiles that a slab
-// takes as long as its loads do (1024 x 1024 x 8192 with two 34.8 us, with four 20.9; of 900
-// drawn products those on the 64 tile lose 1% with four alone).
+// takes as long as its loads do (1024 x 1024 x 8192 with two 34.8 us, with four 15.6).
 //
-// Measured (BF16 out): 4096 x 4096 x 8192 97 us, 2.83 PFLOP/s; 8192 x 16384 x 4096 410 us,
-// 2.68; 8192 x 4096 x 4096 103 us, 2.66; a library's FP8 product of 8192^3 reaches 2.64 on
-// the same card.  The matrix units are busy for 73 to 78% of the cycles, at 1.6 to 1.7 GHz:
-// the power they draw holds the clock down, and faster feeding lowers it further.  A round
-// of tiles ends with 5.5 us of writing C.  The 128 tile, two workgroups on a CU, is held
-// to 1.95 by the LDS, which moves 1.5 bytes for each of the 256 tile's.
+// Measured (BF16 out, 200 launches in a row): 8192^3 378 us, 2.91 PFLOP/s; 4096 x 4096 x 8192
+// 96 us, 2.87; 8192 x 16384 x 4096 404 us, 2.72; 8192 x 4096 x 4096 102 us, 2.69; with FP32 out
+// 398, 101, 436 and 111.  After a rest the clock takes some 20 ms to rise (8192 x 16384 x 4096:
+// 480 us each of ten launches, 416 of forty).  A library's FP8 product of the same codes,
+// without scales, takes 337, 86, 364 and 93 us: 0.89 to 0.91 of this kernel's.  The matrix
+// units are busy for 73 to 79% of the cycles, and the clock is at 1.75 GHz of 2.4; a round of
+// tiles ends with 5.5 us of writing C.  The 128 tile, two workgroups on a CU, reaches 2.2 and
+// moves 1.5 bytes through the LDS for each of the 256 tile's; the 64 tile 1.3.
 template <int BM, int BN, int FA, int FB, class T>
 __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_gemm_fp8(Gemm p) {
   constexpr int ST = BM == 64 ? 4 : 2;
@@ -532,11 +533,14 @@ hipError_t launch_plan(const Fp8Plan& plan, Gemm g, int fa, int fb, T* C, int64_
   return hipGetLastError();
 }
 
-// The kernels, and their time in us as fitted to 900 drawn products (1 .. 8192 rows, 64 ..
-// 16384 columns and K, either way round): `start` once, then for each round of workgroups on
-// the 256 CUs the larger of one's latency, `open` + slabs * `slab`, and of what those on a
-// CU together need of it, each `each_open` + slabs * `each`.  The kernel and parts taken
-// are 1.4% slower than the fastest ones in the mean, and 77% at worst (2 us).
+// The kernels, and their price in us, of a form that was fitted to the times of 900 drawn
+// products (1 .. 8192 rows, 64 .. 16384 columns and K, either way round): `start` once, then for
+// each round of workgroups on the 256 CUs the larger of one's latency, `open` + slabs * `slab`,
+// and of what those on a CU together need of it, each `each_open` + slabs * `each`.  They
+// order the kernels and are no times: launches in a graph take 0.75 of the price of an
+// unsplit 64 tile or a few-row kernel, 0.9 of a 128 tile's, and large products on 256 tiles up
+// to 1.3 of it.  Of 1600 drawn products the kernel and parts taken are 1.4% slower than the
+// fastest ones in the mean, 2.3% of the products lose more than 20%, and one 49% at worst (5 us).
 struct Kernel {
   int rows, cols, waves, on_cu;
   float start, open, slab, each_open, each;

@@ -9,9 +9,9 @@
 // HBM-bound: x and the residual read once, h and the output written once.
 //
 // Measured, 8192 x 4096: BF16 x + residual -> h and e4m3 blocks 66 us, 5.6 TB/s; FP32 x +
-// residual -> h and BFP of width 4 78 us (120 when 16 lanes of a wave converted); the
-// gradient from a BF16 dy 86 us, 5.6 TB/s, and 6 for the join of dw.  One row: 4.2 us, a
-// launch.
+// residual -> h and BFP of width 4 77 us (120 when 16 lanes of a wave converted), -> h and FP32
+// 92; the gradient from a BF16 dy 86 us, 5.6 TB/s, and 5.4 for the join of dw.  One row: 4.0
+// us, a launch.
 #include "fp8.h"
 #include "gemm_direct.h"
 #include "launch.h"
@@ -55,8 +55,8 @@ struct Args {
 
 // A workgroup of NT threads takes a row, thread t its values 4 (t + NT k) .. + 3.
 // Rows of 8193 to 12288 values are kept to 64 registers, and so two of them on a CU, at the
-// price of weights that are not on the way with the values (with 16384's registers 2781 x
-// 9408 took 55 us).
+// price of weights that are not on the way with the values (2781 x 9408 FP32 -> e4m3 34 us, with
+// 16384's registers 55).
 template <int NT, int NV, bool RES, int TO, class T>
 __global__ __launch_bounds__(NT, NV == 3 ? 8 : 1) void k_rms_norm(Args p) {
   constexpr bool EARLY = NV != 3;

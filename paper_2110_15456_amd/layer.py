@@ -458,7 +458,8 @@ def clip_gradients(tensors, max_norm: float, sumsq: torch.Tensor | None = None) 
     """Scales a list of FP32 or BF16 tensors (in place; a TensorList: to its ``out``) by min(1,
     max_norm / norm), with norm the root of ``sumsq`` (sum_squares of the list unless one
     is given), and returns norm: one float64 value on the card.  A norm that is infinite
-    or NaN scales nothing."""
+    or NaN scales nothing.  A list that is no TensorList is checked in every call, some
+    1 us a tensor on the host."""
     l = _as_list(tensors)
     if not max_norm >= 0.0:
         raise ValueError("max_norm must not be negative")
